@@ -211,7 +211,7 @@ def prepare(case, seed):
         state["out"] = {k: torch.empty((t, h), device="cuda", dtype=dt) for k in ("x_out", "n")}
         state["out"] |= {k: torch.empty(t, device="cuda") for k in ("rstd_post", "rstd_pre")}
     else:
-        ctx.reserve_block_norm(t, h, _groups(case))
+        ctx.reserve_block_norm(t, h)
         state["out"] = like("y", "w_post", "w_pre", "gate") | {"dx": torch.empty((t, h), device="cuda", dtype=dt)}
     return state
 
