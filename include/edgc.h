@@ -16,6 +16,9 @@
  *      error-feedback residual stored as E or kept as D plus the factors
  *      ("deferred"), and the compress as one call or in the two phases between
  *      which a data-parallel step exchanges P
+ *   6. the operators of the block whose gradients go through the above: the
+ *      global norm of the gradients and their clipping, the norms before and
+ *      after a block fused with its gate and residual scale, with their backward
  *
  * Conventions
  *   - Every function returns an edgc_status (0 = OK, < 0 = error).  No C++
@@ -23,7 +26,7 @@
  *   - "device" pointers are HIP device memory on the context's GPU, owned by
  *     the caller; "host" pointers are ordinary process memory.  The library
  *     allocates device memory only in edgc_create (scratch) and frees it in
- *     edgc_destroy (and, for batches, in edgc_reserve_batch).  Hot calls
+ *     edgc_destroy (and, for batches and blocks, in edgc_reserve_*).  Hot calls
  *     never allocate, never free and never
  *     synchronise the stream; they only enqueue work on `hip_stream`
  *     (a hipStream_t passed as void*, NULL = the default stream).
@@ -469,6 +472,75 @@ int edgc_entropy_estimate_noalloc(edgc_ctx* ctx, const void* grad, edgc_dtype dt
                                   uint32_t bins, const float* range_lo_hi_or_null,
                                   edgc_entropy_result* out, uint64_t* counts_out_or_null,
                                   void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * 6. The block around the compressor.
+ *
+ * Global norm and clipping, on the descriptors of the batched calls (of which
+ * they read grad, ld, grad_out, ld_out, m and n; no reservation is needed and
+ * a tensor may have any shape):
+ *     S = sum over the list of grad^2,   norm = sqrt(S),
+ *     c = min(1, max_norm / (norm + 1e-6)), or 1 where norm is not finite,
+ *     grad_out = round_dtype(c * grad)
+ * Squares and sums are in 64 bits, in a fixed order: the same list gives the
+ * same bits.  After a decompress, grad and grad_out are both the decompressed
+ * gradient (in place; with c = 1 nothing is then written).
+ *   edgc_grad_sumsq_batch: S -> *sumsq (device double; NULL: a place of the
+ *     context's own); accumulate != 0 adds to what is there, for lists of both
+ *     dtypes.  Between the two calls a sharded job sums S over its ranks.
+ *   edgc_clip_batch: reads S from where the first call put it, clips, and
+ *     writes {norm, c} to norm_coef (device float[2], or NULL).  A norm that is
+ *     not finite (an element was Inf or NaN) hands the gradients on as they
+ *     are: the caller sees it in norm_coef[0].
+ * Errors: EDGC_EINVAL for a null or misaligned pointer, an empty tensor, a
+ * leading dimension below n or over 2^40, two leading dimensions for a
+ * gradient clipped in place, max_norm that is not positive and finite.
+ * ------------------------------------------------------------------------ */
+int edgc_grad_sumsq_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count,
+                          edgc_dtype dtype, int accumulate, double* sumsq, void* hip_stream);
+int edgc_clip_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype,
+                    double max_norm, const double* sumsq, float* norm_coef, void* hip_stream);
+
+/* Norms before and after a block, with its gate and residual scale in between:
+ * what stands between one block's output y and the next block's input n.
+ *     forward:  yh = y * rstd_post,   rstd_post = (mean(y^2) + eps)^(-1/2)
+ *               x_out = x + scale * gate * (yh * w_post)
+ *               n = x_out * rstd_pre * w_pre,  rstd_pre = (mean(x_out^2) + eps)^(-1/2)
+ * x, y, x_out, n: tokens x hidden of dtype, dense.  w_post, w_pre: hidden.
+ * gate: ceil(tokens / rows_per_gate) x hidden, or NULL for 1: token t has row
+ * t / rows_per_gate (rows_per_gate = tokens: one gate; the length of a
+ * sequence: one for each; 1: one for each token).  rstd_*: fp32[tokens], for
+ * the backward pass, or NULL.
+ * Either norm may be left out: y = NULL (before the first block; then w_post
+ * and gate are NULL, and x_out may be) or w_pre = NULL (no n).  x_out may be
+ * the same buffer as x or y, n_out the same as y.
+ *     backward: u = dn * w_pre,  xh = x_out * rstd_pre
+ *               dx = dx_out + rstd_pre * (u - xh * mean(u * xh))
+ *               v = scale * gate * w_post * dx,  dy = rstd_post * (v - yh * mean(v * yh))
+ *               dw_pre = sum over tokens of dn * xh
+ *               dgate = scale * w_post * (sum over the gate row's tokens of dx * yh)
+ *               dw_post = scale * (sum over tokens of gate * dx * yh)
+ * dx is also the gradient of x.  dx may be the same buffer as dx_out, dy the
+ * same as dn or y.  dx_out may be NULL where y is (it then counts as zero).
+ * Arithmetic and sums are fp32 for either dtype, in a fixed order; every
+ * output is rounded once.  The backward pass needs scratch: reserve it for the
+ * largest tokens and hidden (it synchronises the device; not a hot call).
+ * tokens = 0 does nothing (backward: the weight gradients become zero).
+ * Errors: EDGC_EINVAL for null or misaligned pointers, hidden = 0 or over
+ * 16384, tokens over 2^31, rows_per_gate = 0 with a gate, a scale that is not
+ * finite, an eps below zero, or sizes over the reservation. */
+int edgc_reserve_block_norm(edgc_ctx* ctx, uint32_t tokens, uint32_t hidden);
+int edgc_block_norm_forward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, uint32_t hidden,
+                            const void* x, const void* y, const void* w_post, const void* gate,
+                            uint64_t rows_per_gate, const void* w_pre, float scale, float eps,
+                            void* x_out, void* n_out, float* rstd_post, float* rstd_pre,
+                            void* hip_stream);
+int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, uint32_t hidden,
+                             const void* dx_out, const void* dn, const void* x_out, const void* y,
+                             const void* w_post, const void* gate, uint64_t rows_per_gate,
+                             const void* w_pre, const float* rstd_post, const float* rstd_pre,
+                             float scale, void* dx, void* dy, void* dw_post, void* dgate,
+                             void* dw_pre, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -129,6 +129,18 @@ def load_library() -> C.CDLL:
     L.edgc_compress.argtypes = [vp, vp, i32, u32, u32, u64, vp, i32, vp, u32, vp, u32, u32, u32, vp]
     L.edgc_decompress.restype = i32
     L.edgc_decompress.argtypes = [vp, vp, u32, vp, u32, u32, u32, u32, vp, vp, i32, u64, vp]
+    f32 = C.c_float
+    L.edgc_grad_sumsq_batch.restype = i32
+    L.edgc_grad_sumsq_batch.argtypes = [vp, C.POINTER(_Tensor), u32, i32, i32, vp, vp]
+    L.edgc_clip_batch.restype = i32
+    L.edgc_clip_batch.argtypes = [vp, C.POINTER(_Tensor), u32, i32, C.c_double, vp, vp, vp]
+    L.edgc_reserve_block_norm.restype = i32
+    L.edgc_reserve_block_norm.argtypes = [vp, u32, u32]
+    L.edgc_block_norm_forward.restype = i32
+    L.edgc_block_norm_forward.argtypes = [vp, i32, u64, u32, vp, vp, vp, vp, u64, vp, f32, f32, vp, vp, vp, vp, vp]
+    L.edgc_block_norm_backward.restype = i32
+    L.edgc_block_norm_backward.argtypes = [vp, i32, u64, u32, vp, vp, vp, vp, vp, vp, u64, vp, vp, vp, f32, vp, vp, vp, vp,
+                                           vp, vp]
     _lib = L
     return L
 
@@ -345,6 +357,21 @@ def _stream_handle(stream) -> int:
     if _raw_stream is not None and torch.cuda.is_initialized():
         return _raw_stream()
     return int(torch.cuda.current_stream().cuda_stream)
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _check_dense(dtype, shape, **tensors) -> None:
+    """Every given tensor is contiguous, of that dtype and of that shape."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}")
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous of shape {shape}")
 
 
 class PreparedBatch:
@@ -599,3 +626,70 @@ class Context:
         rc = self._L.edgc_residual_materialize_batch(self._h, arr, len(tensors), code, r,
                                                      _stream_handle(stream))
         self._check(rc, "edgc_residual_materialize_batch")
+
+    # -- the block around the compressor --------------------------------------
+    def grad_sumsq_batch(self, tensors: Sequence[Tensor], sumsq=None, accumulate: bool = False, stream=None) -> None:
+        """edgc_grad_sumsq_batch: the sum of squares of the tensors' ``grad``, into ``sumsq`` (a float64 CUDA tensor of one
+        element; None: the context's own place); ``accumulate`` adds to what is there."""
+        if sumsq is not None and (sumsq.dtype != (_torch or _load_torch()).float64 or sumsq.numel() != 1):
+            raise TypeError("sumsq must be one float64")
+        arr, code = self._marshal(tensors)
+        rc = self._L.edgc_grad_sumsq_batch(self._h, arr, len(tensors), code, 1 if accumulate else 0, _ptr(sumsq),
+                                           _stream_handle(stream))
+        self._check(rc, "edgc_grad_sumsq_batch")
+
+    def clip_batch(self, tensors: Sequence[Tensor], max_norm: float, norm_coef=None, sumsq=None, stream=None) -> None:
+        """edgc_clip_batch: ``grad_out`` = coefficient * ``grad``, by the sum of squares of the last
+        :meth:`grad_sumsq_batch` (or ``sumsq``); ``norm_coef`` (float32 CUDA tensor of two) receives the norm and the
+        coefficient."""
+        torch = _torch or _load_torch()
+        if sumsq is not None and (sumsq.dtype != torch.float64 or sumsq.numel() != 1):
+            raise TypeError("sumsq must be one float64")
+        if norm_coef is not None and (norm_coef.dtype != torch.float32 or norm_coef.numel() != 2 or not norm_coef.is_contiguous()):
+            raise TypeError("norm_coef must be two float32")
+        arr, code = self._marshal(tensors)
+        rc = self._L.edgc_clip_batch(self._h, arr, len(tensors), code, float(max_norm), _ptr(sumsq), _ptr(norm_coef),
+                                     _stream_handle(stream))
+        self._check(rc, "edgc_clip_batch")
+
+    def reserve_block_norm(self, tokens: int, hidden: int) -> None:
+        """edgc_reserve_block_norm: scratch of :meth:`block_norm_backward` for up to that many tokens and hidden units."""
+        self._check(self._L.edgc_reserve_block_norm(self._h, tokens, hidden), "edgc_reserve_block_norm")
+
+    @staticmethod
+    def _norm_shapes(x, gate, rows_per_gate, dense, vectors):
+        if x.dim() != 2:
+            raise ValueError("activations must be tokens x hidden")
+        t, h = x.shape
+        _check_dense(x.dtype, (t, h), **dense)
+        _check_dense(x.dtype, (h,), **vectors)
+        if gate is not None:
+            if rows_per_gate < 1:
+                raise ValueError("rows_per_gate must be >= 1 with a gate")
+            _check_dense(x.dtype, (-(-t // rows_per_gate), h), gate=gate)
+        return t, h
+
+    def block_norm_forward(self, x, y, w_post, gate, w_pre, x_out, n_out, rstd_post=None, rstd_pre=None, scale: float = 1.0,
+                           eps: float = 1e-6, rows_per_gate: int = 0, stream=None) -> None:
+        """edgc_block_norm_forward: x_out = x + scale * gate * (norm(y) * w_post), n_out = norm(x_out) * w_pre; tokens x hidden.
+        ``y`` None: the norm before a block alone; ``w_pre`` None: the norm after it alone."""
+        t, h = self._norm_shapes(x, gate, rows_per_gate, dict(x=x, y=y, x_out=x_out, n_out=n_out), dict(w_post=w_post, w_pre=w_pre))
+        _check_dense((_torch or _load_torch()).float32, (t,), rstd_post=rstd_post, rstd_pre=rstd_pre)
+        rc = self._L.edgc_block_norm_forward(self._h, _dtype_code(x), t, h, x.data_ptr(), _ptr(y), _ptr(w_post), _ptr(gate),
+                                             rows_per_gate, _ptr(w_pre), scale, eps, _ptr(x_out), _ptr(n_out), _ptr(rstd_post),
+                                             _ptr(rstd_pre), _stream_handle(stream))
+        self._check(rc, "edgc_block_norm_forward")
+
+    def block_norm_backward(self, dx_out, dn, x_out, y, w_post, gate, w_pre, rstd_post, rstd_pre, dx, dy, dw_post, dgate, dw_pre,
+                            scale: float = 1.0, rows_per_gate: int = 0, stream=None) -> None:
+        """edgc_block_norm_backward: the gradients of what :meth:`block_norm_forward` computed, from those of x_out and n_out."""
+        t, h = self._norm_shapes(dx, gate, rows_per_gate, dict(dx_out=dx_out, dn=dn, x_out=x_out, y=y, dx=dx, dy=dy),
+                                 dict(w_post=w_post, w_pre=w_pre, dw_post=dw_post, dw_pre=dw_pre))
+        _check_dense((_torch or _load_torch()).float32, (t,), rstd_post=rstd_post, rstd_pre=rstd_pre)
+        if gate is not None:
+            _check_dense(dx.dtype, tuple(gate.shape), dgate=dgate)
+        rc = self._L.edgc_block_norm_backward(self._h, _dtype_code(dx), t, h, _ptr(dx_out), _ptr(dn), _ptr(x_out), _ptr(y),
+                                              _ptr(w_post), _ptr(gate), rows_per_gate, _ptr(w_pre), _ptr(rstd_post),
+                                              _ptr(rstd_pre), scale, dx.data_ptr(), _ptr(dy), _ptr(dw_post), _ptr(dgate),
+                                              _ptr(dw_pre), _stream_handle(stream))
+        self._check(rc, "edgc_block_norm_backward")

@@ -12,12 +12,11 @@ namespace edgc {
 const char* const kKernelNames[KID_COUNT] = {
     "k_set_range", "k_minmax", "k_hist", "k_sample_indices", "k_init_q", "k_pass_p",
     "k_reduce_gram", "k_gram_sum", "k_chol", "k_apply", "k_pass_q", "k_reduce_q", "k_decompress",
-    "k_pass_p_deferred", "k_wide_hist", "k_wide_reduce", "k_estimate_one"};
+    "k_pass_p_deferred", "k_wide_hist", "k_wide_reduce", "k_estimate_one", "k_grad_sumsq", "k_clip",
+    "k_norm_forward", "k_norm_backward", "k_norm_sum"};
 }
 
 namespace {
-
-bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 template <typename T>
 hipError_t dev_alloc(T** p, size_t count)
@@ -98,7 +97,10 @@ extern "C" int edgc_create(edgc_ctx** out, int hip_device, uint32_t max_bins, ui
     auto place = [&](size_t bytes) { const size_t at = used; used += (bytes + 255) / 256 * 256; return at; };
     const size_t at_ticket = place(kTicketWords * sizeof(unsigned int));
     const size_t at_wide = place(65536 * sizeof(unsigned long long));
+    const size_t at_sumsq_ticket = place(sizeof(unsigned int));
     const size_t zeroed = used;
+    const size_t at_sumsq = place(sizeof(double));
+    const size_t at_sumsq_part = place(kMaxReduceBlocks * sizeof(double));
     const size_t at_mm = place(2 * kMaxReduceBlocks * sizeof(float));
     const size_t at_copies = place(8 * kCopyBins * sizeof(uint32_t));
     const size_t at_counts = place(static_cast<size_t>(max_bins) * sizeof(unsigned long long));
@@ -117,6 +119,9 @@ extern "C" int edgc_create(edgc_ctx** out, int hip_device, uint32_t max_bins, ui
     s.gram = reinterpret_cast<double*>(s.small + at_gram);
     s.rinv = reinterpret_cast<double*>(s.small + at_rinv);
     s.occupied = reinterpret_cast<uint32_t*>(s.small + at_occupied);
+    s.sumsq = reinterpret_cast<double*>(s.small + at_sumsq);
+    s.sumsq_part = reinterpret_cast<double*>(s.small + at_sumsq_part);
+    s.sumsq_ticket = reinterpret_cast<unsigned int*>(s.small + at_sumsq_ticket);
     ok = ok && dev_alloc(&s.part16, static_cast<size_t>(s.part16_blocks) * 65536) == hipSuccess;
     ok = ok && dev_alloc(&s.part, s.part_elems) == hipSuccess;
     ok = ok && dev_alloc(&s.gram_part, s.gram_part_elems) == hipSuccess;
@@ -206,6 +211,7 @@ extern "C" int edgc_destroy(edgc_ctx* ctx)
     (void)hipDeviceSynchronize();
     for (hipEvent_t e : ctx->prof.pool) (void)hipEventDestroy(e);
     free_batch(ctx);
+    if (ctx->norm.part) (void)hipFree(ctx->norm.part);
     free_scratch(ctx->s);
     delete ctx;
     return EDGC_OK;

@@ -24,6 +24,10 @@ struct Scratch {
     unsigned long long* wide         = nullptr;  // [65536] 64-bit credits per key, zero between calls
     unsigned long long* counts       = nullptr;  // [max_bins] histogram when the caller gives none
     void*               result_dev   = nullptr;  // edgc_entropy_result
+    // gradient norm
+    double*             sumsq        = nullptr;  // the sum of squares, for callers without a place of their own
+    double*             sumsq_part   = nullptr;  // [kMaxReduceBlocks] per block
+    unsigned int*       sumsq_ticket = nullptr;  // last-block ticket, zero between calls
     // compress / decompress
     float*  part      = nullptr;   // split-K partial factors [S][rows][rank_pad]
     size_t  part_elems = 0;
@@ -54,6 +58,8 @@ constexpr size_t rinv_elems(uint32_t max_rank)
 // Largest row count, column count or leading dimension of a compressed matrix: the kernels keep
 // lane offsets of up to four rows (4 * leading dimension + column) in 32 bits.
 constexpr uint64_t kMaxDim = 1ull << 28;
+// Largest leading dimension of the calls that keep element offsets in 64 bits
+constexpr uint64_t kMaxSpan = 1ull << 40;
 
 // ---------------------------------------------------------------------------
 // Grouped launches of the compressor.  Every compressor kernel works on a list of tensors:
@@ -115,11 +121,18 @@ struct BatchSlot {
     TensorScratch cap;
 };
 
+// Scratch of the block operators, of the sizes that edgc_reserve_block_norm has seen.
+struct NormScratch {
+    float*   part = nullptr;        // [blocks][4][hidden] column sums of the backward pass
+    uint32_t tokens = 0, hidden = 0;
+};
+
 // Kernel ids for the optional per-kernel event timing (edgc_profile_begin/end).
 enum KernelId {
     KID_SET_RANGE = 0, KID_MINMAX, KID_HIST, KID_SAMPLE_IDX, KID_INIT_Q, KID_PASS_P,
     KID_REDUCE_GRAM, KID_GRAM_SUM, KID_CHOL, KID_APPLY, KID_PASS_Q, KID_REDUCE_Q, KID_DECOMPRESS,
-    KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_COUNT
+    KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
+    KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 
@@ -166,11 +179,14 @@ struct edgc_ctx {
                                             // (on more than 16384 bins: from half of it on)
     edgc::Scratch s;
     std::vector<edgc::BatchSlot> batch;
+    edgc::NormScratch norm;
     edgc::Profiler prof;
     std::string last_error;
 };
 
 namespace edgc {
+
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 inline int fail(edgc_ctx* ctx, int code, const std::string& msg)
 {
