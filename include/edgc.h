@@ -18,7 +18,8 @@
  *      which a data-parallel step exchanges P
  *   6. the operators of the block whose gradients go through the above: the
  *      global norm of the gradients and their clipping, the norms before and
- *      after a block fused with its gate and residual scale, with their backward
+ *      after a block fused with its gate and residual scale, and the gated
+ *      feed-forward block, with their backward passes
  *
  * Conventions
  *   - Every function returns an edgc_status (0 = OK, < 0 = error).  No C++
@@ -541,6 +542,48 @@ int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, u
                              const void* w_pre, const float* rstd_post, const float* rstd_pre,
                              float scale, void* dx, void* dy, void* dw_post, void* dgate,
                              void* dw_pre, void* hip_stream);
+
+/* The gated feed-forward block, weights as torch.nn.Linear keeps them:
+ *     G = x w_gate^T,  U = x w_up^T,  A = act(G) * U,  y = A w_down^T
+ *     dA = dy w_down,  dG = dA * U * act'(G),  dU = dA * act(G)
+ *     dx = dG w_gate + dU w_up,  dw_gate = dG^T x,  dw_up = dU^T x,  dw_down = dy^T A
+ * x, y, dy, dx: tokens x hidden; G, U: tokens x ff; w_gate, w_up: ff x hidden;
+ * w_down: hidden x ff; all row-major of one dtype, with leading dimensions.
+ * Sums are in fp32.  With EDGC_BF16, A, dG and dU are rounded to bf16 once, as
+ * operands of the next product.  With EDGC_F32 operands are split into three
+ * bf16 planes that add up to them exactly, and six products are summed: the
+ * accuracy of fp32 products (an infinity may come out as NaN).
+ *   edgc_ff_forward: gate and up (both or neither) keep G and U for the
+ *     backward pass.
+ *   edgc_ff_backward: from the kept G and U; the weight gradients are
+ *     overwritten, or added to with accumulate != 0 (micro-batches).  They are
+ *     matrices as the batched calls take them.  No output may overlap an input.
+ * Both need scratch for the largest tokens and the widths at hand:
+ * edgc_reserve_ff (synchronises the device; not a hot call), with backward != 0
+ * for the second.  tokens = 0 does nothing (backward without accumulate: the
+ * weight gradients become zero).
+ * Errors: EDGC_EINVAL for null or misaligned pointers (multiples of the
+ * element's size are enough; 16-byte aligned rows of a multiple of 64 columns
+ * save a copy), hidden or ff 0 or over 2^20, tokens over 2^21, leading
+ * dimensions too small or over 2^40, or sizes over the reservation. */
+typedef enum { EDGC_SILU = 0, EDGC_GELU = 1, EDGC_GELU_TANH = 2 } edgc_act;
+typedef struct {
+    const void *w_gate, *w_up, *w_down;
+    uint64_t    ld_gate, ld_up, ld_down;
+    uint32_t    hidden, ff;
+    edgc_dtype  dtype;
+    edgc_act    act;
+} edgc_ff;
+int edgc_reserve_ff(edgc_ctx* ctx, edgc_dtype dtype, uint32_t tokens, uint32_t hidden, uint32_t ff,
+                    int backward);
+int edgc_ff_forward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ldx, uint32_t tokens,
+                    void* y, uint64_t ldy, void* gate, void* up, uint64_t ld_kept,
+                    void* hip_stream);
+int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ldx, uint32_t tokens,
+                     const void* gate, const void* up, uint64_t ld_kept, const void* dy,
+                     uint64_t ldy, void* dx, uint64_t lddx, void* dw_gate, uint64_t ld_dgate,
+                     void* dw_up, uint64_t ld_dup, void* dw_down, uint64_t ld_ddown,
+                     int accumulate, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -141,6 +141,12 @@ def load_library() -> C.CDLL:
     L.edgc_block_norm_backward.restype = i32
     L.edgc_block_norm_backward.argtypes = [vp, i32, u64, u32, vp, vp, vp, vp, vp, vp, u64, vp, vp, vp, f32, vp, vp, vp, vp,
                                            vp, vp]
+    L.edgc_reserve_ff.restype = i32
+    L.edgc_reserve_ff.argtypes = [vp, i32, u32, u32, u32, i32]
+    L.edgc_ff_forward.restype = i32
+    L.edgc_ff_forward.argtypes = [vp, C.POINTER(_FF), vp, u64, u32, vp, u64, vp, vp, u64, vp]
+    L.edgc_ff_backward.restype = i32
+    L.edgc_ff_backward.argtypes = [vp, C.POINTER(_FF), vp, u64, u32, vp, vp, u64, vp, u64, vp, u64, vp, u64, vp, u64, vp, u64, i32, vp]
     _lib = L
     return L
 
@@ -155,6 +161,12 @@ class _Tensor(C.Structure):
                 ("Q", C.c_void_p), ("P", C.c_void_p), ("ld", C.c_uint64), ("ld_out", C.c_uint64),
                 ("m", C.c_uint32), ("n", C.c_uint32), ("ldq", C.c_uint32), ("ldp", C.c_uint32),
                 ("residual_is_zero", C.c_int32), ("deferred", C.c_uint32)]
+
+
+class _FF(C.Structure):
+    _fields_ = [("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p), ("ld_gate", C.c_uint64),
+                ("ld_up", C.c_uint64), ("ld_down", C.c_uint64), ("hidden", C.c_uint32), ("ff", C.c_uint32),
+                ("dtype", C.c_int32), ("act", C.c_int32)]
 
 
 @dataclass
@@ -361,6 +373,37 @@ def _stream_handle(stream) -> int:
 
 def _ptr(t):
     return t.data_ptr() if t is not None else None
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _rows(name, t, dtype, shape) -> int:
+    """Leading dimension of a matrix of that dtype and shape whose rows are contiguous."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
+        raise ValueError(f"{name} must be of shape {shape} with contiguous rows that do not overlap")
+    return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+
+
+class FeedForward:
+    """The weights of a gated feed-forward block as the library takes them (edgc_ff): w_gate and w_up ff x hidden, w_down
+    hidden x ff, as torch.nn.Linear keeps them; ``act``: "silu", "gelu" or "gelu_tanh".  Pointers and shapes are those the
+    tensors had when it was built."""
+
+    def __init__(self, w_gate, w_up, w_down, act: str = "silu"):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+        if w_gate.dim() != 2:
+            raise ValueError("w_gate must be ff x hidden")
+        self.ff, self.hidden = (int(d) for d in w_gate.shape)
+        self.dtype, self.act = w_gate.dtype, act
+        self.weights = (w_gate, w_up, w_down)
+        lds = [_rows(n, w, self.dtype, s) for n, w, s in (("w_gate", w_gate, (self.ff, self.hidden)),
+                                                          ("w_up", w_up, (self.ff, self.hidden)),
+                                                          ("w_down", w_down, (self.hidden, self.ff)))]
+        self.c = _FF(*[w.data_ptr() for w in self.weights], *lds, self.hidden, self.ff, _dtype_code(w_gate), ACTIVATIONS[act])
 
 
 def _check_dense(dtype, shape, **tensors) -> None:
@@ -693,3 +736,41 @@ class Context:
                                               _ptr(rstd_pre), scale, dx.data_ptr(), _ptr(dy), _ptr(dw_post), _ptr(dgate),
                                               _ptr(dw_pre), _stream_handle(stream))
         self._check(rc, "edgc_block_norm_backward")
+
+    def reserve_ff(self, dtype, tokens: int, hidden: int, ff: int, backward: bool = False) -> None:
+        """edgc_reserve_ff: scratch of :meth:`ff_forward` (and :meth:`ff_backward`) for up to that many tokens of that
+        width; ``dtype``: torch.float32 or torch.bfloat16."""
+        if _torch is None:
+            _load_torch()
+        if dtype not in _codes:
+            raise TypeError("dtype must be float32 or bfloat16")
+        self._check(self._L.edgc_reserve_ff(self._h, _codes[dtype], tokens, hidden, ff, 1 if backward else 0), "edgc_reserve_ff")
+
+    def ff_forward(self, ff: FeedForward, x, y, gate=None, up=None, stream=None) -> None:
+        """edgc_ff_forward: y = (act(x w_gate^T) * (x w_up^T)) w_down^T; x, y tokens x hidden.  ``gate``, ``up`` (tokens x ff)
+        keep the two projections for :meth:`ff_backward`."""
+        t = x.shape[0]
+        ldx, ldy = _rows("x", x, ff.dtype, (t, ff.hidden)), _rows("y", y, ff.dtype, (t, ff.hidden))
+        ldk = 0
+        if gate is not None and up is not None:
+            ldk = _rows("gate", gate, ff.dtype, (t, ff.ff))
+            if _rows("up", up, ff.dtype, (t, ff.ff)) != ldk:
+                raise ValueError("gate and up must have one row stride")
+        rc = self._L.edgc_ff_forward(self._h, C.byref(ff.c), x.data_ptr(), ldx, t, y.data_ptr(), ldy, _ptr(gate), _ptr(up), ldk,
+                                     _stream_handle(stream))
+        self._check(rc, "edgc_ff_forward")
+
+    def ff_backward(self, ff: FeedForward, x, gate, up, dy, dx, dw_gate, dw_up, dw_down, accumulate: bool = False,
+                    stream=None) -> None:
+        """edgc_ff_backward: the gradients of x and of the three weights from dy, x and the kept projections; ``accumulate``
+        adds the weights' gradients to what is there."""
+        t, dt, th, tf = x.shape[0], ff.dtype, (x.shape[0], ff.hidden), (x.shape[0], ff.ff)
+        ldk = _rows("gate", gate, dt, tf)
+        if _rows("up", up, dt, tf) != ldk:
+            raise ValueError("gate and up must have one row stride")
+        rc = self._L.edgc_ff_backward(
+            self._h, C.byref(ff.c), x.data_ptr(), _rows("x", x, dt, th), t, gate.data_ptr(), up.data_ptr(), ldk, dy.data_ptr(),
+            _rows("dy", dy, dt, th), dx.data_ptr(), _rows("dx", dx, dt, th), dw_gate.data_ptr(),
+            _rows("dw_gate", dw_gate, dt, (ff.ff, ff.hidden)), dw_up.data_ptr(), _rows("dw_up", dw_up, dt, (ff.ff, ff.hidden)),
+            dw_down.data_ptr(), _rows("dw_down", dw_down, dt, (ff.hidden, ff.ff)), 1 if accumulate else 0, _stream_handle(stream))
+        self._check(rc, "edgc_ff_backward")

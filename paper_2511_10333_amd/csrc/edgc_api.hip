@@ -13,7 +13,8 @@ const char* const kKernelNames[KID_COUNT] = {
     "k_set_range", "k_minmax", "k_hist", "k_sample_indices", "k_init_q", "k_pass_p",
     "k_reduce_gram", "k_gram_sum", "k_chol", "k_apply", "k_pass_q", "k_reduce_q", "k_decompress",
     "k_pass_p_deferred", "k_wide_hist", "k_wide_reduce", "k_estimate_one", "k_grad_sumsq", "k_clip",
-    "k_norm_forward", "k_norm_backward", "k_norm_sum"};
+    "k_norm_forward", "k_norm_backward", "k_norm_sum", "k_ff_pack", "k_ff_gate", "k_ff_down", "k_ff_dgate", "k_ff_dx",
+    "k_ff_dw", "k_ff_sum"};
 }
 
 namespace {
@@ -129,6 +130,7 @@ extern "C" int edgc_create(edgc_ctx** out, int hip_device, uint32_t max_bins, ui
     ok = ok && hipMemset(s.small, 0, zeroed) == hipSuccess;
     ok = ok && hipDeviceSynchronize() == hipSuccess;
     ok = ok && prepare_entropy_kernels(ctx) == EDGC_OK && prepare_compress_kernels(ctx) == EDGC_OK;
+    ok = ok && prepare_ff_kernels(ctx) == EDGC_OK;
     ok = ok && resolve_static_scratch(ctx) == EDGC_OK;
     if (!ok) {
         (void)hipGetLastError();
@@ -211,7 +213,8 @@ extern "C" int edgc_destroy(edgc_ctx* ctx)
     (void)hipDeviceSynchronize();
     for (hipEvent_t e : ctx->prof.pool) (void)hipEventDestroy(e);
     free_batch(ctx);
-    if (ctx->norm.part) (void)hipFree(ctx->norm.part);
+    for (void* p : {static_cast<void*>(ctx->norm.part), ctx->ff.ws, static_cast<void*>(ctx->ff.part)})
+        if (p) (void)hipFree(p);
     free_scratch(ctx->s);
     delete ctx;
     return EDGC_OK;

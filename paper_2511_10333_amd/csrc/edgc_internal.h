@@ -127,12 +127,20 @@ struct NormScratch {
     uint32_t tokens = 0, hidden = 0;
 };
 
+// Scratch of the feed-forward block (edgc_reserve_ff).
+struct FfScratch {
+    void*    ws = nullptr;          // operands, 16 bits each
+    float*   part = nullptr;        // partial sums of products that are split along k
+    uint64_t elems = 0;
+};
+
 // Kernel ids for the optional per-kernel event timing (edgc_profile_begin/end).
 enum KernelId {
     KID_SET_RANGE = 0, KID_MINMAX, KID_HIST, KID_SAMPLE_IDX, KID_INIT_Q, KID_PASS_P,
     KID_REDUCE_GRAM, KID_GRAM_SUM, KID_CHOL, KID_APPLY, KID_PASS_Q, KID_REDUCE_Q, KID_DECOMPRESS,
     KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
-    KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_COUNT
+    KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_FF_PACK,
+    KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_SUM, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 
@@ -180,6 +188,7 @@ struct edgc_ctx {
     edgc::Scratch s;
     std::vector<edgc::BatchSlot> batch;
     edgc::NormScratch norm;
+    edgc::FfScratch ff;
     edgc::Profiler prof;
     std::string last_error;
 };
@@ -327,6 +336,7 @@ struct CopyList {
 int launch_decompress(edgc_ctx* ctx, Group& g, CopyList& copies, edgc_dtype dt, hipStream_t st);
 int prepare_compress_kernels(edgc_ctx* ctx);
 int prepare_entropy_kernels(edgc_ctx* ctx);
+int prepare_ff_kernels(edgc_ctx* ctx);          // ff.hip
 size_t compress_part_elems(uint64_t max_rows, uint64_t max_cols, uint32_t max_rank, int num_cu);
 
 // the P-pass of groups made of whole tiles only (pass_p_full.hip)

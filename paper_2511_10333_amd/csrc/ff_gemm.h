@@ -1,0 +1,331 @@
+// The matrix products of the gated feed-forward block: C[m][n] = sum over segments and k of A[m][k] B[n][k], both operands bf16 with
+// k contiguous, 16-byte aligned rows and k padded with zeros to whole tiles of 64.
+//
+// fp32 operands come as three bf16 planes that add up to them exactly (24 significant bits = 3 x 8: a plane is the value's leading
+// bits, cut off, not rounded); six products of planes, 2^-24 of the operands left out, are six segments of one sum.  Six bf16 MFMAs
+// take less time than one of fp32 (2.5e15 / 6 against 0.16e15 operations a second).
+//
+// A block of WM x WN waves makes a BM x BN tile from two LDS buffers of 64 k each: the next tile's rows are on their way to
+// registers while the current one is multiplied.  A row of 128 bytes lies in LDS as eight 16-byte units, unit c at c ^ (row & 7),
+// so that the 32 rows of a fragment are read without bank conflicts.  The MFMA's first operand is B: a lane then holds four
+// neighbouring n of one m, which is what the epilogues load and store.
+#pragma once
+
+#include "compress_common.h"
+
+namespace edgc {
+
+constexpr int kFfBk = 64;               // k of a tile
+constexpr int kFfSegs = 12;
+constexpr uint64_t kFfMaxLd = 1ull << 22;   // rows of a tile are addressed in 32 bits from its first
+
+struct FfProblem {
+    const uint16_t* a[kFfSegs];         // per segment
+    const uint16_t* b[kFfSegs];
+    const uint16_t* b2[kFfSegs];        // the gated form: the second matrix of the same shape as b
+    uint64_t lda, ldb;                  // elements
+    uint32_t M, N;                      // of the output (gated: N columns of each of the two)
+    uint32_t ktiles, nseg;              // tiles of a segment; segments
+    uint32_t tiles_m, tiles_n, first;   // tiles of the output; first block
+    uint32_t accumulate;
+    void* out;                          // store: the output; gate, dgate: planes of h
+    uint64_t ldo;
+    // gate: h -> out, the projections -> e0, e1 where given.  dgate: the projections <- e0, e1; their gradients' planes -> o1, o2
+    void *e0, *e1, *o1, *o2;
+    uint64_t lde;
+    uint64_t plane;                     // elements between planes of out, o1, o2
+    uint32_t n_pad;                     // columns of out, o1, o2: those from N on are zeros
+    int32_t act;
+};
+constexpr int kFfProblems = 3;
+struct FfArgs {
+    FfProblem p[kFfProblems];
+    uint32_t count, splits;             // problems; ways the k tiles are split (partial sums: out is [splits][M][N])
+    uint32_t blocks;                    // of one split
+};
+
+enum FfEpi { kFfStore = 0, kFfGate = 1, kFfDgate = 2, kFfPartial = 3 };
+
+// Activation and derivative.  gelu_tanh by the identity (1 + tanh t) / 2 = 1 / (1 + exp(-2 t)).
+__device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
+{
+    if (act == EDGC_SILU) {
+        const float s = 1.0f / (1.0f + expf(-z));
+        a = z * s;
+        da = s * (1.0f + z * (1.0f - s));
+    } else if (act == EDGC_GELU) {
+        const float cdf = 0.5f * erfcf(z * -0.70710678118654752f);
+        a = z * cdf;
+        da = cdf + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    } else {
+        const float k = 0.79788456080286536f, c = 0.044715f;
+        const float s = 1.0f / (1.0f + expf(-2.0f * k * (z + c * z * z * z)));
+        a = z * s;
+        da = s + 2.0f * k * z * s * (1.0f - s) * (1.0f + 3.0f * c * z * z);
+    }
+}
+
+// x = p[0] + p[1] + p[2] in bf16, exactly (unless its last bits lie below the smallest number).  What is not finite is plane 0 alone.
+__device__ __forceinline__ void ff_planes(float x, uint16_t (&p)[3])
+{
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        p[0] = static_cast<uint16_t>((u >> 16) | ((u & 0x7fffffu) ? 0x40u : 0u));
+        p[1] = p[2] = 0;
+        return;
+    }
+    const uint32_t h = u & 0xffff0000u;
+    const float r = x - __uint_as_float(h);
+    const uint32_t m = __float_as_uint(r) & 0xffff0000u;
+    p[0] = static_cast<uint16_t>(h >> 16);
+    p[1] = static_cast<uint16_t>(m >> 16);
+    p[2] = static_cast<uint16_t>(__float_as_uint(r - __uint_as_float(m)) >> 16);
+}
+
+// T's planes of four values, to planes `plane` elements apart
+template <typename T> struct FfType;
+template <> struct FfType<__bf16> {
+    static constexpr int kPlanes = 1;
+    static __device__ __forceinline__ void put4(uint16_t* to, uint64_t, const float (&v)[4])
+    {
+        uint32_t a[1], b[1];
+        pack_pair<1>(v[0], v[1], a);
+        pack_pair<1>(v[2], v[3], b);
+        put_any(to, Bf16Quad{a[0], b[0]});
+    }
+    static __device__ __forceinline__ Bf16Quad load4(const __bf16* p) { return at_any<Bf16Quad>(p); }
+    static __device__ __forceinline__ void widen(const Bf16Quad& q, float (&v)[4])
+    {
+        v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xffff0000u);
+        v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xffff0000u);
+    }
+    static __device__ __forceinline__ void store4(__bf16* p, const float (&v)[4]) { put4(reinterpret_cast<uint16_t*>(p), 0, v); }
+};
+template <> struct FfType<float> {
+    static constexpr int kPlanes = 3;
+    static __device__ __forceinline__ void put4(uint16_t* to, uint64_t plane, const float (&v)[4])
+    {
+        uint16_t q[4][3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ff_planes(v[i], q[i]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+            put_any(to + p * plane, Bf16Quad{q[0][p] | static_cast<uint32_t>(q[1][p]) << 16, q[2][p] | static_cast<uint32_t>(q[3][p]) << 16});
+    }
+    static __device__ __forceinline__ Floats4 load4(const float* p) { return at_any<Floats4>(p); }
+    static __device__ __forceinline__ void widen(const Floats4& q, float (&v)[4]) { v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; }
+    static __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { put_any(p, Floats4{v[0], v[1], v[2], v[3]}); }
+};
+// four neighbours of a row of n columns: what lies beyond is zero, and is not written
+template <typename T>
+__device__ __forceinline__ void ff_load4(const T* row, uint32_t n0, uint32_t n, float (&v)[4])
+{
+    if (n0 + 4 <= n) {
+        FfType<T>::widen(FfType<T>::load4(row + n0), v);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = n0 + i < n ? static_cast<float>(row[n0 + i]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void ff_store4(T* row, uint32_t n0, uint32_t n, const float (&v)[4])
+{
+    if (n0 + 4 <= n) {
+        FfType<T>::store4(row + n0, v);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (n0 + i < n) row[n0 + i] = static_cast<T>(v[i]);
+    }
+}
+
+// What becomes of four neighbouring sums of row m
+template <typename T, int EPI>
+__device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t split, uint32_t m, uint32_t n0, float (&v)[4], float (&v2)[4])
+{
+    if constexpr (EPI == kFfStore) {
+        T* const row = static_cast<T*>(p.out) + m * p.ldo;
+        if (p.accumulate) {
+            float o[4];
+            ff_load4<T>(row, n0, p.N, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += o[i];
+        }
+        ff_store4<T>(row, n0, p.N, v);
+    } else if constexpr (EPI == kFfPartial) {
+        float* const row = static_cast<float*>(p.out) + (static_cast<uint64_t>(split) * p.M + m) * p.N;
+        ff_store4<float>(row, n0, p.N, v);
+    } else if constexpr (EPI == kFfGate) {
+        float h[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            float a, da;
+            ff_act(p.act, v[i], a, da);
+            h[i] = n0 + i < p.N ? a * v2[i] : 0.f;
+        }
+        FfType<T>::put4(static_cast<uint16_t*>(p.out) + m * p.ldo + n0, p.plane, h);
+        if (p.e0) ff_store4<T>(static_cast<T*>(p.e0) + m * p.lde, n0, p.N, v);
+        if (p.e1) ff_store4<T>(static_cast<T*>(p.e1) + m * p.lde, n0, p.N, v2);
+    } else {
+        float g[4], u[4], dg[4], du[4], h[4];
+        ff_load4<T>(static_cast<const T*>(p.e0) + m * p.lde, n0, p.N, g);
+        ff_load4<T>(static_cast<const T*>(p.e1) + m * p.lde, n0, p.N, u);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            float a, da;
+            ff_act(p.act, g[i], a, da);
+            const bool in = n0 + i < p.N;
+            h[i] = in ? a * u[i] : 0.f;
+            dg[i] = in ? v[i] * u[i] * da : 0.f;
+            du[i] = in ? v[i] * a : 0.f;
+        }
+        const uint64_t at = m * p.ldo + n0;
+        FfType<T>::put4(static_cast<uint16_t*>(p.out) + at, p.plane, h);
+        FfType<T>::put4(static_cast<uint16_t*>(p.o1) + at, p.plane, dg);
+        FfType<T>::put4(static_cast<uint16_t*>(p.o2) + at, p.plane, du);
+    }
+}
+
+// Tile of a block: the blocks that the dispatcher places on one XCD (equal id modulo 8) take neighbouring tiles, columns of
+// kFfBand rows of tiles at a time, so that an XCD's L2 holds the operand rows that they share.
+constexpr uint32_t kFfBand = 8;
+__device__ __forceinline__ void ff_tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn)
+{
+    const uint32_t total = tiles_m * tiles_n, per = total / 8, rest = total % 8, xcd = id % 8, at = id / 8;
+    id = xcd * per + min(xcd, rest) + at;       // XCDs below `rest` have one more
+    const uint32_t band = id / (kFfBand * tiles_n), in = id - band * kFfBand * tiles_n;
+    const uint32_t rows = min(kFfBand, tiles_m - band * kFfBand);
+    tm = band * kFfBand + in % rows;
+    tn = in / rows;
+}
+
+template <int BM, int BN, int WM, int WN, typename T, int EPI>
+__global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
+{
+    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = BN / WN / 32;
+    constexpr int LA = BM * 8 / NTH, LB = BN * 8 / NTH;      // 16-byte units that a thread brings of either operand
+    constexpr bool GATED = EPI == kFfGate;
+    static_assert(!GATED || NI == 2, "a wave has 32 columns of either projection");
+    extern __shared__ __align__(16) unsigned char lds[];     // [2][(BM + BN) * 128]
+    constexpr uint32_t kBuf = (BM + BN) * 128;
+
+    const uint32_t split = blockIdx.x / args.blocks, bid = blockIdx.x - split * args.blocks;
+    uint32_t pi = 0;
+#pragma unroll
+    for (int i = 1; i < kFfProblems; ++i) pi += (static_cast<uint32_t>(i) < args.count && bid >= args.p[i].first) ? 1u : 0u;
+    const FfProblem& p = args.p[pi];
+    uint32_t tm, tn;
+    ff_tile_of(bid - p.first, p.tiles_m, p.tiles_n, tm, tn);
+    constexpr uint32_t COLS = GATED ? BN / 2 : BN;
+    const uint32_t m0 = tm * BM, n0 = tn * COLS;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, wm = wave / WN, wn = wave % WN;
+
+    // bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last)
+    uint32_t oa[LA], ob[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const uint32_t row = min(tid / 8 + i * (NTH / 8), p.M - 1 - m0);
+        oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + (tid % 8) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        uint32_t row = tid / 8 + i * (NTH / 8);
+        if constexpr (GATED) row = row / 64 * 32 + row % 32;        // rows 64 w .. + 31: the first matrix, + 32 .. 63: the second
+        row = min(row, p.N - 1 - n0);
+        ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + (tid % 8) * 16;
+    }
+    const uint32_t wat = (tid / 8) * 128 + (((tid % 8) ^ ((tid / 8) & 7)) * 16);        // rows NTH / 8 apart: the same unit
+    const bool second = GATED && (tid / 8) % 64 >= 32;                                  // (NTH / 8 is a multiple of 64 or 32: see below)
+
+    const uint32_t total = p.nseg * p.ktiles;
+    const uint32_t kt0 = static_cast<uint32_t>(static_cast<uint64_t>(total) * split / args.splits);
+    const uint32_t kt1 = static_cast<uint32_t>(static_cast<uint64_t>(total) * (split + 1) / args.splits);
+    uint32_t seg = kt0 / p.ktiles, kt = kt0 - seg * p.ktiles;
+    const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
+
+    u32x4 ra[LA], rb[LB];
+    auto bring = [&]() {
+        const unsigned char* pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_row0 + kt * kFfBk);
+        const unsigned char* pb = reinterpret_cast<const unsigned char*>(p.b[seg] + b_row0 + kt * kFfBk);
+        const unsigned char* pb2 = GATED ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_row0 + kt * kFfBk) : pb;
+#pragma unroll
+        for (int i = 0; i < LA; ++i) ra[i] = *reinterpret_cast<const u32x4*>(pa + oa[i]);
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const bool sec = GATED && (NTH / 8 == 32 ? (i & 1) : second);
+            rb[i] = *reinterpret_cast<const u32x4*>((sec ? pb2 : pb) + ob[i]);
+        }
+        if (++kt == p.ktiles) { kt = 0; ++seg; }
+    };
+    auto put = [&](uint32_t buf) {
+        unsigned char* const la = lds + buf * kBuf;
+#pragma unroll
+        for (int i = 0; i < LA; ++i) *reinterpret_cast<u32x4*>(la + wat + i * (NTH * 16)) = ra[i];
+#pragma unroll
+        for (int i = 0; i < LB; ++i) *reinterpret_cast<u32x4*>(la + BM * 128 + wat + i * (NTH * 16)) = rb[i];
+    };
+
+    f32x16 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    const uint32_t fr = lane & 31, fu = ((lane >> 5) ^ (fr & 7)) * 16;      // fragment row; its unit, to be xored with 2 k / 16
+    const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = BM * 128 + (wn * NI * 32 + fr) * 128 + fu;
+    auto multiply = [&](uint32_t buf) {
+        const unsigned char* const la = lds + buf * kBuf;
+#pragma unroll
+        for (int kk = 0; kk < kFfBk / 16; ++kk) {
+            bf16x8 fa[MI], fb[NI];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        }
+    };
+
+    if (kt0 < kt1) {
+        bring();
+        put(0);
+        __syncthreads();
+        uint32_t buf = 0;
+        for (uint32_t t = kt0 + 1; t < kt1; ++t) {
+            bring();
+            multiply(buf);
+            put(buf ^ 1);       // read last before the barrier that ended the tile before
+            __syncthreads();
+            buf ^= 1;
+        }
+        multiply(buf);
+    }
+
+    // lane: row m of a 32 x 32 square, columns 8 (v / 4) + 4 (lane / 32) + v % 4
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const uint32_t m = m0 + (wm * MI + i) * 32 + fr;
+        if (m >= p.M) continue;
+#pragma unroll
+        for (int j = 0; j < (GATED ? 1 : NI); ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t n = n0 + (GATED ? wn * 32 : (wn * NI + j) * 32) + 8 * q + 4 * (lane >> 5);
+                if (n >= ((EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N)) continue;
+                float v[4], v2[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = acc[i][j][4 * q + e];
+                    v2[e] = GATED ? acc[i][NI - 1][4 * q + e] : 0.f;
+                }
+                ff_epilogue<T, EPI>(p, split, m, n, v, v2);
+            }
+    }
+}
+
+}  // namespace edgc
