@@ -5,8 +5,8 @@
 // bits, cut off, not rounded); six products of planes, 2^-24 of the operands left out, are six segments of one sum.  Six bf16 MFMAs
 // take less time than one of fp32 (2.5e15 / 6 against 0.16e15 operations a second).
 //
-// A block of WM x WN waves makes a BM x BN tile from two LDS buffers of 64 k each: the next tile's rows are on their way to
-// registers while the current one is multiplied.  A row of 128 bytes lies in LDS as eight 16-byte units, unit c at c ^ (row & 7),
+// A block of WM x WN waves makes a BM x BN tile from two LDS buffers of 64 k each: the next tile's rows are on their way to one while
+// the other is multiplied.  A row of 128 bytes lies in LDS as eight 16-byte units, unit c at c ^ (row & 7),
 // so that the 32 rows of a fragment are read without bank conflicts.  The MFMA's first operand is B: a lane then holds four
 // neighbouring n of one m, which is what the epilogues load and store.
 #pragma once
@@ -199,13 +199,47 @@ __device__ __forceinline__ void ff_tile_of(uint32_t id, uint32_t tiles_m, uint32
     tn = in / rows;
 }
 
+// Shared memory's own addresses, for the instructions that take them
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef const __attribute__((address_space(1))) unsigned char global_byte;
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+// 16 bytes from each lane's address to 16 bytes per lane, one after the other, from `to` on
+__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned char* to)
+{
+    __builtin_amdgcn_global_load_lds((global_byte*)from, (lds_byte*)to, 16, 0, 0);
+}
+// The fragments of one step of 16 k: rows 32 apart, which lie 4096 bytes apart in LDS
+__device__ __forceinline__ void read_fragments(uint32_t at_a, uint32_t at_b, bf16x8 (&fa)[4], bf16x8 (&fb)[2])
+{
+    asm volatile("ds_read_b128 %0, %6\n\t"
+                 "ds_read_b128 %4, %7\n\t"
+                 "ds_read_b128 %1, %6 offset:4096\n\t"
+                 "ds_read_b128 %5, %7 offset:4096\n\t"
+                 "ds_read_b128 %2, %6 offset:8192\n\t"
+                 "ds_read_b128 %3, %6 offset:12288\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(fb[0]), "=&v"(fb[1])
+                 : "v"(at_a), "v"(at_b)
+                 : "memory");
+}
+__device__ __forceinline__ void slot_end()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int BM, int BN, int WM, int WN, typename T, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
 {
-    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = BN / WN / 32;
+    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = 2;
     constexpr int LA = BM * 8 / NTH, LB = BN * 8 / NTH;      // 16-byte units that a thread brings of either operand
-    constexpr bool GATED = EPI == kFfGate;
-    static_assert(!GATED || NI == 2, "a wave has 32 columns of either projection");
+    constexpr bool GATED = EPI == kFfGate, TURNS = WM * WN == 8;
+    static_assert(BN / WN == 64, "a wave has 64 columns; gated: 32 of either projection");
+    static_assert(NTH / 8 == 64 || NTH / 8 == 32, "rows of the two projections alternate by 32");
     extern __shared__ __align__(16) unsigned char lds[];     // [2][(BM + BN) * 128]
     constexpr uint32_t kBuf = (BM + BN) * 128;
 
@@ -218,52 +252,31 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
     ff_tile_of(bid - p.first, p.tiles_m, p.tiles_n, tm, tn);
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
     const uint32_t m0 = tm * BM, n0 = tn * COLS;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, wm = wave / WN, wn = wave % WN;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
 
-    // bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last)
+    // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last).  It brings unit
+    // tid % 8 of the LDS row tid / 8 and of the rows NTH / 8 apart from it, which is unit (tid % 8) ^ (row & 7) of the operand's row.
     uint32_t oa[LA], ob[LB];
+    const uint32_t unit = ((tid % 8) ^ ((tid / 8) & 7)) * 16;
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         const uint32_t row = min(tid / 8 + i * (NTH / 8), p.M - 1 - m0);
-        oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + (tid % 8) * 16;
+        oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + unit;
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
         uint32_t row = tid / 8 + i * (NTH / 8);
         if constexpr (GATED) row = row / 64 * 32 + row % 32;        // rows 64 w .. + 31: the first matrix, + 32 .. 63: the second
         row = min(row, p.N - 1 - n0);
-        ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + (tid % 8) * 16;
+        ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + unit;
     }
-    const uint32_t wat = (tid / 8) * 128 + (((tid % 8) ^ ((tid / 8) & 7)) * 16);        // rows NTH / 8 apart: the same unit
-    const bool second = GATED && (tid / 8) % 64 >= 32;                                  // (NTH / 8 is a multiple of 64 or 32: see below)
+    const bool second = GATED && NTH / 8 == 64 && wave >= 4;        // rows 32 .. 63 of every 64
 
     const uint32_t total = p.nseg * p.ktiles;
     const uint32_t kt0 = static_cast<uint32_t>(static_cast<uint64_t>(total) * split / args.splits);
     const uint32_t kt1 = static_cast<uint32_t>(static_cast<uint64_t>(total) * (split + 1) / args.splits);
     uint32_t seg = kt0 / p.ktiles, kt = kt0 - seg * p.ktiles;
     const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
-
-    u32x4 ra[LA], rb[LB];
-    auto bring = [&]() {
-        const unsigned char* pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_row0 + kt * kFfBk);
-        const unsigned char* pb = reinterpret_cast<const unsigned char*>(p.b[seg] + b_row0 + kt * kFfBk);
-        const unsigned char* pb2 = GATED ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_row0 + kt * kFfBk) : pb;
-#pragma unroll
-        for (int i = 0; i < LA; ++i) ra[i] = *reinterpret_cast<const u32x4*>(pa + oa[i]);
-#pragma unroll
-        for (int i = 0; i < LB; ++i) {
-            const bool sec = GATED && (NTH / 8 == 32 ? (i & 1) : second);
-            rb[i] = *reinterpret_cast<const u32x4*>((sec ? pb2 : pb) + ob[i]);
-        }
-        if (++kt == p.ktiles) { kt = 0; ++seg; }
-    };
-    auto put = [&](uint32_t buf) {
-        unsigned char* const la = lds + buf * kBuf;
-#pragma unroll
-        for (int i = 0; i < LA; ++i) *reinterpret_cast<u32x4*>(la + wat + i * (NTH * 16)) = ra[i];
-#pragma unroll
-        for (int i = 0; i < LB; ++i) *reinterpret_cast<u32x4*>(la + BM * 128 + wat + i * (NTH * 16)) = rb[i];
-    };
 
     f32x16 acc[MI][NI];
 #pragma unroll
@@ -275,56 +288,116 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
 
     const uint32_t fr = lane & 31, fu = ((lane >> 5) ^ (fr & 7)) * 16;      // fragment row; its unit, to be xored with 2 k / 16
     const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = BM * 128 + (wn * NI * 32 + fr) * 128 + fu;
-    auto multiply = [&](uint32_t buf) {
-        const unsigned char* const la = lds + buf * kBuf;
+
+    // the next tile of k, to buffer `buf`
+    auto bring = [&](uint32_t buf) {
+        const unsigned char* pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_row0 + kt * kFfBk);
+        const unsigned char* pb = reinterpret_cast<const unsigned char*>((second ? p.b2[seg] : p.b[seg]) + b_row0 + kt * kFfBk);
+        const unsigned char* pb2 = GATED && !second ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_row0 + kt * kFfBk) : pb;
+        unsigned char* const to = lds + buf * kBuf + wave * 1024;
 #pragma unroll
-        for (int kk = 0; kk < kFfBk / 16; ++kk) {
-            bf16x8 fa[MI], fb[NI];
+        for (int i = 0; i < LA; ++i) load_to_lds(pa + oa[i], to + i * (NTH * 16));
 #pragma unroll
-            for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
-#pragma unroll
-            for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-        }
+        for (int i = 0; i < LB; ++i)
+            load_to_lds((GATED && NTH / 8 == 32 && (i & 1) ? pb2 : pb) + ob[i], to + BM * 128 + i * (NTH * 16));
+        if (++kt == p.ktiles) { kt = 0; ++seg; }
     };
 
-    if (kt0 < kt1) {
-        bring();
-        put(0);
-        __syncthreads();
+    if constexpr (TURNS) {
+        // The waves take turns: of the two on a SIMD, one reads fragments (and asks for the next tile) while the other
+        // multiplies, and a barrier ends either's slot.  Wave group 1 is one slot behind group 0.  Tile t is read in slots 8 t to
+        // 8 t + 7; tile t + 1 is asked for in slots 8 t and 8 t + 1, into the buffer that was read last in slot 8 t - 1, and waited
+        // for before the barrier that ends slot 8 t + 7.
+        const bool behind = wave >= 4;
+        bf16x8 fa[4], fb[2];
+        const uint32_t base = lds_address(lds);
+        if (kt0 < kt1) {
+            bring(0);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        slot_end();
+        if (behind) slot_end();
         uint32_t buf = 0;
-        for (uint32_t t = kt0 + 1; t < kt1; ++t) {
-            bring();
-            multiply(buf);
-            put(buf ^ 1);       // read last before the barrier that ended the tile before
-            __syncthreads();
+        for (uint32_t t = kt0; t < kt1; ++t) {
+            const uint32_t at_a = base + buf * kBuf + ra0, at_b = base + buf * kBuf + rb0;
+#pragma unroll
+            for (int kk = 0; kk < kFfBk / 16; ++kk) {
+                if (kk == 0 && t + 1 < kt1) bring(buf ^ 1);
+                read_fragments(at_a ^ (kk * 32), at_b ^ (kk * 32), fa, fb);
+                if (kk == 3 && behind) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                slot_end();
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_s_setprio(0);
+                if (kk == 3 && !behind) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                slot_end();
+            }
             buf ^= 1;
         }
-        multiply(buf);
+        if (!behind) slot_end();
+    } else {
+        auto multiply = [&](uint32_t buf) {
+            const unsigned char* const la = lds + buf * kBuf;
+#pragma unroll
+            for (int kk = 0; kk < kFfBk / 16; ++kk) {
+                bf16x8 fa[MI], fb[NI];
+#pragma unroll
+                for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+            }
+        };
+        uint32_t buf = 0;
+        if (kt0 < kt1) bring(0);
+        for (uint32_t t = kt0; t < kt1; ++t) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();            // tile t is there, and every wave is past its reads of tile t - 1
+            if (t + 1 < kt1) bring(buf ^ 1);
+            multiply(buf);
+            buf ^= 1;
+        }
+        __syncthreads();
     }
 
-    // lane: row m of a 32 x 32 square, columns 8 (v / 4) + 4 (lane / 32) + v % 4
+    // Through LDS, 32 rows of the wave at a time, so that a row's columns are loaded and stored together: a lane holds row lane % 32
+    // of a 32 x 32 square and its columns 8 (v / 4) + 4 (lane / 32) + v % 4.
+    constexpr uint32_t kRow = 68;       // floats: 64 and a pad that spreads the rows over the banks
+    float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kRow);
+    static_assert(WM * WN * 32 * kRow * 4 <= 2 * kBuf, "the staging areas fit where the tiles were");
+    constexpr uint32_t kLanes = GATED ? 8 : 16;     // per row, four columns each
+    const uint32_t c4 = (lane % kLanes) * 4, n = n0 + wn * (GATED ? 32 : 64) + c4;
+    const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        const uint32_t m = m0 + (wm * MI + i) * 32 + fr;
-        if (m >= p.M) continue;
 #pragma unroll
-        for (int j = 0; j < (GATED ? 1 : NI); ++j)
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t n = n0 + (GATED ? wn * 32 : (wn * NI + j) * 32) + 8 * q + 4 * (lane >> 5);
-                if (n >= ((EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N)) continue;
-                float v[4], v2[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = acc[i][j][4 * q + e];
-                    v2[e] = GATED ? acc[i][NI - 1][4 * q + e] : 0.f;
-                }
-                ff_epilogue<T, EPI>(p, split, m, n, v, v2);
+                const float4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                *reinterpret_cast<float4*>(mine + fr * kRow + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
             }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 4
+        for (uint32_t r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+            const uint32_t r = r0 + lane / kLanes, m = m0 + (wm * MI + i) * 32 + r;
+            const float4 x = *reinterpret_cast<const float4*>(mine + r * kRow + c4);
+            const float4 x2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kRow + 32 + c4) : x;
+            if (m >= p.M || n >= n_end) continue;
+            float v[4] = {x.x, x.y, x.z, x.w}, v2[4] = {x2.x, x2.y, x2.z, x2.w};
+            ff_epilogue<T, EPI>(p, split, m, n, v, v2);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
 }
 
