@@ -14,7 +14,7 @@ const char* const kKernelNames[KID_COUNT] = {
     "k_reduce_gram", "k_gram_sum", "k_chol", "k_apply", "k_pass_q", "k_reduce_q", "k_decompress",
     "k_pass_p_deferred", "k_wide_hist", "k_wide_reduce", "k_estimate_one", "k_grad_sumsq", "k_clip",
     "k_norm_forward", "k_norm_backward", "k_norm_sum", "k_ff_pack", "k_ff_gate", "k_ff_down", "k_ff_dgate", "k_ff_dx",
-    "k_ff_dw", "k_ff_sum"};
+    "k_ff_dw", "k_ff_join"};
 }
 
 namespace {

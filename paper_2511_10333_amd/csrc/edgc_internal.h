@@ -140,7 +140,7 @@ enum KernelId {
     KID_REDUCE_GRAM, KID_GRAM_SUM, KID_CHOL, KID_APPLY, KID_PASS_Q, KID_REDUCE_Q, KID_DECOMPRESS,
     KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
     KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_FF_PACK,
-    KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_SUM, KID_COUNT
+    KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_JOIN, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 

@@ -68,29 +68,6 @@ __global__ __launch_bounds__(256) void k_ff_pack(const PackList list)
     }
 }
 
-// Adds the partial sums of a split product up
-struct FfSumArgs {
-    FfProblem p;
-    const float* part;
-    uint32_t splits;
-};
-template <typename T>
-__global__ __launch_bounds__(256) void k_ff_sum(const FfSumArgs a)
-{
-    const uint32_t quads = (a.p.N + 3) / 4;
-    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x, m = i / quads;
-    const uint32_t n0 = static_cast<uint32_t>(i - m * quads) * 4;
-    if (m >= a.p.M) return;
-    float v[4] = {}, none[4] = {};
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        float x[4];
-        ff_load4<float>(a.part + (static_cast<uint64_t>(s) * a.p.M + m) * a.p.N, n0, a.p.N, x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += x[e];
-    }
-    ff_epilogue<T, kFfStore>(a.p, 0, static_cast<uint32_t>(m), n0, v, none);
-}
-
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
@@ -131,7 +108,6 @@ struct FfPlan {
     }
 };
 
-constexpr uint64_t kPartElems = 512ull * 128 * 128;      // partial sums of split products
 constexpr uint32_t kFfMaxTokens = 1u << 21, kFfMaxWidth = 1u << 20;
 
 struct Packer {
@@ -163,66 +139,64 @@ struct Packer {
     }
 };
 
+// Blocks of a tile shape that share a compute unit (by LDS)
+constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / (2u * (bm + bn) * 128u); }
+// The fewest steps of k that are worth a worker, which then writes a tile's sums and has them read again
+constexpr uint64_t kMinSteps = 8;
+
 template <int BM, int BN, int WM, int WN, typename T, int EPI>
 int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
-    uint32_t first = 0;
+    uint32_t tiles = 0;
     double flops = 0.0, bytes = 0.0;
     constexpr uint32_t COLS = EPI == kFfGate ? BN / 2 : BN;
+    a.ksteps = a.p[0].ktiles * a.p[0].nseg;
     for (uint32_t i = 0; i < a.count; ++i) {
         FfProblem& p = a.p[i];
         p.tiles_m = (p.M + BM - 1) / BM;
         p.tiles_n = (p.N + COLS - 1) / COLS;
-        p.first = first;
-        first += p.tiles_m * p.tiles_n;
-        const double k = static_cast<double>(p.ktiles) * p.nseg * kFfBk, both = EPI == kFfGate ? 2.0 : 1.0;
+        p.first = tiles;
+        tiles += p.tiles_m * p.tiles_n;
+        const double k = static_cast<double>(a.ksteps) * kFfBk, both = EPI == kFfGate ? 2.0 : 1.0;
         flops += 2.0 * p.M * p.N * k * both;
         bytes += 2.0 * (p.M + p.N * both) * k;
     }
-    a.blocks = first;
-    constexpr uint32_t lds = 2 * (BM + BN) * 128;
-    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, WM, WN, T, EPI><<<first * a.splits, 64 * WM * WN, lds, st>>>(a));
+    const uint32_t places = static_cast<uint32_t>(ctx->num_cu) * blocks_per_cu(BM, BN);
+    a.whole = tiles / places * places;
+    a.rest = tiles - a.whole;
+    a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, a.rest * static_cast<uint64_t>(a.ksteps) / kMinSteps));
+    // (a last round that is nearly full is not worth the sums' way through memory)
+    if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
+    a.part = ctx->ff.part;
+    constexpr uint32_t lds = 2 * (BM + BN) * 128, threads = 64 * WM * WN;
+    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, WM, WN, T, EPI><<<a.whole + a.workers, threads, lds, st>>>(a));
     EDGC_HIP_TRY(ctx, hipGetLastError());
+    if (a.rest) {
+        EDGC_LAUNCH(ctx, st, KID_FF_JOIN, 4.0 * BM * BN * (a.workers + a.rest), 0.0,
+                    k_ff_join<BM, BN, WM, WN, T, EPI><<<a.rest * (BM / WM / 32), threads, 0, st>>>(a));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+    }
     return EDGC_OK;
 }
 
-uint64_t tiles_of(const FfArgs& a, uint64_t bm, uint64_t bn)
-{
-    uint64_t n = 0;
-    for (uint32_t i = 0; i < a.count; ++i) n += ((a.p[i].M + bm - 1) / bm) * ((a.p[i].N + bn - 1) / bn);
-    return n;
-}
+// Sums that workers can leave behind: at most two per place of the larger tile shape
+uint64_t part_elems(const edgc_ctx* ctx) { return 2ull * ctx->num_cu * std::max(256 * 256 * blocks_per_cu(256, 256), 128 * 128 * blocks_per_cu(128, 128)); }
 
 template <typename T, int EPI>
 int launch_product(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
-    const uint64_t cu = static_cast<uint64_t>(ctx->num_cu), half = EPI == kFfGate ? 2 : 1;
-    const uint64_t big = tiles_of(a, 256, 256 / half), mid = tiles_of(a, 128, 128 / half);
-    a.splits = 1;
-    if constexpr (EPI == kFfStore) {
-        // few tiles of a long k: split, and added up by a launch of its own
-        const uint64_t k = static_cast<uint64_t>(a.p[0].nseg) * a.p[0].ktiles;
-        if (a.count == 1 && mid * 2 <= cu && k >= 16) {
-            const uint64_t s = std::min<uint64_t>({cu * 2 / mid, k / 8, kPartElems / (static_cast<uint64_t>(a.p[0].M) * a.p[0].N)});
-            if (s > 1) {
-                FfSumArgs sum{};
-                sum.p = a.p[0];
-                sum.part = ctx->ff.part;
-                sum.splits = static_cast<uint32_t>(s);
-                a.splits = static_cast<uint32_t>(s);
-                a.p[0].out = ctx->ff.part;
-                if (int rc = launch_tiles<128, 128, 2, 2, T, kFfPartial>(ctx, a, kid, st)) return rc;
-                const uint64_t quads = static_cast<uint64_t>(sum.p.M) * ((sum.p.N + 3) / 4);
-                EDGC_LAUNCH(ctx, st, KID_FF_SUM, 4.0 * s * sum.p.M * sum.p.N, 0.0,
-                            k_ff_sum<T><<<static_cast<uint32_t>((quads + 255) / 256), 256, 0, st>>>(sum));
-                EDGC_HIP_TRY(ctx, hipGetLastError());
-                return EDGC_OK;
-            }
-        }
-    }
-    // rounds of tiles on the compute units, a tile of 128 x 128 taking a quarter of the work and two of them at a time
-    const double t_big = static_cast<double>((big + cu - 1) / cu), t_mid = 0.6 * static_cast<double>((mid + 2 * cu - 1) / (2 * cu));
-    if (t_big <= t_mid) return launch_tiles<256, 256, 2, 4, T, EPI>(ctx, a, kid, st);
+    // The time that either tile shape would take, in steps of k of a 256 x 256 tile on a compute unit.  Measured: a tile of 128 x 128
+    // has a quarter of the work and gets it done at 0.65 of the rate.
+    auto time_of = [&](uint64_t bm, uint64_t bn, double step) {
+        uint64_t tiles = 0;
+        for (uint32_t i = 0; i < a.count; ++i) tiles += ((a.p[i].M + bm - 1) / bm) * ((a.p[i].N + bn - 1) / bn);
+        const uint64_t steps = static_cast<uint64_t>(a.p[0].ktiles) * a.p[0].nseg, places = static_cast<uint64_t>(ctx->num_cu) * blocks_per_cu(bm, bm);
+        const double each = static_cast<double>(tiles * steps) / places;
+        return step * std::max(each, static_cast<double>(std::min<uint64_t>(steps, kMinSteps)));
+    };
+    constexpr uint64_t half = EPI == kFfGate ? 2 : 1;
+    if (time_of(256, 256 / half, 1.0) <= time_of(128, 128 / half, 0.25 * blocks_per_cu(128, 128) / 0.65))
+        return launch_tiles<256, 256, 2, 4, T, EPI>(ctx, a, kid, st);
     return launch_tiles<128, 128, 2, 2, T, EPI>(ctx, a, kid, st);
 }
 
@@ -427,7 +401,7 @@ extern "C" int edgc_reserve_ff(edgc_ctx* ctx, edgc_dtype dtype, uint32_t tokens,
     FfPlan plan(tokens, hidden, ff, dtype);
     uint64_t elems = plan.forward();
     if (backward) elems = std::max(elems, plan.backward());
-    if (hipMalloc(&ctx->ff.ws, elems * 2) != hipSuccess || hipMalloc(reinterpret_cast<void**>(&ctx->ff.part), kPartElems * sizeof(float)) != hipSuccess) {
+    if (hipMalloc(&ctx->ff.ws, elems * 2) != hipSuccess || hipMalloc(reinterpret_cast<void**>(&ctx->ff.part), part_elems(ctx) * sizeof(float)) != hipSuccess) {
         (void)hipGetLastError();
         if (ctx->ff.ws) (void)hipFree(ctx->ff.ws);
         ctx->ff = FfScratch{};

@@ -38,13 +38,22 @@ struct FfProblem {
     int32_t act;
 };
 constexpr int kFfProblems = 3;
+// The tiles of the output that make whole rounds of the compute units are a block each.  The rest's steps of k are shared evenly by
+// `workers` further blocks, so that all of them end together; a worker goes through its steps tile by tile, and leaves the sums of
+// tiles that it has a part of in `part` (slot: worker + tile), where k_ff_join adds them up.
 struct FfArgs {
     FfProblem p[kFfProblems];
-    uint32_t count, splits;             // problems; ways the k tiles are split (partial sums: out is [splits][M][N])
-    uint32_t blocks;                    // of one split
+    uint32_t count, whole;              // problems; tiles of a block each
+    uint32_t rest, workers, ksteps;     // the other tiles; blocks that share them; steps of k of a tile (the same in all problems)
+    float* part;                        // [workers + rest][BM * BN]
 };
+// steps of worker w: [ff_share(w), ff_share(w + 1)) of rest * ksteps
+__host__ __device__ inline uint64_t ff_share(const FfArgs& a, uint32_t w)
+{
+    return static_cast<uint64_t>(a.rest) * a.ksteps * w / a.workers;
+}
 
-enum FfEpi { kFfStore = 0, kFfGate = 1, kFfDgate = 2, kFfPartial = 3 };
+enum FfEpi { kFfStore = 0, kFfGate = 1, kFfDgate = 2 };
 
 // Activation and derivative.  gelu_tanh by the identity (1 + tanh t) / 2 = 1 / (1 + exp(-2 t)).
 __device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
@@ -141,7 +150,7 @@ __device__ __forceinline__ void ff_store4(T* row, uint32_t n0, uint32_t n, const
 
 // What becomes of four neighbouring sums of row m
 template <typename T, int EPI>
-__device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t split, uint32_t m, uint32_t n0, float (&v)[4], float (&v2)[4])
+__device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t m, uint32_t n0, float (&v)[4], float (&v2)[4])
 {
     if constexpr (EPI == kFfStore) {
         T* const row = static_cast<T*>(p.out) + m * p.ldo;
@@ -152,9 +161,6 @@ __device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t split, 
             for (int i = 0; i < 4; ++i) v[i] += o[i];
         }
         ff_store4<T>(row, n0, p.N, v);
-    } else if constexpr (EPI == kFfPartial) {
-        float* const row = static_cast<float*>(p.out) + (static_cast<uint64_t>(split) * p.M + m) * p.N;
-        ff_store4<float>(row, n0, p.N, v);
     } else if constexpr (EPI == kFfGate) {
         float h[4];
 #pragma unroll
@@ -232,6 +238,55 @@ __device__ __forceinline__ void slot_end()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+__device__ __forceinline__ const FfProblem& ff_problem_of(const FfArgs& args, uint32_t tile)
+{
+    uint32_t pi = 0;
+#pragma unroll
+    for (int i = 1; i < kFfProblems; ++i) pi += (static_cast<uint32_t>(i) < args.count && tile >= args.p[i].first) ? 1u : 0u;
+    return args.p[pi];
+}
+
+// The sums of 32 rows of a wave, of which a lane holds row lane % 32 and of either half the columns 8 (v / 4) + 4 (lane / 32) + v % 4:
+// through LDS (the wave's own part of it), so that a row's columns are loaded and stored together.
+constexpr uint32_t kFfRow = 68;         // floats: 64 and a pad that spreads the rows over the banks
+template <typename T, int EPI>
+__device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16 (&acc)[2], float* mine, uint32_t lane, uint32_t m0, uint32_t n0)
+{
+    constexpr bool GATED = EPI == kFfGate;
+    constexpr uint32_t kLanes = GATED ? 8 : 16;     // per row, four columns each
+    const uint32_t c4 = (lane % kLanes) * 4, n = n0 + c4;
+    const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 v = {acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
+            *reinterpret_cast<float4*>(mine + (lane & 31) * kFfRow + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 4
+    for (uint32_t r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+        const uint32_t r = r0 + lane / kLanes, m = m0 + r;
+        const float4 x = *reinterpret_cast<const float4*>(mine + r * kFfRow + c4);
+        const float4 x2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kFfRow + 32 + c4) : x;
+        if (m >= p.M || n >= n_end) continue;
+        float v[4] = {x.x, x.y, x.z, x.w}, v2[4] = {x2.x, x2.y, x2.z, x2.w};
+        ff_epilogue<T, EPI>(p, m, n, v, v2);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Where a worker leaves the sums of a tile: in the order of its registers
+template <int BM, int BN>
+__device__ __forceinline__ float4* ff_slot(float* part, uint32_t slot, uint32_t i, uint32_t j, uint32_t q, uint32_t tid, uint32_t threads)
+{
+    return reinterpret_cast<float4*>(part + static_cast<uint64_t>(slot) * (BM * BN)) + ((i * 2 + j) * 4 + q) * threads + tid;
+}
+
 template <int BM, int BN, int WM, int WN, typename T, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
 {
@@ -243,14 +298,20 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
     extern __shared__ __align__(16) unsigned char lds[];     // [2][(BM + BN) * 128]
     constexpr uint32_t kBuf = (BM + BN) * 128;
 
-    const uint32_t split = blockIdx.x / args.blocks, bid = blockIdx.x - split * args.blocks;
-    uint32_t pi = 0;
-#pragma unroll
-    for (int i = 1; i < kFfProblems; ++i) pi += (static_cast<uint32_t>(i) < args.count && bid >= args.p[i].first) ? 1u : 0u;
-    const FfProblem& p = args.p[pi];
-    uint32_t tm, tn;
-    ff_tile_of(bid - p.first, p.tiles_m, p.tiles_n, tm, tn);
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
+    static_assert(WM * WN * 32 * kFfRow * 4 <= 2 * kBuf, "the waves' parts of LDS in ff_finish fit where the tiles were");
+    const bool shares = blockIdx.x >= args.whole;
+    const uint32_t worker = blockIdx.x - args.whole;
+    uint64_t step = shares ? ff_share(args, worker) : 0, steps_end = shares ? ff_share(args, worker + 1) : args.ksteps;
+  while (step < steps_end) {
+    const uint32_t at = shares ? static_cast<uint32_t>(step / args.ksteps) : 0;
+    const uint32_t tile = shares ? args.whole + at : blockIdx.x;
+    const uint32_t kt0 = static_cast<uint32_t>(step - static_cast<uint64_t>(at) * args.ksteps);
+    const uint32_t kt1 = static_cast<uint32_t>(min(static_cast<uint64_t>(args.ksteps), kt0 + (steps_end - step)));
+    step += kt1 - kt0;
+    const FfProblem& p = ff_problem_of(args, tile);
+    uint32_t tm, tn;
+    ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
     const uint32_t m0 = tm * BM, n0 = tn * COLS;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
 
@@ -272,9 +333,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
     }
     const bool second = GATED && NTH / 8 == 64 && wave >= 4;        // rows 32 .. 63 of every 64
 
-    const uint32_t total = p.nseg * p.ktiles;
-    const uint32_t kt0 = static_cast<uint32_t>(static_cast<uint64_t>(total) * split / args.splits);
-    const uint32_t kt1 = static_cast<uint32_t>(static_cast<uint64_t>(total) * (split + 1) / args.splits);
     uint32_t seg = kt0 / p.ktiles, kt = kt0 - seg * p.ktiles;
     const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
 
@@ -311,10 +369,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
         const bool behind = wave >= 4;
         bf16x8 fa[4], fb[2];
         const uint32_t base = lds_address(lds);
-        if (kt0 < kt1) {
-            bring(0);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
+        bring(0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         slot_end();
         if (behind) slot_end();
         uint32_t buf = 0;
@@ -355,7 +411,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
             }
         };
         uint32_t buf = 0;
-        if (kt0 < kt1) bring(0);
+        bring(0);
         for (uint32_t t = kt0; t < kt1; ++t) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();            // tile t is there, and every wave is past its reads of tile t - 1
@@ -366,39 +422,53 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
         __syncthreads();
     }
 
-    // Through LDS, 32 rows of the wave at a time, so that a row's columns are loaded and stored together: a lane holds row lane % 32
-    // of a 32 x 32 square and its columns 8 (v / 4) + 4 (lane / 32) + v % 4.
-    constexpr uint32_t kRow = 68;       // floats: 64 and a pad that spreads the rows over the banks
-    float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kRow);
-    static_assert(WM * WN * 32 * kRow * 4 <= 2 * kBuf, "the staging areas fit where the tiles were");
-    constexpr uint32_t kLanes = GATED ? 8 : 16;     // per row, four columns each
-    const uint32_t c4 = (lane % kLanes) * 4, n = n0 + wn * (GATED ? 32 : 64) + c4;
-    const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
+    if (kt1 - kt0 == args.ksteps) {
+        float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
+        for (int i = 0; i < MI; ++i)
+            ff_finish<T, EPI>(p, acc[i], mine, lane, m0 + (wm * MI + i) * 32, n0 + wn * (GATED ? 32 : 64));
+    } else {
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *ff_slot<BM, BN>(args.part, worker + at, i, j, q, tid, NTH) =
+                        float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    }
+    if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
+  }
+}
+
+// Adds up the sums that several workers have of a tile, in the order of the workers: 32 rows of every wave's part per block
+template <int BM, int BN, int WM, int WN, typename T, int EPI>
+__global__ __launch_bounds__(64 * WM * WN) void k_ff_join(const FfArgs args)
+{
+    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32;
+    constexpr bool GATED = EPI == kFfGate;
+    __shared__ float stage[WM * WN * 32 * kFfRow];
+    const uint32_t at = blockIdx.x / MI, i = blockIdx.x % MI, tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    const uint64_t s0 = static_cast<uint64_t>(at) * args.ksteps, s1 = s0 + args.ksteps, all = static_cast<uint64_t>(args.rest) * args.ksteps;
+    uint32_t w = static_cast<uint32_t>(s0 * args.workers / all);
+    while (ff_share(args, w + 1) <= s0) ++w;        // the first worker with a step of this tile
+    if (ff_share(args, w) <= s0 && ff_share(args, w + 1) >= s1) return;     // which had them all
+    f32x16 acc[2] = {};
+    for (; w < args.workers && ff_share(args, w) < s1; ++w) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                *reinterpret_cast<float4*>(mine + fr * kRow + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
+                const float4 v = *ff_slot<BM, BN>(args.part, w + at, i, j, q, tid, NTH);
+                acc[j][4 * q] += v.x; acc[j][4 * q + 1] += v.y; acc[j][4 * q + 2] += v.z; acc[j][4 * q + 3] += v.w;
             }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll 4
-        for (uint32_t r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-            const uint32_t r = r0 + lane / kLanes, m = m0 + (wm * MI + i) * 32 + r;
-            const float4 x = *reinterpret_cast<const float4*>(mine + r * kRow + c4);
-            const float4 x2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kRow + 32 + c4) : x;
-            if (m >= p.M || n >= n_end) continue;
-            float v[4] = {x.x, x.y, x.z, x.w}, v2[4] = {x2.x, x2.y, x2.z, x2.w};
-            ff_epilogue<T, EPI>(p, split, m, n, v, v2);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
+    const uint32_t tile = args.whole + at;
+    const FfProblem& p = ff_problem_of(args, tile);
+    uint32_t tm, tn;
+    ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
+    ff_finish<T, EPI>(p, acc, stage + wave * (32 * kFfRow), lane, tm * BM + (wave / WN * MI + i) * 32,
+                      tn * (GATED ? BN / 2 : BN) + wave % WN * (GATED ? 32 : 64));
 }
 
 }  // namespace edgc
