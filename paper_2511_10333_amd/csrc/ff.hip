@@ -141,8 +141,8 @@ struct Packer {
 
 // Blocks of a tile shape that share a compute unit (by LDS)
 constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / (2u * (bm + bn) * 128u); }
-// The fewest steps of k that are worth a worker, which then writes a tile's sums and has them read again
-constexpr uint64_t kMinSteps = 8;
+// The least k that is worth a worker, which then writes a tile's sums and has them read again
+constexpr uint64_t kMinK = 512;
 
 template <int BM, int BN, int WM, int WN, typename T, int EPI>
 int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
@@ -150,21 +150,22 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     uint32_t tiles = 0;
     double flops = 0.0, bytes = 0.0;
     constexpr uint32_t COLS = EPI == kFfGate ? BN / 2 : BN;
-    a.ksteps = a.p[0].ktiles * a.p[0].nseg;
+    constexpr int BK = ff_bk(WM, WN);
+    a.ksteps = a.p[0].ktiles * (kFfBk / BK) * a.p[0].nseg;
     for (uint32_t i = 0; i < a.count; ++i) {
         FfProblem& p = a.p[i];
         p.tiles_m = (p.M + BM - 1) / BM;
         p.tiles_n = (p.N + COLS - 1) / COLS;
         p.first = tiles;
         tiles += p.tiles_m * p.tiles_n;
-        const double k = static_cast<double>(a.ksteps) * kFfBk, both = EPI == kFfGate ? 2.0 : 1.0;
+        const double k = static_cast<double>(a.ksteps) * BK, both = EPI == kFfGate ? 2.0 : 1.0;
         flops += 2.0 * p.M * p.N * k * both;
         bytes += 2.0 * (p.M + p.N * both) * k;
     }
     const uint32_t places = static_cast<uint32_t>(ctx->num_cu) * blocks_per_cu(BM, BN);
     a.whole = tiles / places * places;
     a.rest = tiles - a.whole;
-    a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, a.rest * static_cast<uint64_t>(a.ksteps) / kMinSteps));
+    a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, static_cast<uint64_t>(a.rest) * a.ksteps * BK / kMinK));
     // (a last round that is nearly full is not worth the sums' way through memory)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;
@@ -185,14 +186,14 @@ uint64_t part_elems(const edgc_ctx* ctx) { return 2ull * ctx->num_cu * std::max(
 template <typename T, int EPI>
 int launch_product(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
-    // The time that either tile shape would take, in steps of k of a 256 x 256 tile on a compute unit.  Measured: a tile of 128 x 128
+    // The time that either tile shape would take, in steps of 64 k of a 256 x 256 tile on a compute unit.  Measured: a tile of 128 x 128
     // has a quarter of the work and gets it done at 0.65 of the rate.
     auto time_of = [&](uint64_t bm, uint64_t bn, double step) {
         uint64_t tiles = 0;
         for (uint32_t i = 0; i < a.count; ++i) tiles += ((a.p[i].M + bm - 1) / bm) * ((a.p[i].N + bn - 1) / bn);
         const uint64_t steps = static_cast<uint64_t>(a.p[0].ktiles) * a.p[0].nseg, places = static_cast<uint64_t>(ctx->num_cu) * blocks_per_cu(bm, bm);
         const double each = static_cast<double>(tiles * steps) / places;
-        return step * std::max(each, static_cast<double>(std::min<uint64_t>(steps, kMinSteps)));
+        return step * std::max(each, static_cast<double>(std::min<uint64_t>(steps, kMinK / kFfBk)));
     };
     constexpr uint64_t half = EPI == kFfGate ? 2 : 1;
     if (time_of(256, 256 / half, 1.0) <= time_of(128, 128 / half, 0.25 * blocks_per_cu(128, 128) / 0.65))

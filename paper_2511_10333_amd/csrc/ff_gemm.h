@@ -5,9 +5,10 @@
 // bits, cut off, not rounded); six products of planes, 2^-24 of the operands left out, are six segments of one sum.  Six bf16 MFMAs
 // take less time than one of fp32 (2.5e15 / 6 against 0.16e15 operations a second).
 //
-// A block of WM x WN waves makes a BM x BN tile from two LDS buffers of 64 k each: the next tile's rows are on their way to one while
-// the other is multiplied.  A row of 128 bytes lies in LDS as eight 16-byte units, unit c at c ^ (row & 7),
-// so that the 32 rows of a fragment are read without bank conflicts.  The MFMA's first operand is B: a lane then holds four
+// A block of WM x WN waves makes a BM x BN tile; tiles of 64 or 32 k of the operands come to LDS buffers while earlier ones are
+// multiplied.  A row of 128 (64) bytes lies in LDS as eight (four) 16-byte units, unit c at c ^ (row / 2 & 7) (at
+// c ^ (row / 4 & 3)): a read of 16 bytes per lane takes lanes 0-3, 12-15 and 20-27 of either half at once, then the other sixteen,
+// and their rows then lie in different banks.  (At c ^ (row & 7) and c ^ (row / 2 & 3) half of LDS's cycles were conflicts.)  The MFMA's first operand is B: a lane then holds four
 // neighbouring n of one m, which is what the epilogues load and store.
 #pragma once
 
@@ -15,7 +16,7 @@
 
 namespace edgc {
 
-constexpr int kFfBk = 64;               // k of a tile
+constexpr int kFfBk = 64;               // operands' k are padded to a multiple of this
 constexpr int kFfSegs = 12;
 constexpr uint64_t kFfMaxLd = 1ull << 22;   // rows of a tile are addressed in 32 bits from its first
 
@@ -25,7 +26,7 @@ struct FfProblem {
     const uint16_t* b2[kFfSegs];        // the gated form: the second matrix of the same shape as b
     uint64_t lda, ldb;                  // elements
     uint32_t M, N;                      // of the output (gated: N columns of each of the two)
-    uint32_t ktiles, nseg;              // tiles of a segment; segments
+    uint32_t ktiles, nseg;              // times 64 k of a segment; segments
     uint32_t tiles_m, tiles_n, first;   // tiles of the output; first block
     uint32_t accumulate;
     void* out;                          // store: the output; gate, dgate: planes of h
@@ -217,20 +218,29 @@ __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned 
 {
     __builtin_amdgcn_global_load_lds((global_byte*)from, (lds_byte*)to, 16, 0, 0);
 }
-// The fragments of one step of 16 k: rows 32 apart, which lie 4096 bytes apart in LDS
-__device__ __forceinline__ void read_fragments(uint32_t at_a, uint32_t at_b, bf16x8 (&fa)[4], bf16x8 (&fb)[2])
+// The fragments of a tile of 32 k: rows 32 apart lie 2048 bytes apart in LDS, the second 16 k at the address ^ 32
+__device__ __forceinline__ void read_fragments(uint32_t at_a, uint32_t at_b, bf16x8 (&fa)[2][4], bf16x8 (&fb)[2][2])
 {
-    asm volatile("ds_read_b128 %0, %6\n\t"
-                 "ds_read_b128 %4, %7\n\t"
-                 "ds_read_b128 %1, %6 offset:4096\n\t"
-                 "ds_read_b128 %5, %7 offset:4096\n\t"
-                 "ds_read_b128 %2, %6 offset:8192\n\t"
-                 "ds_read_b128 %3, %6 offset:12288\n\t"
+    asm volatile("ds_read_b128 %0, %12\n\t"
+                 "ds_read_b128 %8, %14\n\t"
+                 "ds_read_b128 %9, %14 offset:2048\n\t"
+                 "ds_read_b128 %1, %12 offset:2048\n\t"
+                 "ds_read_b128 %2, %12 offset:4096\n\t"
+                 "ds_read_b128 %3, %12 offset:6144\n\t"
+                 "ds_read_b128 %4, %13\n\t"
+                 "ds_read_b128 %10, %15\n\t"
+                 "ds_read_b128 %11, %15 offset:2048\n\t"
+                 "ds_read_b128 %5, %13 offset:2048\n\t"
+                 "ds_read_b128 %6, %13 offset:4096\n\t"
+                 "ds_read_b128 %7, %13 offset:6144\n\t"
                  "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(fb[0]), "=&v"(fb[1])
-                 : "v"(at_a), "v"(at_b)
+                 : "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[0][2]), "=&v"(fa[0][3]), "=&v"(fa[1][0]), "=&v"(fa[1][1]),
+                   "=&v"(fa[1][2]), "=&v"(fa[1][3]), "=&v"(fb[0][0]), "=&v"(fb[0][1]), "=&v"(fb[1][0]), "=&v"(fb[1][1])
+                 : "v"(at_a), "v"(at_a ^ 32u), "v"(at_b), "v"(at_b ^ 32u)
                  : "memory");
 }
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void slot_end()
 {
     __builtin_amdgcn_sched_barrier(0);
@@ -287,158 +297,201 @@ __device__ __forceinline__ float4* ff_slot(float* part, uint32_t slot, uint32_t 
     return reinterpret_cast<float4*>(part + static_cast<uint64_t>(slot) * (BM * BN)) + ((i * 2 + j) * 4 + q) * threads + tid;
 }
 
+// Waves of a block that take turns (below): tiles of 32 k in four buffers.  Otherwise tiles of 64 k in two.
+constexpr bool ff_turns(int wm, int wn) { return wm * wn == 8; }
+constexpr int ff_bk(int wm, int wn) { return ff_turns(wm, wn) ? 32 : 64; }
+
 template <int BM, int BN, int WM, int WN, typename T, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
 {
-    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = 2;
-    constexpr int LA = BM * 8 / NTH, LB = BN * 8 / NTH;      // 16-byte units that a thread brings of either operand
-    constexpr bool GATED = EPI == kFfGate, TURNS = WM * WN == 8;
+    constexpr bool GATED = EPI == kFfGate, TURNS = ff_turns(WM, WN);
+    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = 2, BK = ff_bk(WM, WN), UNITS = BK / 8;
+    constexpr int ROWS = NTH / UNITS, LA = BM / ROWS, LB = BN / ROWS;       // rows that the block brings at a time
     static_assert(BN / WN == 64, "a wave has 64 columns; gated: 32 of either projection");
-    static_assert(NTH / 8 == 64 || NTH / 8 == 32, "rows of the two projections alternate by 32");
-    extern __shared__ __align__(16) unsigned char lds[];     // [2][(BM + BN) * 128]
-    constexpr uint32_t kBuf = (BM + BN) * 128;
-
+    static_assert(ROWS == 128 || ROWS == 32, "rows of the two projections alternate by 32");
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr uint32_t kBuf = (BM + BN) * BK * 2, kBufs = TURNS ? 4 : 2;
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
-    static_assert(WM * WN * 32 * kFfRow * 4 <= 2 * kBuf, "the waves' parts of LDS in ff_finish fit where the tiles were");
+    static_assert(WM * WN * 32 * kFfRow * 4 <= kBufs * kBuf, "the waves' parts of LDS in ff_finish fit where the tiles were");
+
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
     const bool shares = blockIdx.x >= args.whole;
     const uint32_t worker = blockIdx.x - args.whole;
-    uint64_t step = shares ? ff_share(args, worker) : 0, steps_end = shares ? ff_share(args, worker + 1) : args.ksteps;
-  while (step < steps_end) {
-    const uint32_t at = shares ? static_cast<uint32_t>(step / args.ksteps) : 0;
-    const uint32_t tile = shares ? args.whole + at : blockIdx.x;
-    const uint32_t kt0 = static_cast<uint32_t>(step - static_cast<uint64_t>(at) * args.ksteps);
-    const uint32_t kt1 = static_cast<uint32_t>(min(static_cast<uint64_t>(args.ksteps), kt0 + (steps_end - step)));
-    step += kt1 - kt0;
-    const FfProblem& p = ff_problem_of(args, tile);
-    uint32_t tm, tn;
-    ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
-    const uint32_t m0 = tm * BM, n0 = tn * COLS;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
+    uint64_t step = shares ? ff_share(args, worker) : 0;
+    const uint64_t steps_end = shares ? ff_share(args, worker + 1) : args.ksteps;
+    while (step < steps_end) {
+        const uint32_t at = shares ? static_cast<uint32_t>(step / args.ksteps) : 0;
+        const uint32_t tile = shares ? args.whole + at : blockIdx.x;
+        const uint32_t kt0 = static_cast<uint32_t>(step - static_cast<uint64_t>(at) * args.ksteps);
+        const uint32_t kt1 = static_cast<uint32_t>(min(static_cast<uint64_t>(args.ksteps), kt0 + (steps_end - step)));
+        step += kt1 - kt0;
+        const FfProblem& p = ff_problem_of(args, tile);
+        uint32_t tm, tn;
+        ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
+        const uint32_t m0 = tm * BM, n0 = tn * COLS;
 
-    // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last).  It brings unit
-    // tid % 8 of the LDS row tid / 8 and of the rows NTH / 8 apart from it, which is unit (tid % 8) ^ (row & 7) of the operand's row.
-    uint32_t oa[LA], ob[LB];
-    const uint32_t unit = ((tid % 8) ^ ((tid / 8) & 7)) * 16;
+        // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last): to unit
+        // tid % UNITS of the LDS row tid / UNITS and of those ROWS apart from it, whose bits choose which unit of the operand's.
+        uint32_t oa[LA], ob[LB];
+        const uint32_t unit = ((tid % UNITS) ^ (TURNS ? tid / UNITS / 4 & 3 : tid / UNITS / 2 & 7)) * 16;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-        const uint32_t row = min(tid / 8 + i * (NTH / 8), p.M - 1 - m0);
-        oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + unit;
-    }
-#pragma unroll
-    for (int i = 0; i < LB; ++i) {
-        uint32_t row = tid / 8 + i * (NTH / 8);
-        if constexpr (GATED) row = row / 64 * 32 + row % 32;        // rows 64 w .. + 31: the first matrix, + 32 .. 63: the second
-        row = min(row, p.N - 1 - n0);
-        ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + unit;
-    }
-    const bool second = GATED && NTH / 8 == 64 && wave >= 4;        // rows 32 .. 63 of every 64
-
-    uint32_t seg = kt0 / p.ktiles, kt = kt0 - seg * p.ktiles;
-    const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
-
-    f32x16 acc[MI][NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-
-    const uint32_t fr = lane & 31, fu = ((lane >> 5) ^ (fr & 7)) * 16;      // fragment row; its unit, to be xored with 2 k / 16
-    const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = BM * 128 + (wn * NI * 32 + fr) * 128 + fu;
-
-    // the next tile of k, to buffer `buf`
-    auto bring = [&](uint32_t buf) {
-        const unsigned char* pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_row0 + kt * kFfBk);
-        const unsigned char* pb = reinterpret_cast<const unsigned char*>((second ? p.b2[seg] : p.b[seg]) + b_row0 + kt * kFfBk);
-        const unsigned char* pb2 = GATED && !second ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_row0 + kt * kFfBk) : pb;
-        unsigned char* const to = lds + buf * kBuf + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < LA; ++i) load_to_lds(pa + oa[i], to + i * (NTH * 16));
-#pragma unroll
-        for (int i = 0; i < LB; ++i)
-            load_to_lds((GATED && NTH / 8 == 32 && (i & 1) ? pb2 : pb) + ob[i], to + BM * 128 + i * (NTH * 16));
-        if (++kt == p.ktiles) { kt = 0; ++seg; }
-    };
-
-    if constexpr (TURNS) {
-        // The waves take turns: of the two on a SIMD, one reads fragments (and asks for the next tile) while the other
-        // multiplies, and a barrier ends either's slot.  Wave group 1 is one slot behind group 0.  Tile t is read in slots 8 t to
-        // 8 t + 7; tile t + 1 is asked for in slots 8 t and 8 t + 1, into the buffer that was read last in slot 8 t - 1, and waited
-        // for before the barrier that ends slot 8 t + 7.
-        const bool behind = wave >= 4;
-        bf16x8 fa[4], fb[2];
-        const uint32_t base = lds_address(lds);
-        bring(0);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        slot_end();
-        if (behind) slot_end();
-        uint32_t buf = 0;
-        for (uint32_t t = kt0; t < kt1; ++t) {
-            const uint32_t at_a = base + buf * kBuf + ra0, at_b = base + buf * kBuf + rb0;
-#pragma unroll
-            for (int kk = 0; kk < kFfBk / 16; ++kk) {
-                if (kk == 0 && t + 1 < kt1) bring(buf ^ 1);
-                read_fragments(at_a ^ (kk * 32), at_b ^ (kk * 32), fa, fb);
-                if (kk == 3 && behind) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                slot_end();
-                __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-                __builtin_amdgcn_s_setprio(0);
-                if (kk == 3 && !behind) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                slot_end();
-            }
-            buf ^= 1;
+        for (int i = 0; i < LA; ++i) {
+            const uint32_t row = min(tid / UNITS + i * ROWS, p.M - 1 - m0);
+            oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + unit;
         }
-        if (!behind) slot_end();
-    } else {
-        auto multiply = [&](uint32_t buf) {
-            const unsigned char* const la = lds + buf * kBuf;
 #pragma unroll
-            for (int kk = 0; kk < kFfBk / 16; ++kk) {
-                bf16x8 fa[MI], fb[NI];
-#pragma unroll
-                for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
-#pragma unroll
-                for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < LB; ++i) {
+            uint32_t row = tid / UNITS + i * ROWS;
+            if constexpr (GATED) row = row / 64 * 32 + row % 32;        // rows 64 w .. + 31: the first matrix, + 32 .. 63: the second
+            row = min(row, p.N - 1 - n0);
+            ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + unit;
+        }
+        // which of the two this wave brings, where it is the same for all its rows
+        const bool second = GATED && ROWS == 128 && (wave * (64 / UNITS) & 32);
+
+        const uint32_t per_seg = p.ktiles * (64 / BK);
+        uint32_t seg = kt0 / per_seg, left = per_seg - (kt0 - seg * per_seg);
+        const unsigned char *pa, *pb, *pb2;
+        auto to_segment = [&](uint32_t k) {
+            const uint64_t a_at = m0 * p.lda + k, b_at = n0 * p.ldb + k;
+            pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_at);
+            pb = reinterpret_cast<const unsigned char*>((second ? p.b2[seg] : p.b[seg]) + b_at);
+            pb2 = GATED && ROWS == 32 ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_at) : pb;
+        };
+        to_segment((kt0 - seg * per_seg) * BK);
+        auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa + oa[i], lds + buf * kBuf + wave * 1024 + i * (ROWS * BK * 2)); };
+        auto bring_b = [&](uint32_t buf, int i) {
+            load_to_lds((GATED && ROWS == 32 && (i & 1) ? pb2 : pb) + ob[i], lds + buf * kBuf + BM * BK * 2 + wave * 1024 + i * (ROWS * BK * 2));
+        };
+        auto next = [&]() {
+            pa += BK * 2;
+            pb += BK * 2;
+            pb2 += BK * 2;
+            if (--left == 0 && seg + 1 < p.nseg) {
+                ++seg;
+                left = per_seg;
+                to_segment(0);
             }
         };
-        uint32_t buf = 0;
-        bring(0);
-        for (uint32_t t = kt0; t < kt1; ++t) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();            // tile t is there, and every wave is past its reads of tile t - 1
-            if (t + 1 < kt1) bring(buf ^ 1);
-            multiply(buf);
-            buf ^= 1;
-        }
-        __syncthreads();
-    }
-
-    if (kt1 - kt0 == args.ksteps) {
-        float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);
+        auto bring = [&](uint32_t buf) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
-            ff_finish<T, EPI>(p, acc[i], mine, lane, m0 + (wm * MI + i) * 32, n0 + wn * (GATED ? 32 : 64));
-    } else {
+            for (int i = 0; i < LA; ++i) bring_a(buf, i);
+#pragma unroll
+            for (int i = 0; i < LB; ++i) bring_b(buf, i);
+            next();
+        };
+
+        f32x16 acc[MI][NI];
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *ff_slot<BM, BN>(args.part, worker + at, i, j, q, tid, NTH) =
-                        float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+        const uint32_t fr = lane & 31;          // row of a fragment
+
+        if constexpr (TURNS) {
+            // Of the two waves on a SIMD, one reads the fragments of a tile while the other multiplies the ones that it has read (and
+            // asks for a later tile in between); a barrier ends either's slot.  Group 0 reads tile t in slot 2 t and multiplies in
+            // 2 t + 1, group 1 one slot later.  Tile t + 3 is asked for in the multiplying of tile t, slots 2 t + 1 and 2 t + 2, into
+            // the buffer that was read last in slot 2 t - 1, and each group waits for its part of tile t + 1 before the barrier
+            // that ends slot 2 t + 1, four loads per tile.
+            static_assert(LA == 2 && LB == 2 && MI == 4, "");
+            const bool behind = wave >= 4;
+            const uint32_t fu = ((lane >> 5) ^ (fr / 4 & 3)) * 16, base = lds_address(lds);
+            const uint32_t ra0 = base + (wm * 128 + fr) * 64 + fu, rb0 = base + BM * 64 + (wn * 64 + fr) * 64 + fu;
+            // (beyond the last tile the last one is asked for again, and not read: the loop has no cases)
+            const uint32_t n = kt1 - kt0;
+            uint32_t asked = 0;
+            auto next_or_stay = [&]() {
+                if (++asked < n) next();
+            };
+#pragma unroll
+            for (uint32_t b = 0; b < 3; ++b) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) bring_a(b, i);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) bring_b(b, i);
+                next_or_stay();
+            }
+            wait_loads<8>();
+            slot_end();
+            if (behind) slot_end();
+            for (uint32_t t = 0; t < n; ++t) {
+                const uint32_t buf = (t & 3) * kBuf, to = (t + 3) & 3;
+                bf16x8 fa[2][4], fb[2][2];
+                read_fragments(ra0 + buf, rb0 + buf, fa, fb);
+                if (behind) wait_loads<4>();
+                slot_end();
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i < 2) bring_a(to, i);
+                    else bring_b(to, i - 2);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int kk = i / 2, ii = i % 2 * 2 + h;
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) acc[ii][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][ii], acc[ii][j], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                next_or_stay();
+                if (!behind) wait_loads<8>();
+                slot_end();
+            }
+            if (!behind) slot_end();
+            wait_loads<0>();
+            slot_end();
+        } else {
+            const uint32_t fu = ((lane >> 5) ^ (fr / 2 & 7)) * 16;      // to be xored with 2 k / 16
+            const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = BM * 128 + (wn * NI * 32 + fr) * 128 + fu;
+            auto multiply = [&](uint32_t buf) {
+                const unsigned char* const la = lds + buf * kBuf;
+#pragma unroll
+                for (int kk = 0; kk < BK / 16; ++kk) {
+                    bf16x8 fa[MI], fb[NI];
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+                }
+            };
+            uint32_t buf = 0;
+            bring(0);
+            for (uint32_t t = kt0; t < kt1; ++t) {
+                wait_loads<0>();
+                __syncthreads();            // tile t is there, and every wave is past its reads of tile t - 1
+                if (t + 1 < kt1) bring(buf ^ 1);
+                multiply(buf);
+                buf ^= 1;
+            }
+            __syncthreads();
+        }
+
+        if (kt1 - kt0 == args.ksteps) {
+            float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+                ff_finish<T, EPI>(p, acc[i], mine, lane, m0 + (wm * MI + i) * 32, n0 + wn * (GATED ? 32 : 64));
+        } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *ff_slot<BM, BN>(args.part, worker + at, i, j, q, tid, NTH) =
+                            float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        }
+        if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
     }
-    if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
-  }
 }
 
 // Adds up the sums that several workers have of a tile, in the order of the workers: 32 rows of every wave's part per block
