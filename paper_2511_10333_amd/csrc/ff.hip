@@ -139,42 +139,42 @@ struct Packer {
     }
 };
 
-// Blocks of a tile shape that share a compute unit (by LDS)
-constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / (2u * (bm + bn) * 128u); }
+// LDS of a tile shape: two buffers, of A three where there is room; blocks that share a compute unit's
+constexpr uint32_t lds_bytes(int bm, int bn) { return ((bm == 256 ? 3u : 2u) * bm + 2u * bn) * 128u; }
+constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / lds_bytes(bm, bn); }
 // The least k that is worth a worker, which then writes a tile's sums and has them read again
 constexpr uint64_t kMinK = 512;
 
-template <int BM, int BN, int WM, int WN, typename T, int EPI>
+template <int BM, int BN, typename T, int EPI>
 int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
     uint32_t tiles = 0;
     double flops = 0.0, bytes = 0.0;
     constexpr uint32_t COLS = EPI == kFfGate ? BN / 2 : BN;
-    constexpr int BK = ff_bk(WM, WN);
-    a.ksteps = a.p[0].ktiles * (kFfBk / BK) * a.p[0].nseg;
+    a.ksteps = a.p[0].ktiles * a.p[0].nseg;
     for (uint32_t i = 0; i < a.count; ++i) {
         FfProblem& p = a.p[i];
         p.tiles_m = (p.M + BM - 1) / BM;
         p.tiles_n = (p.N + COLS - 1) / COLS;
         p.first = tiles;
         tiles += p.tiles_m * p.tiles_n;
-        const double k = static_cast<double>(a.ksteps) * BK, both = EPI == kFfGate ? 2.0 : 1.0;
+        const double k = static_cast<double>(a.ksteps) * kFfBk, both = EPI == kFfGate ? 2.0 : 1.0;
         flops += 2.0 * p.M * p.N * k * both;
         bytes += 2.0 * (p.M + p.N * both) * k;
     }
     const uint32_t places = static_cast<uint32_t>(ctx->num_cu) * blocks_per_cu(BM, BN);
     a.whole = tiles / places * places;
     a.rest = tiles - a.whole;
-    a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, static_cast<uint64_t>(a.rest) * a.ksteps * BK / kMinK));
+    a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, static_cast<uint64_t>(a.rest) * a.ksteps * kFfBk / kMinK));
     // (a last round that is nearly full is not worth the sums' way through memory)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;
-    constexpr uint32_t lds = 2 * (BM + BN) * 128, threads = 64 * WM * WN;
-    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, WM, WN, T, EPI><<<a.whole + a.workers, threads, lds, st>>>(a));
+    constexpr uint32_t lds = lds_bytes(BM, BN);
+    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, T, EPI><<<a.whole + a.workers, 256, lds, st>>>(a));
     EDGC_HIP_TRY(ctx, hipGetLastError());
     if (a.rest) {
         EDGC_LAUNCH(ctx, st, KID_FF_JOIN, 4.0 * BM * BN * (a.workers + a.rest), 0.0,
-                    k_ff_join<BM, BN, WM, WN, T, EPI><<<a.rest * (BM / WM / 32), threads, 0, st>>>(a));
+                    k_ff_join<BM, BN, T, EPI><<<a.rest * (BM / 64) * (BN / 128), 256, 0, st>>>(a));
         EDGC_HIP_TRY(ctx, hipGetLastError());
     }
     return EDGC_OK;
@@ -197,16 +197,16 @@ int launch_product(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     };
     constexpr uint64_t half = EPI == kFfGate ? 2 : 1;
     if (time_of(256, 256 / half, 1.0) <= time_of(128, 128 / half, 0.25 * blocks_per_cu(128, 128) / 0.65))
-        return launch_tiles<256, 256, 2, 4, T, EPI>(ctx, a, kid, st);
-    return launch_tiles<128, 128, 2, 2, T, EPI>(ctx, a, kid, st);
+        return launch_tiles<256, 256, T, EPI>(ctx, a, kid, st);
+    return launch_tiles<128, 128, T, EPI>(ctx, a, kid, st);
 }
 
-template <int BM, int BN, int WM, int WN, typename T>
+template <int BM, int BN, typename T>
 hipError_t prepare_tiles()
 {
-    const int lds = 2 * (BM + BN) * 128;
-    for (const void* f : {reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, WM, WN, T, kFfStore>), reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, WM, WN, T, kFfGate>),
-                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, WM, WN, T, kFfDgate>)})
+    const int lds = lds_bytes(BM, BN);
+    for (const void* f : {reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfStore>), reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfGate>),
+                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfDgate>)})
         if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return e;
     return hipSuccess;
 }
@@ -377,8 +377,8 @@ int check_rows(edgc_ctx* ctx, const void* p, uint64_t ld, uint64_t cols, size_t 
 
 int prepare_ff_kernels(edgc_ctx* ctx)
 {
-    hipError_t e = prepare_tiles<256, 256, 2, 4, __bf16>();
-    if (e == hipSuccess) e = prepare_tiles<256, 256, 2, 4, float>();
+    hipError_t e = prepare_tiles<256, 256, __bf16>();
+    if (e == hipSuccess) e = prepare_tiles<256, 256, float>();
     EDGC_HIP_TRY(ctx, e);
     return EDGC_OK;
 }

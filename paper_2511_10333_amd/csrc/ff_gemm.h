@@ -5,14 +5,16 @@
 // bits, cut off, not rounded); six products of planes, 2^-24 of the operands left out, are six segments of one sum.  Six bf16 MFMAs
 // take less time than one of fp32 (2.5e15 / 6 against 0.16e15 operations a second).
 //
-// A block of WM x WN waves makes a BM x BN tile; tiles of 64 or 32 k of the operands come to LDS buffers while earlier ones are
-// multiplied.  A row of 128 (64) bytes lies in LDS as eight (four) 16-byte units, unit c at c ^ (row / 2 & 7) (at
-// c ^ (row / 4 & 3)): a read of 16 bytes per lane takes lanes 0-3, 12-15 and 20-27 of either half at once, then the other sixteen,
-// and their rows then lie in different banks.  (At c ^ (row & 7) and c ^ (row / 2 & 3) half of LDS's cycles were conflicts.)  The MFMA's first operand is B: a lane then holds four
+// A block of 2 x 2 waves makes a BM x BN tile; tiles of 64 k of the operands come straight to LDS while earlier ones are multiplied.  A
+// row of 128 bytes lies there as eight 16-byte units, unit c at c ^ (row / 2 & 7): a read of 16 bytes per lane takes lanes 0-3, 12-15
+// and 20-27 of either half at once, then the other sixteen, and their rows then lie in different banks.  (At c ^ (row & 7) half of
+// LDS's cycles were conflicts.)  The MFMA's first operand is B: a lane then holds four
 // neighbouring n of one m, which is what the epilogues load and store.
 #pragma once
 
 #include "compress_common.h"
+
+#include <type_traits>
 
 namespace edgc {
 
@@ -56,20 +58,22 @@ __host__ __device__ inline uint64_t ff_share(const FfArgs& a, uint32_t w)
 
 enum FfEpi { kFfStore = 0, kFfGate = 1, kFfDgate = 2 };
 
-// Activation and derivative.  gelu_tanh by the identity (1 + tanh t) / 2 = 1 / (1 + exp(-2 t)).
+// Activation and derivative.  gelu_tanh by the identity (1 + tanh t) / 2 = 1 / (1 + exp(-2 t)).  The hardware's powers of two and
+// reciprocals, exact to an ulp: an epilogue of library calls took a quarter of the time of the products of a tile of 5120 k.
+__device__ __forceinline__ float ff_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z)); }
 __device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
 {
     if (act == EDGC_SILU) {
-        const float s = 1.0f / (1.0f + expf(-z));
+        const float s = ff_sigmoid(z);
         a = z * s;
         da = s * (1.0f + z * (1.0f - s));
     } else if (act == EDGC_GELU) {
         const float cdf = 0.5f * erfcf(z * -0.70710678118654752f);
         a = z * cdf;
-        da = cdf + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+        da = cdf + z * __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z) * 0.39894228040143268f;
     } else {
         const float k = 0.79788456080286536f, c = 0.044715f;
-        const float s = 1.0f / (1.0f + expf(-2.0f * k * (z + c * z * z * z)));
+        const float s = ff_sigmoid(2.0f * k * (z + c * z * z * z));
         a = z * s;
         da = s + 2.0f * k * z * s * (1.0f - s) * (1.0f + 3.0f * c * z * z);
     }
@@ -126,21 +130,21 @@ template <> struct FfType<float> {
     static __device__ __forceinline__ void widen(const Floats4& q, float (&v)[4]) { v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; }
     static __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { put_any(p, Floats4{v[0], v[1], v[2], v[3]}); }
 };
-// four neighbours of a row of n columns: what lies beyond is zero, and is not written
-template <typename T>
+// Four neighbours of a row of n columns; FULL: all of them in it.  What lies beyond is zero, and is not written.
+template <typename T, bool FULL>
 __device__ __forceinline__ void ff_load4(const T* row, uint32_t n0, uint32_t n, float (&v)[4])
 {
-    if (n0 + 4 <= n) {
+    if (FULL || n0 + 4 <= n) {
         FfType<T>::widen(FfType<T>::load4(row + n0), v);
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) v[i] = n0 + i < n ? static_cast<float>(row[n0 + i]) : 0.f;
     }
 }
-template <typename T>
+template <typename T, bool FULL>
 __device__ __forceinline__ void ff_store4(T* row, uint32_t n0, uint32_t n, const float (&v)[4])
 {
-    if (n0 + 4 <= n) {
+    if (FULL || n0 + 4 <= n) {
         FfType<T>::store4(row + n0, v);
     } else {
 #pragma unroll
@@ -149,41 +153,51 @@ __device__ __forceinline__ void ff_store4(T* row, uint32_t n0, uint32_t n, const
     }
 }
 
-// What becomes of four neighbouring sums of row m
-template <typename T, int EPI>
-__device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t m, uint32_t n0, float (&v)[4], float (&v2)[4])
+// What the epilogue of four neighbouring sums of a row loads: the kept projections, or what is added to
+struct FfLoaded {
+    float a[4], b[4];
+};
+template <typename T, int EPI, bool FULL>
+__device__ __forceinline__ void ff_load(const FfProblem& p, uint32_t m, uint32_t n0, FfLoaded& x)
+{
+    if constexpr (EPI == kFfDgate) {
+        ff_load4<T, FULL>(static_cast<const T*>(p.e0) + m * p.lde, n0, p.N, x.a);
+        ff_load4<T, FULL>(static_cast<const T*>(p.e1) + m * p.lde, n0, p.N, x.b);
+    } else if constexpr (EPI == kFfStore) {
+        if (p.accumulate) ff_load4<T, FULL>(static_cast<const T*>(p.out) + m * p.ldo, n0, p.N, x.a);
+    }
+}
+// What becomes of the sums
+template <typename T, int EPI, bool FULL>
+__device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t m, uint32_t n0, float (&v)[4], float (&v2)[4], const FfLoaded& x)
 {
     if constexpr (EPI == kFfStore) {
-        T* const row = static_cast<T*>(p.out) + m * p.ldo;
-        if (p.accumulate) {
-            float o[4];
-            ff_load4<T>(row, n0, p.N, o);
+        if (p.accumulate)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += o[i];
-        }
-        ff_store4<T>(row, n0, p.N, v);
+            for (int i = 0; i < 4; ++i) v[i] += x.a[i];
+        ff_store4<T, FULL>(static_cast<T*>(p.out) + m * p.ldo, n0, p.N, v);
     } else if constexpr (EPI == kFfGate) {
         float h[4];
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
             float a, da;
             ff_act(p.act, v[i], a, da);
-            h[i] = n0 + i < p.N ? a * v2[i] : 0.f;
+            h[i] = FULL || n0 + i < p.N ? a * v2[i] : 0.f;
         }
         FfType<T>::put4(static_cast<uint16_t*>(p.out) + m * p.ldo + n0, p.plane, h);
-        if (p.e0) ff_store4<T>(static_cast<T*>(p.e0) + m * p.lde, n0, p.N, v);
-        if (p.e1) ff_store4<T>(static_cast<T*>(p.e1) + m * p.lde, n0, p.N, v2);
+        if (p.e0) {
+            ff_store4<T, FULL>(static_cast<T*>(p.e0) + m * p.lde, n0, p.N, v);
+            ff_store4<T, FULL>(static_cast<T*>(p.e1) + m * p.lde, n0, p.N, v2);
+        }
     } else {
-        float g[4], u[4], dg[4], du[4], h[4];
-        ff_load4<T>(static_cast<const T*>(p.e0) + m * p.lde, n0, p.N, g);
-        ff_load4<T>(static_cast<const T*>(p.e1) + m * p.lde, n0, p.N, u);
+        float dg[4], du[4], h[4];
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
             float a, da;
-            ff_act(p.act, g[i], a, da);
-            const bool in = n0 + i < p.N;
-            h[i] = in ? a * u[i] : 0.f;
-            dg[i] = in ? v[i] * u[i] * da : 0.f;
+            ff_act(p.act, x.a[i], a, da);
+            const bool in = FULL || n0 + i < p.N;
+            h[i] = in ? a * x.b[i] : 0.f;
+            dg[i] = in ? v[i] * x.b[i] * da : 0.f;
             du[i] = in ? v[i] * a : 0.f;
         }
         const uint64_t at = m * p.ldo + n0;
@@ -213,38 +227,20 @@ __device__ __forceinline__ uint32_t lds_address(const void* p)
 {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
 }
-// 16 bytes from each lane's address to 16 bytes per lane, one after the other, from `to` on
-__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned char* to)
+// 16 bytes per lane from `base` + its offset to LDS, one lane's after the other's, from address `to` on.  An instruction of its own,
+// since the compiler would otherwise have every later read of LDS wait for it: wait_loads and a barrier stand before the reads.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to)
 {
-    __builtin_amdgcn_global_load_lds((global_byte*)from, (lds_byte*)to, 16, 0, 0);
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base));
 }
-// The fragments of a tile of 32 k: rows 32 apart lie 2048 bytes apart in LDS, the second 16 k at the address ^ 32
-__device__ __forceinline__ void read_fragments(uint32_t at_a, uint32_t at_b, bf16x8 (&fa)[2][4], bf16x8 (&fb)[2][2])
-{
-    asm volatile("ds_read_b128 %0, %12\n\t"
-                 "ds_read_b128 %8, %14\n\t"
-                 "ds_read_b128 %9, %14 offset:2048\n\t"
-                 "ds_read_b128 %1, %12 offset:2048\n\t"
-                 "ds_read_b128 %2, %12 offset:4096\n\t"
-                 "ds_read_b128 %3, %12 offset:6144\n\t"
-                 "ds_read_b128 %4, %13\n\t"
-                 "ds_read_b128 %10, %15\n\t"
-                 "ds_read_b128 %11, %15 offset:2048\n\t"
-                 "ds_read_b128 %5, %13 offset:2048\n\t"
-                 "ds_read_b128 %6, %13 offset:4096\n\t"
-                 "ds_read_b128 %7, %13 offset:6144\n\t"
-                 "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[0][2]), "=&v"(fa[0][3]), "=&v"(fa[1][0]), "=&v"(fa[1][1]),
-                   "=&v"(fa[1][2]), "=&v"(fa[1][3]), "=&v"(fb[0][0]), "=&v"(fb[0][1]), "=&v"(fb[1][0]), "=&v"(fb[1][1])
-                 : "v"(at_a), "v"(at_a ^ 32u), "v"(at_b), "v"(at_b ^ 32u)
-                 : "memory");
-}
+// every wave's reads of LDS and all but its last N loads are done
 template <int N>
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void slot_end()
+__device__ __forceinline__ void tile_barrier()
 {
     __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -256,65 +252,98 @@ __device__ __forceinline__ const FfProblem& ff_problem_of(const FfArgs& args, ui
     return args.p[pi];
 }
 
-// The sums of 32 rows of a wave, of which a lane holds row lane % 32 and of either half the columns 8 (v / 4) + 4 (lane / 32) + v % 4:
-// through LDS (the wave's own part of it), so that a row's columns are loaded and stored together.
+// f(0), f(1), .. f(N - 1), each with a constant (a loop of this length is not unrolled whatever it is told)
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void ff_each(F&& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        ff_each<N, I + 1>(f);
+    }
+}
+
+// The sums of 32 rows and 2 x 32 columns (gated: of either projection), of which a lane holds row lane % 32 and of either half the
+// columns 8 (v / 4) + 4 (lane / 32) + v % 4: through LDS (the wave's own part of it), so that a row's columns are loaded and stored together.
 constexpr uint32_t kFfRow = 68;         // floats: 64 and a pad that spreads the rows over the banks
+template <int EPI> constexpr uint32_t kFfLanes = EPI == kFfGate ? 8 : 16;       // per row, four columns each
+template <int EPI> constexpr int kFfPasses = 32 * kFfLanes<EPI> / 64;           // over the rows
+
+// what the epilogue of such a square loads, asked for ahead of it
 template <typename T, int EPI>
-__device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16 (&acc)[2], float* mine, uint32_t lane, uint32_t m0, uint32_t n0)
+__device__ __forceinline__ void ff_ask(const FfProblem& p, FfLoaded (&x)[kFfPasses<EPI>], uint32_t lane, uint32_t m0, uint32_t n0)
+{
+#pragma unroll
+    for (int k = 0; k < kFfPasses<EPI>; ++k)
+        ff_load<T, EPI, true>(p, m0 + k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>, n0 + lane % kFfLanes<EPI> * 4, x[k]);
+}
+// FULL: the square lies inside the output, and `x` holds what its epilogue loads
+template <typename T, int EPI, bool FULL>
+__device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left, const f32x16& right, float* mine, uint32_t lane, uint32_t m0,
+                                          uint32_t n0, const FfLoaded (&x)[kFfPasses<EPI>])
 {
     constexpr bool GATED = EPI == kFfGate;
-    constexpr uint32_t kLanes = GATED ? 8 : 16;     // per row, four columns each
-    const uint32_t c4 = (lane % kLanes) * 4, n = n0 + c4;
-    const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
+    const uint32_t c4 = lane % kFfLanes<EPI> * 4, n = n0 + c4;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float4 v = {acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
+            const f32x16& a = j ? right : left;
+            const float4 v = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
             *reinterpret_cast<float4*>(mine + (lane & 31) * kFfRow + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
         }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll 4
-    for (uint32_t r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-        const uint32_t r = r0 + lane / kLanes, m = m0 + r;
-        const float4 x = *reinterpret_cast<const float4*>(mine + r * kFfRow + c4);
-        const float4 x2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kFfRow + 32 + c4) : x;
-        if (m >= p.M || n >= n_end) continue;
-        float v[4] = {x.x, x.y, x.z, x.w}, v2[4] = {x2.x, x2.y, x2.z, x2.w};
-        ff_epilogue<T, EPI>(p, m, n, v, v2);
+    auto row = [&](int k, const FfLoaded& loaded) {
+        const uint32_t r = k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>;
+        const float4 s = *reinterpret_cast<const float4*>(mine + r * kFfRow + c4);
+        const float4 s2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kFfRow + 32 + c4) : s;
+        float v[4] = {s.x, s.y, s.z, s.w}, v2[4] = {s2.x, s2.y, s2.z, s2.w};
+        ff_epilogue<T, EPI, FULL>(p, m0 + r, n, v, v2, loaded);
+    };
+    if constexpr (FULL) {
+#pragma unroll
+        for (int k = 0; k < kFfPasses<EPI>; ++k) row(k, x[k]);
+    } else {
+        const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
+#pragma unroll 1
+        for (int k = 0; k < kFfPasses<EPI>; ++k) {
+            const uint32_t m = m0 + k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>;
+            if (m >= p.M || n >= n_end) continue;
+            FfLoaded loaded;
+            ff_load<T, EPI, false>(p, m, n, loaded);
+            row(k, loaded);
+        }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Where a worker leaves the sums of a tile: in the order of its registers
-template <int BM, int BN>
-__device__ __forceinline__ float4* ff_slot(float* part, uint32_t slot, uint32_t i, uint32_t j, uint32_t q, uint32_t tid, uint32_t threads)
+// Where a worker leaves the sums of a tile: in the order of its registers, NI squares of 32 x 32 in a row of them
+template <int BM, int BN, int NI>
+__device__ __forceinline__ float4* ff_slot(float* part, uint32_t slot, uint32_t i, uint32_t j, uint32_t q, uint32_t tid)
 {
-    return reinterpret_cast<float4*>(part + static_cast<uint64_t>(slot) * (BM * BN)) + ((i * 2 + j) * 4 + q) * threads + tid;
+    constexpr uint32_t threads = 256;
+    return reinterpret_cast<float4*>(part + static_cast<uint64_t>(slot) * (BM * BN)) + ((i * NI + j) * 4 + q) * threads + tid;
 }
 
-// Waves of a block that take turns (below): tiles of 32 k in four buffers.  Otherwise tiles of 64 k in two.
-constexpr bool ff_turns(int wm, int wn) { return wm * wn == 8; }
-constexpr int ff_bk(int wm, int wn) { return ff_turns(wm, wn) ? 32 : 64; }
+// Rows of B that a wave has of its NI * 32: gated, the first half are the first projection's and the others the second's
+template <bool GATED, int NI>
+__device__ __forceinline__ uint32_t ff_column(uint32_t row) { return GATED ? row / (NI * 32) * (NI * 16) + row % (NI * 16) : row; }
 
-template <int BM, int BN, int WM, int WN, typename T, int EPI>
-__global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
+template <int BM, int BN, typename T, int EPI>
+__global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
 {
-    constexpr bool GATED = EPI == kFfGate, TURNS = ff_turns(WM, WN);
-    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32, NI = 2, BK = ff_bk(WM, WN), UNITS = BK / 8;
-    constexpr int ROWS = NTH / UNITS, LA = BM / ROWS, LB = BN / ROWS;       // rows that the block brings at a time
-    static_assert(BN / WN == 64, "a wave has 64 columns; gated: 32 of either projection");
-    static_assert(ROWS == 128 || ROWS == 32, "rows of the two projections alternate by 32");
-    extern __shared__ __align__(16) unsigned char lds[];
-    constexpr uint32_t kBuf = (BM + BN) * BK * 2, kBufs = TURNS ? 4 : 2;
+    constexpr bool GATED = EPI == kFfGate, LARGE = BM == 256;
+    constexpr int MI = BM / 64, NI = BN / 64, LA = BM / 32, LB = BN / 32;       // squares of a wave; its loads per tile of 64 k
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
-    static_assert(WM * WN * 32 * kFfRow * 4 <= kBufs * kBuf, "the waves' parts of LDS in ff_finish fit where the tiles were");
+    constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = BN * 128, kAtB = kBufsA * kBytesA;
+    static_assert(MI == NI, "");
+    extern __shared__ __align__(16) unsigned char lds[];        // [kBufsA][kBytesA], [2][kBytesB]
+    static_assert(4 * 32 * kFfRow * 4 <= kAtB + 2 * kBytesB, "the waves' parts of LDS in ff_finish fit where the tiles were");
 
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / 2, wn = wave % 2;
     const bool shares = blockIdx.x >= args.whole;
     const uint32_t worker = blockIdx.x - args.whole;
     uint64_t step = shares ? ff_share(args, worker) : 0;
@@ -330,55 +359,50 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
         ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
         const uint32_t m0 = tm * BM, n0 = tn * COLS;
 
-        // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last): to unit
-        // tid % UNITS of the LDS row tid / UNITS and of those ROWS apart from it, whose bits choose which unit of the operand's.
+        // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last).  Load i of a wave
+        // fills the eight rows of LDS from 8 (4 i + wave) on, whose bits choose which unit of the operand's row goes where.
         uint32_t oa[LA], ob[LB];
-        const uint32_t unit = ((tid % UNITS) ^ (TURNS ? tid / UNITS / 4 & 3 : tid / UNITS / 2 & 7)) * 16;
+        const uint32_t row = wave * 8 + lane / 8, unit = (lane % 8 ^ row / 2 % 8) * 16;     // (32 rows on: the same unit)
 #pragma unroll
-        for (int i = 0; i < LA; ++i) {
-            const uint32_t row = min(tid / UNITS + i * ROWS, p.M - 1 - m0);
-            oa[i] = row * static_cast<uint32_t>(p.lda) * 2 + unit;
-        }
+        for (int i = 0; i < LA; ++i) oa[i] = min(row + i * 32, p.M - 1 - m0) * static_cast<uint32_t>(p.lda) * 2 + unit;
 #pragma unroll
-        for (int i = 0; i < LB; ++i) {
-            uint32_t row = tid / UNITS + i * ROWS;
-            if constexpr (GATED) row = row / 64 * 32 + row % 32;        // rows 64 w .. + 31: the first matrix, + 32 .. 63: the second
-            row = min(row, p.N - 1 - n0);
-            ob[i] = row * static_cast<uint32_t>(p.ldb) * 2 + unit;
-        }
-        // which of the two this wave brings, where it is the same for all its rows
-        const bool second = GATED && ROWS == 128 && (wave * (64 / UNITS) & 32);
+        for (int i = 0; i < LB; ++i)
+            ob[i] = min(ff_column<GATED, NI>(row + i * 32), p.N - 1 - n0) * static_cast<uint32_t>(p.ldb) * 2 + unit;
 
-        const uint32_t per_seg = p.ktiles * (64 / BK);
-        uint32_t seg = kt0 / per_seg, left = per_seg - (kt0 - seg * per_seg);
-        const unsigned char *pa, *pb, *pb2;
-        auto to_segment = [&](uint32_t k) {
-            const uint64_t a_at = m0 * p.lda + k, b_at = n0 * p.ldb + k;
-            pa = reinterpret_cast<const unsigned char*>(p.a[seg] + a_at);
-            pb = reinterpret_cast<const unsigned char*>((second ? p.b2[seg] : p.b[seg]) + b_at);
-            pb2 = GATED && ROWS == 32 ? reinterpret_cast<const unsigned char*>(p.b2[seg] + b_at) : pb;
+        const uint32_t per_seg = p.ktiles;
+        const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
+        // where the next tile of either operand is; B comes later than A, so each has a place of its own
+        struct Place {
+            uint32_t seg, left;
         };
-        to_segment((kt0 - seg * per_seg) * BK);
-        auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa + oa[i], lds + buf * kBuf + wave * 1024 + i * (ROWS * BK * 2)); };
-        auto bring_b = [&](uint32_t buf, int i) {
-            load_to_lds((GATED && ROWS == 32 && (i & 1) ? pb2 : pb) + ob[i], lds + buf * kBuf + BM * BK * 2 + wave * 1024 + i * (ROWS * BK * 2));
-        };
-        auto next = [&]() {
-            pa += BK * 2;
-            pb += BK * 2;
-            pb2 += BK * 2;
-            if (--left == 0 && seg + 1 < p.nseg) {
-                ++seg;
-                left = per_seg;
-                to_segment(0);
+        Place na{kt0 / per_seg, 0}, nb;
+        na.left = per_seg - (kt0 - na.seg * per_seg);
+        nb = na;
+        const uint32_t k0 = (kt0 - na.seg * per_seg) * kFfBk;
+        const uint16_t *pa = p.a[na.seg] + a_row0 + k0, *pb = p.b[nb.seg] + b_row0 + k0;
+        const uint16_t* pb2 = GATED ? p.b2[nb.seg] + b_row0 + k0 : pb;
+        auto next_a = [&]() {
+            pa += kFfBk;
+            if (--na.left == 0 && na.seg + 1 < p.nseg) {
+                pa = p.a[++na.seg] + a_row0;
+                na.left = per_seg;
             }
         };
-        auto bring = [&](uint32_t buf) {
-#pragma unroll
-            for (int i = 0; i < LA; ++i) bring_a(buf, i);
-#pragma unroll
-            for (int i = 0; i < LB; ++i) bring_b(buf, i);
-            next();
+        auto next_b = [&]() {
+            pb += kFfBk;
+            pb2 += kFfBk;
+            if (--nb.left == 0 && nb.seg + 1 < p.nseg) {
+                pb = p.b[++nb.seg] + b_row0;
+                pb2 = GATED ? p.b2[nb.seg] + b_row0 : pb;
+                nb.left = per_seg;
+            }
+        };
+        const uint32_t base = lds_address(lds) + wave * 1024;
+        auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa, oa[i], base + buf * kBytesA + i * 4096); };
+        auto bring_b = [&](uint32_t buf, int i) {
+            // gated: LB / 2 loads of either matrix for each wave of the tile's columns
+            const bool second = GATED && (i * 32) % (NI * 32) >= NI * 16;
+            load_to_lds(second ? pb2 : pb, ob[i], base + kAtB + buf * kBytesB + i * 4096);
         };
 
         f32x16 acc[MI][NI];
@@ -388,98 +412,91 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-        const uint32_t fr = lane & 31;          // row of a fragment
 
-        if constexpr (TURNS) {
-            // Of the two waves on a SIMD, one reads the fragments of a tile while the other multiplies the ones that it has read (and
-            // asks for a later tile in between); a barrier ends either's slot.  Group 0 reads tile t in slot 2 t and multiplies in
-            // 2 t + 1, group 1 one slot later.  Tile t + 3 is asked for in the multiplying of tile t, slots 2 t + 1 and 2 t + 2, into
-            // the buffer that was read last in slot 2 t - 1, and each group waits for its part of tile t + 1 before the barrier
-            // that ends slot 2 t + 1, four loads per tile.
-            static_assert(LA == 2 && LB == 2 && MI == 4, "");
-            const bool behind = wave >= 4;
-            const uint32_t fu = ((lane >> 5) ^ (fr / 4 & 3)) * 16, base = lds_address(lds);
-            const uint32_t ra0 = base + (wm * 128 + fr) * 64 + fu, rb0 = base + BM * 64 + (wn * 64 + fr) * 64 + fu;
-            // (beyond the last tile the last one is asked for again, and not read: the loop has no cases)
-            const uint32_t n = kt1 - kt0;
-            uint32_t asked = 0;
-            auto next_or_stay = [&]() {
-                if (++asked < n) next();
-            };
+        // A tile's four steps of 16 k: while one is multiplied, the fragments of the next are read (in the last one, the first of the
+        // next tile).  The barrier before the last step ends the reads of the tile: from there on B of tile t + 2 is asked for, into
+        // the place of tile t's.  A has three buffers where they fit (LARGE), and A of tile t + 2 is asked for in the first two
+        // steps of tile t.  Either has four steps at least to come: the barrier of tile t has to find tile t + 1 there, and after that
+        // tile was asked for came A of tile t + 2 only.
+        const uint32_t fr = lane & 31, fu = ((lane >> 5) ^ (fr / 2 & 7)) * 16;  // row of a fragment; its unit, to be xored with 2 k / 16
+        const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = kAtB + (wn * NI * 32 + fr) * 128 + fu;
+        const uint32_t n = kt1 - kt0;
+        bf16x8 fa[2][MI], fb[2][NI];
+        auto read = [&](uint32_t buf_a, uint32_t buf_b, int kk, int f) {        // fragment f of the step: NI of B, MI of A, as they are used
+            const int to = kk & 1;
+            if (f < NI) fb[to][f] = *reinterpret_cast<const bf16x8*>(lds + ((rb0 + buf_b * kBytesB) ^ (kk * 32)) + f * 4096);
+            else fa[to][f - NI] = *reinterpret_cast<const bf16x8*>(lds + ((ra0 + buf_a * kBytesA) ^ (kk * 32)) + (f - NI) * 4096);
+        };
+        for (uint32_t t = 0; t < 2 && t < n; ++t) {
 #pragma unroll
-            for (uint32_t b = 0; b < 3; ++b) {
+            for (int i = 0; i < LA; ++i) bring_a(t, i);
+            next_a();
 #pragma unroll
-                for (int i = 0; i < 2; ++i) bring_a(b, i);
+            for (int i = 0; i < LB; ++i) bring_b(t, i);
+            next_b();
+        }
+        if (n > 1) tile_barrier<LA + LB>();
+        else tile_barrier<0>();
 #pragma unroll
-                for (int i = 0; i < 2; ++i) bring_b(b, i);
-                next_or_stay();
-            }
-            wait_loads<8>();
-            slot_end();
-            if (behind) slot_end();
-            for (uint32_t t = 0; t < n; ++t) {
-                const uint32_t buf = (t & 3) * kBuf, to = (t + 3) & 3;
-                bf16x8 fa[2][4], fb[2][2];
-                read_fragments(ra0 + buf, rb0 + buf, fa, fb);
-                if (behind) wait_loads<4>();
-                slot_end();
-                __builtin_amdgcn_s_setprio(1);
+        for (int f = 0; f < MI + NI; ++f) read(0, 0, 0, f);
+        uint32_t buf_a = 0, ask_a = kBufsA - 1;     // buffers of this tile's A and of the one asked for next
+        for (uint32_t t = 0; t < n; ++t) {
+            const uint32_t buf_b = t & 1, next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1;
+            const bool more_a = LARGE && t + 2 < n, more_b = t + 2 < n;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (i < 2) bring_a(to, i);
-                    else bring_b(to, i - 2);
-                    __builtin_amdgcn_sched_barrier(0);
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk == 3) {
+                    if (more_a) tile_barrier<LA>();
+                    else tile_barrier<0>();
+                }
+                const int from = kk & 1;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int kk = i / 2, ii = i % 2 * 2 + h;
-#pragma unroll
-                        for (int j = 0; j < NI; ++j) acc[ii][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][ii], acc[ii][j], 0, 0, 0);
+                for (int c = 0; c < MI + NI; ++c) {
+                    if (kk < 3) read(buf_a, buf_b, kk + 1, c);
+                    else read(next_buf_a, buf_b ^ 1, 0, c);
+                    if (LARGE && kk < 2 && more_a && c % 2 == 0) bring_a(ask_a, kk * (LA / 2) + c / 2);
+                    if (kk == 3 && more_b) {
+                        bring_b(buf_b, c);
+                        if (!LARGE) bring_a(buf_b, c);
                     }
                     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int m = c * MI * NI / (MI + NI); m < (c + 1) * MI * NI / (MI + NI); ++m)
+                        acc[m / NI][m % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][m % NI], fa[from][m / NI], acc[m / NI][m % NI], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_s_setprio(0);
-                next_or_stay();
-                if (!behind) wait_loads<8>();
-                slot_end();
+                if (LARGE && kk == 1 && more_a) next_a();
             }
-            if (!behind) slot_end();
-            wait_loads<0>();
-            slot_end();
-        } else {
-            const uint32_t fu = ((lane >> 5) ^ (fr / 2 & 7)) * 16;      // to be xored with 2 k / 16
-            const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = BM * 128 + (wn * NI * 32 + fr) * 128 + fu;
-            auto multiply = [&](uint32_t buf) {
-                const unsigned char* const la = lds + buf * kBuf;
-#pragma unroll
-                for (int kk = 0; kk < BK / 16; ++kk) {
-                    bf16x8 fa[MI], fb[NI];
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(la + (ra0 ^ (kk * 32)) + i * 4096);
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(la + (rb0 ^ (kk * 32)) + j * 4096);
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-#pragma unroll
-                        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-                }
-            };
-            uint32_t buf = 0;
-            bring(0);
-            for (uint32_t t = kt0; t < kt1; ++t) {
-                wait_loads<0>();
-                __syncthreads();            // tile t is there, and every wave is past its reads of tile t - 1
-                if (t + 1 < kt1) bring(buf ^ 1);
-                multiply(buf);
-                buf ^= 1;
+            if (more_b) {
+                next_b();
+                if (!LARGE) next_a();
             }
-            __syncthreads();
+            buf_a = next_buf_a;
+            ask_a = ask_a + 1 == kBufsA ? 0 : ask_a + 1;
         }
+        tile_barrier<0>();
 
         if (kt1 - kt0 == args.ksteps) {
             float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-                ff_finish<T, EPI>(p, acc[i], mine, lane, m0 + (wm * MI + i) * 32, n0 + wn * (GATED ? 32 : 64));
+            auto m_of = [&](int s) { return m0 + (wm * MI + s / (NI / 2)) * 32; };
+            auto n_of = [&](int s) { return n0 + (GATED ? wn * NI * 16 + s % (NI / 2) * 32 : wn * NI * 32 + s % (NI / 2) * 64); };
+            auto left_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][(GATED ? 1 : 2) * (s % (NI / 2))]; };
+            auto right_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][GATED ? s % (NI / 2) + NI / 2 : 2 * (s % (NI / 2)) + 1]; };
+            constexpr int SQUARES = MI * NI / 2;
+            FfLoaded x[2][kFfPasses<EPI>];
+            if (m0 + BM <= p.M && n0 + COLS <= p.N) {
+                ff_ask<T, EPI>(p, x[0], lane, m_of(0), n_of(0));
+                ff_each<SQUARES>([&](auto sq) {
+                    constexpr int s = decltype(sq)::value;
+                    if constexpr (s + 1 < SQUARES) ff_ask<T, EPI>(p, x[(s + 1) & 1], lane, m_of(s + 1), n_of(s + 1));
+                    ff_finish<T, EPI, true>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[s & 1]);
+                });
+            } else {
+                ff_each<SQUARES>([&](auto sq) {
+                    constexpr int s = decltype(sq)::value;
+                    ff_finish<T, EPI, false>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[0]);
+                });
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < MI; ++i)
@@ -487,41 +504,46 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ff_gemm(const FfArgs args)
                 for (int j = 0; j < NI; ++j)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *ff_slot<BM, BN>(args.part, worker + at, i, j, q, tid, NTH) =
+                        *ff_slot<BM, BN, NI>(args.part, worker + at, i, j, q, tid) =
                             float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         }
         if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
     }
 }
 
-// Adds up the sums that several workers have of a tile, in the order of the workers: 32 rows of every wave's part per block
-template <int BM, int BN, int WM, int WN, typename T, int EPI>
-__global__ __launch_bounds__(64 * WM * WN) void k_ff_join(const FfArgs args)
+// Adds up the sums that several workers have of a tile, in the order of the workers: 32 rows and a pair of squares of every wave's
+// part per block
+template <int BM, int BN, typename T, int EPI>
+__global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
 {
-    constexpr int NTH = 64 * WM * WN, MI = BM / WM / 32;
+    constexpr int MI = BM / 64, NI = BN / 64;
     constexpr bool GATED = EPI == kFfGate;
-    __shared__ float stage[WM * WN * 32 * kFfRow];
-    const uint32_t at = blockIdx.x / MI, i = blockIdx.x % MI, tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    __shared__ float stage[4 * 32 * kFfRow];
+    const uint32_t per = MI * NI / 2, at = blockIdx.x / per, i = blockIdx.x % per / (NI / 2), j = blockIdx.x % (NI / 2);
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     const uint64_t s0 = static_cast<uint64_t>(at) * args.ksteps, s1 = s0 + args.ksteps, all = static_cast<uint64_t>(args.rest) * args.ksteps;
     uint32_t w = static_cast<uint32_t>(s0 * args.workers / all);
     while (ff_share(args, w + 1) <= s0) ++w;        // the first worker with a step of this tile
     if (ff_share(args, w) <= s0 && ff_share(args, w + 1) >= s1) return;     // which had them all
+    const uint32_t js[2] = {GATED ? j : 2 * j, GATED ? j + NI / 2 : 2 * j + 1};
     f32x16 acc[2] = {};
     for (; w < args.workers && ff_share(args, w) < s1; ++w) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float4 v = *ff_slot<BM, BN>(args.part, w + at, i, j, q, tid, NTH);
-                acc[j][4 * q] += v.x; acc[j][4 * q + 1] += v.y; acc[j][4 * q + 2] += v.z; acc[j][4 * q + 3] += v.w;
+                const float4 v = *ff_slot<BM, BN, NI>(args.part, w + at, i, js[h], q, tid);
+                acc[h][4 * q] += v.x; acc[h][4 * q + 1] += v.y; acc[h][4 * q + 2] += v.z; acc[h][4 * q + 3] += v.w;
             }
     }
     const uint32_t tile = args.whole + at;
     const FfProblem& p = ff_problem_of(args, tile);
     uint32_t tm, tn;
     ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
-    ff_finish<T, EPI>(p, acc, stage + wave * (32 * kFfRow), lane, tm * BM + (wave / WN * MI + i) * 32,
-                      tn * (GATED ? BN / 2 : BN) + wave % WN * (GATED ? 32 : 64));
+    const uint32_t wm = wave / 2, wn = wave % 2;
+    const FfLoaded none[kFfPasses<EPI>] = {};
+    ff_finish<T, EPI, false>(p, acc[0], acc[1], stage + wave * (32 * kFfRow), lane, tm * BM + (wm * MI + i) * 32,
+                             tn * (GATED ? BN / 2 : BN) + (GATED ? wn * NI * 16 + j * 32 : wn * NI * 32 + j * 64), none);
 }
 
 }  // namespace edgc
