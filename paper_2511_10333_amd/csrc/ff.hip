@@ -11,60 +11,62 @@
 
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 namespace edgc {
 namespace {
 
 // ---------------------------------------------------------------------------------------------
-// Copies into operand form: 64 x 64 elements per block, up to kPacks matrices per launch
+// Copies into operand form: rows and columns padded with zeros to multiples of 64, fp32 as three planes.  64 x 64 elements per block, a
+// thread eight neighbours at a time; up to kPacks matrices per launch
 // ---------------------------------------------------------------------------------------------
-constexpr int kPacks = 6;
+constexpr int kPacks = 5;
 struct PackItem {
     const void* src;
     uint16_t* dst;
-    uint64_t ld, ldd, plane, src_plane;     // elements: of the source, the copy; between planes of the copy, of the source
+    uint64_t ld, ldd, plane;                // elements: of the source, the copy; between planes of the copy
     uint32_t rows, cols, tiles_c, first;    // of the source; tiles across; first block
-    uint32_t trans;
 };
 struct PackList {
     PackItem t[kPacks];
     uint32_t count, blocks;
 };
-
-// T: element of the source; PLANES: what one element becomes
-template <typename T, int PLANES>
+template <typename T>
 __global__ __launch_bounds__(256) void k_ff_pack(const PackList list)
 {
-    __shared__ uint16_t s[PLANES][64][66];
+    constexpr int P = FfType<T>::kPlanes;
     uint32_t k = 0;
 #pragma unroll
     for (int i = 1; i < kPacks; ++i) k += (static_cast<uint32_t>(i) < list.count && blockIdx.x >= list.t[i].first) ? 1u : 0u;
     const PackItem& t = list.t[k];
-    const uint32_t id = blockIdx.x - t.first, r0 = id / t.tiles_c * 64, c0 = id % t.tiles_c * 64;
-    const uint32_t cl = threadIdx.x % 64, rl = threadIdx.x / 64;
-    const T* const src = static_cast<const T*>(t.src) + blockIdx.y * t.src_plane;
-    uint16_t* const dst = t.dst + blockIdx.y * t.plane;
+    const uint32_t id = blockIdx.x - t.first, c = id % t.tiles_c * 64 + threadIdx.x % 8 * 8;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t r = rl + i * 4;
-        uint16_t p[PLANES] = {};
-        if (r0 + r < t.rows && c0 + cl < t.cols) {
-            const T v = src[(r0 + r) * t.ld + c0 + cl];
-            if constexpr (PLANES == 3) ff_planes(v, p);
-            else p[0] = __builtin_bit_cast(uint16_t, v);
+    for (int half = 0; half < 2; ++half) {
+        const uint32_t r = id / t.tiles_c * 64 + half * 32 + threadIdx.x / 8;
+        float v[2][4] = {};
+        if (r < t.rows) {
+            const T* const row = static_cast<const T*>(t.src) + r * t.ld;
+            ff_load4<T, false>(row, c, t.cols, v[0]);
+            ff_load4<T, false>(row, c + 4, t.cols, v[1]);
         }
+        uint16_t* const to = t.dst + r * t.ldd + c;
+        if constexpr (P == 1) {
+            bf16x8 w[1];
+            const float all[8] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+            pack8<1>(all, w);
+            *reinterpret_cast<bf16x8*>(to) = w[0];
+        } else {
+            uint16_t q[8][3];
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q) s[q][r][cl] = p[q];
-    }
-    __syncthreads();
-    // rows of the copy: source rows (columns of the source where transposed); zeros up to its padded length
-    const uint32_t d0 = t.trans ? c0 : r0, e0 = t.trans ? r0 : c0, dn = t.trans ? t.cols : t.rows;
+            for (int e = 0; e < 8; ++e) ff_planes(v[e / 4][e % 4], q[e]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t r = rl + i * 4;
-        if (d0 + r >= dn) continue;
+            for (int p = 0; p < 3; ++p) {
+                u32x4 w;
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q) dst[q * t.plane + (d0 + r) * t.ldd + e0 + cl] = t.trans ? s[q][cl][r] : s[q][r][cl];
+                for (int e = 0; e < 4; ++e) w[e] = q[2 * e][p] | static_cast<uint32_t>(q[2 * e + 1][p]) << 16;
+                *reinterpret_cast<u32x4*>(to + p * t.plane) = w;
+            }
+        }
     }
 }
 
@@ -80,30 +82,26 @@ struct Operand {
 
 // Where a pass keeps its operands, in elements of 16 bits from the start of the scratch; the sizes count every operand as copied.
 struct FfPlan {
-    uint64_t T, H, F, Tp, Hp, Fp, planes, used = 0;
+    uint64_t T, H, F, planes, used = 0;     // tokens, hidden, ff, padded
     FfPlan(uint64_t tokens, uint64_t hidden, uint64_t ff, edgc_dtype dt)
-        : T(tokens), H(hidden), F(ff), Tp(pad64(tokens)), Hp(pad64(hidden)), Fp(pad64(ff)), planes(dt == EDGC_F32 ? 3 : 1) {}
+        : T(pad64(tokens)), H(pad64(hidden)), F(pad64(ff)), planes(dt == EDGC_F32 ? 3 : 1) {}
     uint64_t take(uint64_t rows, uint64_t ld)
     {
         const uint64_t at = used;
         used += planes * rows * ld;         // (rows of 128 bytes: everything stays 16-byte aligned)
         return at;
     }
-    // forward
-    uint64_t x = 0, wg = 0, wu = 0, wd = 0, h = 0;
+    uint64_t x = 0, wg = 0, wu = 0, wd = 0, h = 0, dy = 0, dg = 0, du = 0;
     uint64_t forward()
     {
         used = 0;
-        x = take(T, Hp); wg = take(F, Hp); wu = take(F, Hp); wd = take(H, Fp); h = take(T, Fp);
+        x = take(T, H); wg = take(F, H); wu = take(F, H); wd = take(H, F); h = take(T, F);
         return used;
     }
-    // backward
-    uint64_t dy = 0, wdt = 0, dg = 0, du = 0, wgt = 0, wut = 0, ht = 0, dgt = 0, dut = 0, xt = 0, dyt = 0;
     uint64_t backward()
     {
-        used = 0;
-        dy = take(T, Hp); wdt = take(F, Hp); h = take(T, Fp); dg = take(T, Fp); du = take(T, Fp); wgt = take(H, Fp); wut = take(H, Fp);
-        ht = take(F, Tp); dgt = take(F, Tp); dut = take(F, Tp); xt = take(H, Tp); dyt = take(H, Tp);
+        forward();
+        dy = take(T, H); dg = take(T, F); du = take(T, F);
         return used;
     }
 };
@@ -114,25 +112,24 @@ struct Packer {
     edgc_ctx* ctx;
     hipStream_t st;
     PackList list{};
-    // copies rows x cols (ld) to `dst`, k padded; planes: of a source that is planes already
-    void add(const void* src, uint64_t ld, uint64_t src_plane, uint64_t rows, uint64_t cols, bool trans, uint16_t* dst, uint64_t plane)
+    void add(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, uint16_t* dst)
     {
         PackItem& t = list.t[list.count++];
-        t.src = src; t.dst = dst; t.ld = ld; t.src_plane = src_plane;
+        t.src = src; t.dst = dst; t.ld = ld;
         t.rows = static_cast<uint32_t>(rows); t.cols = static_cast<uint32_t>(cols);
-        t.trans = trans; t.plane = plane; t.ldd = pad64(trans ? rows : cols);
+        t.ldd = pad64(cols); t.plane = pad64(rows) * t.ldd;
         t.tiles_c = static_cast<uint32_t>(pad64(cols) / 64);
         t.first = list.blocks;
         list.blocks += static_cast<uint32_t>(pad64(rows) / 64) * t.tiles_c;
     }
-    template <typename T, int PLANES>
-    int flush(uint32_t z)
+    template <typename T>
+    int flush()
     {
         if (list.count == 0) return EDGC_OK;
         double bytes = 0.0;
         for (uint32_t i = 0; i < list.count; ++i)
-            bytes += static_cast<double>(list.t[i].rows) * list.t[i].cols * z * (sizeof(T) + 2.0 * PLANES);
-        EDGC_LAUNCH(ctx, st, KID_FF_PACK, bytes, 0.0, k_ff_pack<T, PLANES><<<dim3(list.blocks, z), 256, 0, st>>>(list));
+            bytes += static_cast<double>(list.t[i].rows) * list.t[i].cols * (sizeof(T) + 2.0 * FfType<T>::kPlanes);
+        EDGC_LAUNCH(ctx, st, KID_FF_PACK, bytes, 0.0, k_ff_pack<T><<<list.blocks, 256, 0, st>>>(list));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         list = PackList{};
         return EDGC_OK;
@@ -145,7 +142,7 @@ constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / lds_byt
 // The least k that is worth a worker, which then writes a tile's sums and has them read again
 constexpr uint64_t kMinK = 512;
 
-template <int BM, int BN, typename T, int EPI>
+template <int BM, int BN, bool TA, bool TB, typename T, int EPI>
 int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
     uint32_t tiles = 0;
@@ -170,7 +167,7 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;
     constexpr uint32_t lds = lds_bytes(BM, BN);
-    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, T, EPI><<<a.whole + a.workers, 256, lds, st>>>(a));
+    EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, TA, TB, T, EPI><<<a.whole + a.workers, 256, lds, st>>>(a));
     EDGC_HIP_TRY(ctx, hipGetLastError());
     if (a.rest) {
         EDGC_LAUNCH(ctx, st, KID_FF_JOIN, 4.0 * BM * BN * (a.workers + a.rest), 0.0,
@@ -183,7 +180,7 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 // Sums that workers can leave behind: at most two per place of the larger tile shape
 uint64_t part_elems(const edgc_ctx* ctx) { return 2ull * ctx->num_cu * std::max(256 * 256 * blocks_per_cu(256, 256), 128 * 128 * blocks_per_cu(128, 128)); }
 
-template <typename T, int EPI>
+template <bool TA, bool TB, typename T, int EPI>
 int launch_product(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
 {
     // The time that either tile shape would take, in steps of 64 k of a 256 x 256 tile on a compute unit.  Measured: a tile of 128 x 128
@@ -197,17 +194,19 @@ int launch_product(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     };
     constexpr uint64_t half = EPI == kFfGate ? 2 : 1;
     if (time_of(256, 256 / half, 1.0) <= time_of(128, 128 / half, 0.25 * blocks_per_cu(128, 128) / 0.65))
-        return launch_tiles<256, 256, T, EPI>(ctx, a, kid, st);
-    return launch_tiles<128, 128, T, EPI>(ctx, a, kid, st);
+        return launch_tiles<256, 256, TA, TB, T, EPI>(ctx, a, kid, st);
+    return launch_tiles<128, 128, TA, TB, T, EPI>(ctx, a, kid, st);
 }
 
 template <int BM, int BN, typename T>
 hipError_t prepare_tiles()
 {
-    const int lds = lds_bytes(BM, BN);
-    for (const void* f : {reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfStore>), reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfGate>),
-                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, T, kFfDgate>)})
-        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return e;
+    for (const void* f : {reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, false, T, kFfStore>),
+                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, true, T, kFfStore>),
+                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, true, true, T, kFfStore>),
+                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, false, T, kFfGate>),
+                          reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, true, T, kFfDgate>)})
+        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(BM, BN))) return e;
     return hipSuccess;
 }
 
@@ -230,114 +229,117 @@ template <typename T>
 struct FfPass {
     static constexpr int P = FfType<T>::kPlanes;
     edgc_ctx* ctx;
-    hipStream_t st;
     uint16_t* ws;
     Packer pk;
-    FfPass(edgc_ctx* c, hipStream_t s) : ctx(c), st(s), ws(static_cast<uint16_t*>(c->ff.ws)), pk{c, s} {}
+    FfPass(edgc_ctx* c, hipStream_t s) : ctx(c), ws(static_cast<uint16_t*>(c->ff.ws)), pk{c, s} {}
 
-    // a caller's matrix as an operand: as it stands where its rows allow it
-    Operand operand(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, bool trans, uint64_t at)
+    // a matrix in the scratch
+    Operand own(uint64_t at, uint64_t rows, uint64_t cols) const { return {ws + at, pad64(cols), pad64(rows) * pad64(cols)}; }
+    // Whether a caller's matrix can be an operand as it stands, with k along its columns, its rows, or (in two products) either:
+    // whole 16-byte units, whole tiles of 64 k
+    static bool stands(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, bool k_cols, bool k_rows)
     {
-        if (P == 1 && !trans && aligned_to(src, 16) && ld % 8 == 0 && cols % 64 == 0 && ld <= kFfMaxLd)
-            return {static_cast<const uint16_t*>(src), ld, 0};
-        const uint64_t ldd = pad64(trans ? rows : cols), plane = (trans ? cols : rows) * ldd;
-        pk.add(src, ld, 0, rows, cols, trans, ws + at, plane);
-        return {ws + at, ldd, plane};
+        return P == 1 && aligned_to(src, 16) && ld % 8 == 0 && ld <= kFfMaxLd && cols % (k_cols ? 64 : 8) == 0 && (!k_rows || rows % 64 == 0);
     }
-    // planes in the scratch, transposed
-    Operand transposed(uint64_t from, uint64_t rows, uint64_t cols, uint64_t at)
+    // it, or a copy of it
+    Operand operand(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, bool as_it_stands, uint64_t at)
     {
-        const uint64_t ld = pad64(cols), ldd = pad64(rows), plane = cols * ldd;
-        pk.add(ws + from, ld, rows * ld, rows, cols, true, ws + at, plane);
-        return {ws + at, ldd, plane};
+        if (as_it_stands) return {static_cast<const uint16_t*>(src), ld, 0};
+        pk.add(src, ld, rows, cols, ws + at);
+        return own(at, rows, cols);
+    }
+    Operand operand(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, bool k_cols, bool k_rows, uint64_t at)
+    {
+        return operand(src, ld, rows, cols, stands(src, ld, rows, cols, k_cols, k_rows), at);
+    }
+    // the weights of the two projections: one leading dimension for both
+    std::pair<Operand, Operand> projections(const edgc_ff& w, bool k_cols, const FfPlan& plan)
+    {
+        const bool both = w.ld_gate == w.ld_up && stands(w.w_gate, w.ld_gate, w.ff, w.hidden, k_cols, !k_cols) &&
+                          stands(w.w_up, w.ld_up, w.ff, w.hidden, k_cols, !k_cols);
+        return {operand(w.w_gate, w.ld_gate, w.ff, w.hidden, both, plan.wg), operand(w.w_up, w.ld_up, w.ff, w.hidden, both, plan.wu)};
     }
 };
 
 template <typename T>
-int ff_forward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t T_, void* y, uint64_t ldy, void* gate, void* up,
+int ff_forward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t tokens, void* y, uint64_t ldy, void* gate, void* up,
                uint64_t ldg, hipStream_t st)
 {
     constexpr int P = FfType<T>::kPlanes;
-    FfPlan plan(T_, w.hidden, w.ff, P == 3 ? EDGC_F32 : EDGC_BF16);
+    const uint64_t H = w.hidden, F = w.ff;
+    FfPlan plan(tokens, H, F, w.dtype);
     plan.forward();
     FfPass<T> pass(ctx, st);
-    const uint64_t H = w.hidden, F = w.ff;
-    const Operand ox = pass.operand(x, ldx, T_, H, false, plan.x), og = pass.operand(w.w_gate, w.ld_gate, F, H, false, plan.wg),
-                  ou = pass.operand(w.w_up, w.ld_up, F, H, false, plan.wu), od = pass.operand(w.w_down, w.ld_down, H, F, false, plan.wd);
-    Operand og2 = og, ou2 = ou;
-    if (og.ld != ou.ld) {       // one stride for both projections: copy what is not
-        if (og.ld != plan.Hp) og2 = {pass.ws + plan.wg, plan.Hp, F * plan.Hp}, pass.pk.add(w.w_gate, w.ld_gate, 0, F, H, false, pass.ws + plan.wg, F * plan.Hp);
-        if (ou.ld != plan.Hp) ou2 = {pass.ws + plan.wu, plan.Hp, F * plan.Hp}, pass.pk.add(w.w_up, w.ld_up, 0, F, H, false, pass.ws + plan.wu, F * plan.Hp);
-    }
-    if (int rc = pass.pk.template flush<T, P>(1)) return rc;
+    const Operand ox = pass.operand(x, ldx, tokens, H, true, false, plan.x);
+    const auto [og, ou] = pass.projections(w, true, plan);
+    const Operand od = pass.operand(w.w_down, w.ld_down, H, F, true, false, plan.wd), oh = pass.own(plan.h, tokens, F);
+    if (int rc = pass.pk.template flush<T>()) return rc;
     FfArgs a{};
     a.count = 1;
     FfProblem& p = a.p[0];
-    add_segments(p, ox, og2, &ou2, P);
-    p.M = static_cast<uint32_t>(T_); p.N = w.ff; p.ktiles = static_cast<uint32_t>(plan.Hp / kFfBk);
-    p.out = pass.ws + plan.h; p.ldo = plan.Fp; p.plane = T_ * plan.Fp; p.n_pad = static_cast<uint32_t>(plan.Fp);
+    add_segments(p, ox, og, &ou, P);
+    p.M = static_cast<uint32_t>(tokens); p.N = w.ff; p.ktiles = static_cast<uint32_t>(plan.H / kFfBk);
+    p.out = pass.ws + plan.h; p.ldo = oh.ld; p.plane = oh.plane; p.n_pad = static_cast<uint32_t>(plan.F); p.m_pad = p.M;
     p.e0 = gate; p.e1 = up; p.lde = ldg; p.act = w.act;
-    if (int rc = launch_product<T, kFfGate>(ctx, a, KID_FF_GATE, st)) return rc;
+    if (int rc = launch_product<false, false, T, kFfGate>(ctx, a, KID_FF_GATE, st)) return rc;
     FfArgs b{};
     b.count = 1;
     FfProblem& q = b.p[0];
-    add_segments(q, {pass.ws + plan.h, plan.Fp, T_ * plan.Fp}, od, nullptr, P);
-    q.M = static_cast<uint32_t>(T_); q.N = w.hidden; q.ktiles = static_cast<uint32_t>(plan.Fp / kFfBk);
+    add_segments(q, oh, od, nullptr, P);
+    q.M = static_cast<uint32_t>(tokens); q.N = w.hidden; q.ktiles = static_cast<uint32_t>(plan.F / kFfBk);
     q.out = y; q.ldo = ldy;
-    return launch_product<T, kFfStore>(ctx, b, KID_FF_DOWN, st);
+    return launch_product<false, false, T, kFfStore>(ctx, b, KID_FF_DOWN, st);
 }
 
 template <typename T>
-int ff_backward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t T_, const void* gate, const void* up, uint64_t ldg,
+int ff_backward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t tokens, const void* gate, const void* up, uint64_t ldg,
                 const void* dy, uint64_t ldy, void* dx, uint64_t lddx, void* dwg, uint64_t lddg, void* dwu, uint64_t lddu, void* dwd,
                 uint64_t lddd, int accumulate, hipStream_t st)
 {
     constexpr int P = FfType<T>::kPlanes;
-    FfPlan plan(T_, w.hidden, w.ff, P == 3 ? EDGC_F32 : EDGC_BF16);
+    const uint64_t H = w.hidden, F = w.ff;
+    FfPlan plan(tokens, H, F, w.dtype);
     plan.backward();
     FfPass<T> pass(ctx, st);
-    const uint64_t H = w.hidden, F = w.ff;
-    const Operand ody = pass.operand(dy, ldy, T_, H, false, plan.dy), owd = pass.operand(w.w_down, w.ld_down, H, F, true, plan.wdt),
-                  owg = pass.operand(w.w_gate, w.ld_gate, F, H, true, plan.wgt), owu = pass.operand(w.w_up, w.ld_up, F, H, true, plan.wut),
-                  oxt = pass.operand(x, ldx, T_, H, true, plan.xt), odyt = pass.operand(dy, ldy, T_, H, true, plan.dyt);
-    if (int rc = pass.pk.template flush<T, P>(1)) return rc;
+    const Operand ody = pass.operand(dy, ldy, tokens, H, true, true, plan.dy), ox = pass.operand(x, ldx, tokens, H, false, true, plan.x),
+                  od = pass.operand(w.w_down, w.ld_down, H, F, false, true, plan.wd), oh = pass.own(plan.h, tokens, F),
+                  odg = pass.own(plan.dg, tokens, F), odu = pass.own(plan.du, tokens, F);
+    const auto [og, ou] = pass.projections(w, false, plan);
+    if (int rc = pass.pk.template flush<T>()) return rc;
     {
         FfArgs a{};
         a.count = 1;
         FfProblem& p = a.p[0];
-        add_segments(p, ody, owd, nullptr, P);
-        p.M = static_cast<uint32_t>(T_); p.N = w.ff; p.ktiles = static_cast<uint32_t>(plan.Hp / kFfBk);
+        add_segments(p, ody, od, nullptr, P);
+        p.M = static_cast<uint32_t>(tokens); p.N = w.ff; p.ktiles = static_cast<uint32_t>(plan.H / kFfBk);
         p.out = pass.ws + plan.h; p.o1 = pass.ws + plan.dg; p.o2 = pass.ws + plan.du;
-        p.ldo = plan.Fp; p.plane = T_ * plan.Fp; p.n_pad = static_cast<uint32_t>(plan.Fp);
+        p.ldo = oh.ld; p.plane = oh.plane; p.n_pad = static_cast<uint32_t>(plan.F); p.m_pad = static_cast<uint32_t>(plan.T);
         p.e0 = const_cast<void*>(gate); p.e1 = const_cast<void*>(up); p.lde = ldg; p.act = w.act;
-        if (int rc = launch_product<T, kFfDgate>(ctx, a, KID_FF_DGATE, st)) return rc;
+        if (int rc = launch_product<false, true, T, kFfDgate>(ctx, a, KID_FF_DGATE, st)) return rc;
     }
-    const Operand oht = pass.transposed(plan.h, T_, F, plan.ht), odgt = pass.transposed(plan.dg, T_, F, plan.dgt),
-                  odut = pass.transposed(plan.du, T_, F, plan.dut);
-    if (int rc = pass.pk.template flush<__bf16, 1>(P)) return rc;
     {
         FfArgs a{};
         a.count = 1;
         FfProblem& p = a.p[0];
-        add_segments(p, {pass.ws + plan.dg, plan.Fp, T_ * plan.Fp}, owg, nullptr, P);
-        add_segments(p, {pass.ws + plan.du, plan.Fp, T_ * plan.Fp}, owu, nullptr, P);
-        p.M = static_cast<uint32_t>(T_); p.N = w.hidden; p.ktiles = static_cast<uint32_t>(plan.Fp / kFfBk);
+        add_segments(p, odg, og, nullptr, P);
+        add_segments(p, odu, ou, nullptr, P);
+        p.M = static_cast<uint32_t>(tokens); p.N = w.hidden; p.ktiles = static_cast<uint32_t>(plan.F / kFfBk);
         p.out = dx; p.ldo = lddx;
-        if (int rc = launch_product<T, kFfStore>(ctx, a, KID_FF_DX, st)) return rc;
+        if (int rc = launch_product<false, true, T, kFfStore>(ctx, a, KID_FF_DX, st)) return rc;
     }
     FfArgs a{};
     a.count = 3;
-    const Operand left[3] = {odgt, odut, odyt}, right[3] = {oxt, oxt, oht};
+    const Operand left[3] = {odg, odu, ody}, right[3] = {ox, ox, oh};
     void* const out[3] = {dwg, dwu, dwd};
     const uint64_t ldo[3] = {lddg, lddu, lddd};
     for (int i = 0; i < 3; ++i) {
         FfProblem& p = a.p[i];
         add_segments(p, left[i], right[i], nullptr, P);
         p.M = i < 2 ? w.ff : w.hidden; p.N = i < 2 ? w.hidden : w.ff;
-        p.ktiles = static_cast<uint32_t>(plan.Tp / kFfBk);
+        p.ktiles = static_cast<uint32_t>(plan.T / kFfBk);
         p.out = out[i]; p.ldo = ldo[i]; p.accumulate = accumulate ? 1 : 0;
     }
-    return launch_product<T, kFfStore>(ctx, a, KID_FF_DW, st);
+    return launch_product<true, true, T, kFfStore>(ctx, a, KID_FF_DW, st);
 }
 
 // zeros in a matrix (the weight gradients of no tokens)

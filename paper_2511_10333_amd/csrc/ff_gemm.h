@@ -1,5 +1,6 @@
 // The matrix products of the gated feed-forward block: C[m][n] = sum over segments and k of A[m][k] B[n][k], both operands bf16 with
-// k contiguous, 16-byte aligned rows and k padded with zeros to whole tiles of 64.
+// 16-byte aligned rows and k a multiple of 64.  Either lies in memory with k along its rows, or (TA, TB) as its transpose, m or n
+// along the rows.
 //
 // fp32 operands come as three bf16 planes that add up to them exactly (24 significant bits = 3 x 8: a plane is the value's leading
 // bits, cut off, not rounded); six products of planes, 2^-24 of the operands left out, are six segments of one sum.  Six bf16 MFMAs
@@ -8,7 +9,10 @@
 // A block of 2 x 2 waves makes a BM x BN tile; tiles of 64 k of the operands come straight to LDS while earlier ones are multiplied.  A
 // row of 128 bytes lies there as eight 16-byte units, unit c at c ^ (row / 2 & 7): a read of 16 bytes per lane takes lanes 0-3, 12-15
 // and 20-27 of either half at once, then the other sixteen, and their rows then lie in different banks.  (At c ^ (row & 7) half of
-// LDS's cycles were conflicts.)  The MFMA's first operand is B: a lane then holds four
+// LDS's cycles were conflicts.)  A transposed operand lies there as it does in memory, 64 rows of k, and is read by the instruction
+// that transposes: of 16 lanes, lane s brings four neighbours of row s / 4, and lane d gets element d of the four rows' 16.  Its 32-byte
+// pieces c of row k lie at c ^ (2 (k & 3) + (k / 8 & 1)), so that the rows that lanes 0-31, and lanes 0-15 and 32-47, take are in
+// different banks.  The MFMA's first operand is B: a lane then holds four
 // neighbouring n of one m, which is what the epilogues load and store.
 #pragma once
 
@@ -37,7 +41,7 @@ struct FfProblem {
     void *e0, *e1, *o1, *o2;
     uint64_t lde;
     uint64_t plane;                     // elements between planes of out, o1, o2
-    uint32_t n_pad;                     // columns of out, o1, o2: those from N on are zeros
+    uint32_t n_pad, m_pad;              // columns and rows of out, o1, o2: those from N and M on are zeros
     int32_t act;
 };
 constexpr int kFfProblems = 3;
@@ -182,10 +186,10 @@ __device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t m, uint
         for (uint32_t i = 0; i < 4; ++i) {
             float a, da;
             ff_act(p.act, v[i], a, da);
-            h[i] = FULL || n0 + i < p.N ? a * v2[i] : 0.f;
+            h[i] = FULL || (n0 + i < p.N && m < p.M) ? a * v2[i] : 0.f;
         }
         FfType<T>::put4(static_cast<uint16_t*>(p.out) + m * p.ldo + n0, p.plane, h);
-        if (p.e0) {
+        if (p.e0 && (FULL || m < p.M)) {
             ff_store4<T, FULL>(static_cast<T*>(p.e0) + m * p.lde, n0, p.N, v);
             ff_store4<T, FULL>(static_cast<T*>(p.e1) + m * p.lde, n0, p.N, v2);
         }
@@ -195,7 +199,7 @@ __device__ __forceinline__ void ff_epilogue(const FfProblem& p, uint32_t m, uint
         for (uint32_t i = 0; i < 4; ++i) {
             float a, da;
             ff_act(p.act, x.a[i], a, da);
-            const bool in = FULL || n0 + i < p.N;
+            const bool in = FULL || (n0 + i < p.N && m < p.M);
             h[i] = in ? a * x.b[i] : 0.f;
             dg[i] = in ? v[i] * x.b[i] * da : 0.f;
             du[i] = in ? v[i] * a : 0.f;
@@ -305,13 +309,13 @@ __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left
 #pragma unroll
         for (int k = 0; k < kFfPasses<EPI>; ++k) row(k, x[k]);
     } else {
-        const uint32_t n_end = (EPI == kFfGate || EPI == kFfDgate) ? p.n_pad : p.N;
+        const uint32_t n_end = EPI == kFfStore ? p.N : p.n_pad, m_end = EPI == kFfStore ? p.M : p.m_pad;
 #pragma unroll 1
         for (int k = 0; k < kFfPasses<EPI>; ++k) {
             const uint32_t m = m0 + k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>;
-            if (m >= p.M || n >= n_end) continue;
-            FfLoaded loaded;
-            ff_load<T, EPI, false>(p, m, n, loaded);
+            if (m >= m_end || n >= n_end) continue;
+            FfLoaded loaded = {};
+            if (m < p.M) ff_load<T, EPI, false>(p, m, n, loaded);
             row(k, loaded);
         }
     }
@@ -328,14 +332,57 @@ __device__ __forceinline__ float4* ff_slot(float* part, uint32_t slot, uint32_t 
     return reinterpret_cast<float4*>(part + static_cast<uint64_t>(slot) * (BM * BN)) + ((i * NI + j) * 4 + q) * threads + tid;
 }
 
+// Bytes from the tile's first element to the unit of 16 bytes that a lane brings in load i of its wave.  `last`: the last row of the
+// operand that there is, from the tile's first; transposed: its last column.
+template <bool TRANS, int WIDTH, typename F>
+__device__ __forceinline__ uint32_t ff_place(uint32_t wave, uint32_t lane, int i, F&& row_of, uint32_t last, uint32_t ld)
+{
+    if constexpr (!TRANS) {
+        const uint32_t row = (i * 4 + wave) * 8 + lane / 8, unit = lane % 8 ^ row / 2 % 8;
+        return min(row_of(row), last) * ld * 2 + unit * 16;
+    } else {
+        constexpr uint32_t UNITS = WIDTH / 8;       // of a row of k
+        const uint32_t k = (i * 4 + wave) * (64 / UNITS) + lane / UNITS, unit = lane % UNITS ^ (k % 4 * 2 + k / 8 % 2) * 2;
+        return k * ld * 2 + min(unit, last / 8) * 16;
+    }
+}
+// A wave's fragments, of 32 rows (columns, transposed) and 16 k each, from column `first` of the tile on
+template <bool TRANS, int WIDTH>
+struct FfFragments {
+    uint32_t at;
+    __device__ __forceinline__ FfFragments(uint32_t lane, uint32_t first)
+    {
+        if constexpr (!TRANS) {
+            const uint32_t row = lane % 32;
+            at = (first + row) * 128 + (lane / 32 ^ row / 2 % 8) * 16;              // to be xored with 16 k's 32 bytes
+        } else {
+            const uint32_t k = lane / 32 * 8 + lane % 16 / 4;
+            at = k * (WIDTH * 2) + ((first + lane / 16 % 2 * 16 + lane % 4 * 4) * 2 ^ (k % 4 * 2 + k / 8 % 2) * 32);    // with f's 64 bytes
+        }
+    }
+    __device__ __forceinline__ bf16x8 read(const unsigned char* tile, int kk, int f) const
+    {
+        if constexpr (!TRANS) {
+            return *reinterpret_cast<const bf16x8*>(tile + (at ^ (kk * 32)) + f * 4096);
+        } else {
+            typedef __attribute__((address_space(3))) bf16x4 lds_x4;
+            const unsigned char* const q = tile + (at ^ (f * 64)) + kk * (WIDTH * 32);
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_x4*)q);
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_x4*)(q + WIDTH * 8));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+};
+
 // Rows of B that a wave has of its NI * 32: gated, the first half are the first projection's and the others the second's
 template <bool GATED, int NI>
 __device__ __forceinline__ uint32_t ff_column(uint32_t row) { return GATED ? row / (NI * 32) * (NI * 16) + row % (NI * 16) : row; }
 
-template <int BM, int BN, typename T, int EPI>
+template <int BM, int BN, bool TA, bool TB, typename T, int EPI>
 __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
 {
     constexpr bool GATED = EPI == kFfGate, LARGE = BM == 256;
+    static_assert(!GATED || !TB, "the projections' weights have k along their rows");
     constexpr int MI = BM / 64, NI = BN / 64, LA = BM / 32, LB = BN / 32;       // squares of a wave; its loads per tile of 64 k
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
     constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = BN * 128, kAtB = kBufsA * kBytesA;
@@ -359,41 +406,43 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
         ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
         const uint32_t m0 = tm * BM, n0 = tn * COLS;
 
-        // Bytes from the tile's first row to the units that this thread brings (rows beyond the matrix: its last).  Load i of a wave
-        // fills the eight rows of LDS from 8 (4 i + wave) on, whose bits choose which unit of the operand's row goes where.
+        // Bytes from the tile's first element to the units that this thread brings.  Load i of a wave fills 1 KB of LDS, from
+        // 1024 (4 i + wave) on: eight rows of an operand, or two or four rows of k of a transposed one.  What lies beyond the matrix
+        // is its last row or unit again.
         uint32_t oa[LA], ob[LB];
-        const uint32_t row = wave * 8 + lane / 8, unit = (lane % 8 ^ row / 2 % 8) * 16;     // (32 rows on: the same unit)
 #pragma unroll
-        for (int i = 0; i < LA; ++i) oa[i] = min(row + i * 32, p.M - 1 - m0) * static_cast<uint32_t>(p.lda) * 2 + unit;
+        for (int i = 0; i < LA; ++i) oa[i] = ff_place<TA, BM>(wave, lane, i, [&](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
 #pragma unroll
         for (int i = 0; i < LB; ++i)
-            ob[i] = min(ff_column<GATED, NI>(row + i * 32), p.N - 1 - n0) * static_cast<uint32_t>(p.ldb) * 2 + unit;
+            ob[i] = ff_place<TB, BN>(wave, lane, i, [&](uint32_t r) { return ff_column<GATED, NI>(r); }, p.N - 1 - n0, static_cast<uint32_t>(p.ldb));
 
         const uint32_t per_seg = p.ktiles;
-        const uint64_t a_row0 = m0 * p.lda, b_row0 = n0 * p.ldb;
-        // where the next tile of either operand is; B comes later than A, so each has a place of its own
+        // elements from an operand's first to the tile's, and from a tile of k to the next
+        const uint64_t a_first = TA ? m0 : m0 * p.lda, b_first = TB ? n0 : n0 * p.ldb;
+        const uint64_t a_step = TA ? kFfBk * p.lda : kFfBk, b_step = TB ? kFfBk * p.ldb : kFfBk;
+        // where the next tile of either operand is; B is asked for later than A, so each has a place of its own
         struct Place {
             uint32_t seg, left;
         };
         Place na{kt0 / per_seg, 0}, nb;
-        na.left = per_seg - (kt0 - na.seg * per_seg);
+        const uint32_t in_seg = kt0 - na.seg * per_seg;
+        na.left = per_seg - in_seg;
         nb = na;
-        const uint32_t k0 = (kt0 - na.seg * per_seg) * kFfBk;
-        const uint16_t *pa = p.a[na.seg] + a_row0 + k0, *pb = p.b[nb.seg] + b_row0 + k0;
-        const uint16_t* pb2 = GATED ? p.b2[nb.seg] + b_row0 + k0 : pb;
+        const uint16_t *pa = p.a[na.seg] + a_first + in_seg * a_step, *pb = p.b[nb.seg] + b_first + in_seg * b_step;
+        const uint16_t* pb2 = GATED ? p.b2[nb.seg] + b_first + in_seg * b_step : pb;
         auto next_a = [&]() {
-            pa += kFfBk;
+            pa += a_step;
             if (--na.left == 0 && na.seg + 1 < p.nseg) {
-                pa = p.a[++na.seg] + a_row0;
+                pa = p.a[++na.seg] + a_first;
                 na.left = per_seg;
             }
         };
         auto next_b = [&]() {
-            pb += kFfBk;
-            pb2 += kFfBk;
+            pb += b_step;
+            pb2 += b_step;
             if (--nb.left == 0 && nb.seg + 1 < p.nseg) {
-                pb = p.b[++nb.seg] + b_row0;
-                pb2 = GATED ? p.b2[nb.seg] + b_row0 : pb;
+                pb = p.b[++nb.seg] + b_first;
+                pb2 = GATED ? p.b2[nb.seg] + b_first : pb;
                 nb.left = per_seg;
             }
         };
@@ -418,14 +467,14 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
         // the place of tile t's.  A has three buffers where they fit (LARGE), and A of tile t + 2 is asked for in the first two
         // steps of tile t.  Either has four steps at least to come: the barrier of tile t has to find tile t + 1 there, and after that
         // tile was asked for came A of tile t + 2 only.
-        const uint32_t fr = lane & 31, fu = ((lane >> 5) ^ (fr / 2 & 7)) * 16;  // row of a fragment; its unit, to be xored with 2 k / 16
-        const uint32_t ra0 = (wm * MI * 32 + fr) * 128 + fu, rb0 = kAtB + (wn * NI * 32 + fr) * 128 + fu;
+        const FfFragments<TA, BM> frag_a(lane, wm * MI * 32);
+        const FfFragments<TB, BN> frag_b(lane, wn * NI * 32);
         const uint32_t n = kt1 - kt0;
         bf16x8 fa[2][MI], fb[2][NI];
         auto read = [&](uint32_t buf_a, uint32_t buf_b, int kk, int f) {        // fragment f of the step: NI of B, MI of A, as they are used
             const int to = kk & 1;
-            if (f < NI) fb[to][f] = *reinterpret_cast<const bf16x8*>(lds + ((rb0 + buf_b * kBytesB) ^ (kk * 32)) + f * 4096);
-            else fa[to][f - NI] = *reinterpret_cast<const bf16x8*>(lds + ((ra0 + buf_a * kBytesA) ^ (kk * 32)) + (f - NI) * 4096);
+            if (f < NI) fb[to][f] = frag_b.read(lds + kAtB + buf_b * kBytesB, kk, f);
+            else fa[to][f - NI] = frag_a.read(lds + buf_a * kBytesA, kk, f - NI);
         };
         for (uint32_t t = 0; t < 2 && t < n; ++t) {
 #pragma unroll
