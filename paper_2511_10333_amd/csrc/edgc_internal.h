@@ -131,6 +131,7 @@ struct NormScratch {
 struct FfScratch {
     void*    ws = nullptr;          // operands, 16 bits each
     float*   part = nullptr;        // partial sums of products that are split along k
+    unsigned int* tickets = nullptr;    // of blocks that share k, zero between calls
     uint64_t elems = 0;
 };
 

@@ -7,7 +7,7 @@
 // Backward: dA, whose epilogue makes dG, dU and A from the kept projections (dA itself is never stored), dx over both halves in one
 // sum, and the three weight gradients in one launch.  Products: ff_gemm.h.  Operands that are not laid out for them (k contiguous
 // and a multiple of 64, 16-byte aligned, bf16) are first copied into the reserved scratch, transposed or split where needed.
-#include "ff_gemm.h"
+#include "ff_few.h"
 
 #include <algorithm>
 #include <cmath>
@@ -261,10 +261,62 @@ struct FfPass {
     }
 };
 
+// Few tokens.  About 16 waves on a compute unit, each with eight steps of k at least: 4 to 16 waves of a block share k, and where there
+// are fewer blocks than compute units eight waves and up to four blocks.  (24 tokens, fp32, 2048 rows of 8192: 128 blocks of 16 waves
+// 38.5 us, 512 of 8 22.6; one token, bf16, 4096 rows of 16384: 256 of 16 27.6 us, 512 of 8 31.3.)
+template <typename T, bool GATED>
+int launch_few(edgc_ctx* ctx, FfFewArgs& a, int kid, hipStream_t st)
+{
+    const uint32_t blocks = (a.N + 15) / 16, steps = (a.K + FfFew<T>::kStep - 1) / FfFew<T>::kStep, cu = static_cast<uint32_t>(ctx->num_cu);
+    uint32_t waves = 4, splits = 1;
+    while (waves < (blocks < cu ? 8u : 16u) && blocks * waves < cu * 16 && steps >= waves * 16) waves *= 2;
+    while (splits < kFfFewSplits && blocks < cu && blocks * splits < cu * 2 && steps >= waves * splits * 16) splits *= 2;
+    a.part = ctx->ff.part;
+    a.tickets = ctx->ff.tickets;
+    const double mats = GATED ? 2.0 : 1.0;
+    auto go = [&](auto groups) {
+        constexpr int G = decltype(groups)::value;
+        const uint32_t lds = waves * (GATED ? 2 : 1) * G * 64 * 16;
+        EDGC_LAUNCH(ctx, st, kid, sizeof(T) * mats * a.N * a.K, 2.0 * mats * a.tokens * a.N * a.K,
+                    k_ff_few<T, G, GATED><<<dim3(blocks, splits), waves * 64, lds, st>>>(a));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        return static_cast<int>(EDGC_OK);
+    };
+    if (a.tokens <= 16) return go(std::integral_constant<int, 1>{});
+    if (a.tokens <= 32) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 4>{});
+}
+
+template <typename T>
+hipError_t prepare_few()
+{
+    for (const void* f : {reinterpret_cast<const void*>(&k_ff_few<T, 1, false>), reinterpret_cast<const void*>(&k_ff_few<T, 2, false>),
+                          reinterpret_cast<const void*>(&k_ff_few<T, 4, false>), reinterpret_cast<const void*>(&k_ff_few<T, 1, true>),
+                          reinterpret_cast<const void*>(&k_ff_few<T, 2, true>), reinterpret_cast<const void*>(&k_ff_few<T, 4, true>)})
+        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * 2 * 4 * 64 * 16)) return e;
+    return hipSuccess;
+}
+
+template <typename T>
+int ff_forward_few(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint32_t tokens, void* y, uint64_t ldy, void* gate, void* up,
+                   uint64_t ldg, hipStream_t st)
+{
+    FfFewArgs a{};
+    a.x = x; a.ldx = ldx; a.w = w.w_gate; a.w2 = w.w_up; a.ldw = w.ld_gate; a.ldw2 = w.ld_up;
+    a.tokens = tokens; a.N = w.ff; a.K = w.hidden; a.act = w.act;
+    a.out = ctx->ff.ws; a.ldo = w.ff; a.keep = gate; a.keep2 = up; a.ldk = ldg;
+    if (int rc = launch_few<T, true>(ctx, a, KID_FF_GATE, st)) return rc;
+    FfFewArgs b{};
+    b.x = ctx->ff.ws; b.ldx = w.ff; b.w = w.w_down; b.ldw = w.ld_down;
+    b.tokens = tokens; b.N = w.hidden; b.K = w.ff; b.out = y; b.ldo = ldy;
+    return launch_few<T, false>(ctx, b, KID_FF_DOWN, st);
+}
+
 template <typename T>
 int ff_forward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t tokens, void* y, uint64_t ldy, void* gate, void* up,
                uint64_t ldg, hipStream_t st)
 {
+    if (tokens <= kFfFewTokens) return ff_forward_few<T>(ctx, w, x, ldx, static_cast<uint32_t>(tokens), y, ldy, gate, up, ldg, st);
     constexpr int P = FfType<T>::kPlanes;
     const uint64_t H = w.hidden, F = w.ff;
     FfPlan plan(tokens, H, F, w.dtype);
@@ -381,6 +433,8 @@ int prepare_ff_kernels(edgc_ctx* ctx)
 {
     hipError_t e = prepare_tiles<256, 256, __bf16>();
     if (e == hipSuccess) e = prepare_tiles<256, 256, float>();
+    if (e == hipSuccess) e = prepare_few<__bf16>();
+    if (e == hipSuccess) e = prepare_few<float>();
     EDGC_HIP_TRY(ctx, e);
     return EDGC_OK;
 }
@@ -404,9 +458,16 @@ extern "C" int edgc_reserve_ff(edgc_ctx* ctx, edgc_dtype dtype, uint32_t tokens,
     FfPlan plan(tokens, hidden, ff, dtype);
     uint64_t elems = plan.forward();
     if (backward) elems = std::max(elems, plan.backward());
-    if (hipMalloc(&ctx->ff.ws, elems * 2) != hipSuccess || hipMalloc(reinterpret_cast<void**>(&ctx->ff.part), part_elems(ctx) * sizeof(float)) != hipSuccess) {
+    const uint64_t part_bytes = part_elems(ctx) * sizeof(float);
+    bool ok = hipMalloc(&ctx->ff.ws, elems * 2) == hipSuccess;
+    // the tickets lie behind the sums
+    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ff.part), part_bytes + kFfFewBlocks * sizeof(unsigned int)) == hipSuccess;
+    ctx->ff.tickets = reinterpret_cast<unsigned int*>(ctx->ff.part + part_elems(ctx));
+    ok = ok && hipMemset(ctx->ff.tickets, 0, kFfFewBlocks * sizeof(unsigned int)) == hipSuccess && hipDeviceSynchronize() == hipSuccess;
+    if (!ok) {
         (void)hipGetLastError();
         if (ctx->ff.ws) (void)hipFree(ctx->ff.ws);
+        if (ctx->ff.part) (void)hipFree(ctx->ff.part);
         ctx->ff = FfScratch{};
         return fail(ctx, EDGC_ENOMEM, "feed-forward scratch allocation failed");
     }
