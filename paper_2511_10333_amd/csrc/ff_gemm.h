@@ -571,12 +571,15 @@ __global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
     const uint32_t per = MI * NI / 2, at = blockIdx.x / per, i = blockIdx.x % per / (NI / 2), j = blockIdx.x % (NI / 2);
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     const uint64_t s0 = static_cast<uint64_t>(at) * args.ksteps, s1 = s0 + args.ksteps, all = static_cast<uint64_t>(args.rest) * args.ksteps;
-    uint32_t w = static_cast<uint32_t>(s0 * args.workers / all);
-    while (ff_share(args, w + 1) <= s0) ++w;        // the first worker with a step of this tile
-    if (ff_share(args, w) <= s0 && ff_share(args, w + 1) >= s1) return;     // which had them all
+    // the workers that have a step of this tile
+    uint32_t first = static_cast<uint32_t>(s0 * args.workers / all), last = static_cast<uint32_t>((s1 - 1) * args.workers / all);
+    while (ff_share(args, first + 1) <= s0) ++first;
+    while (last + 1 < args.workers && ff_share(args, last + 1) < s1) ++last;
+    if (first == last) return;                      // one, which has finished it
     const uint32_t js[2] = {GATED ? j : 2 * j, GATED ? j + NI / 2 : 2 * j + 1};
     f32x16 acc[2] = {};
-    for (; w < args.workers && ff_share(args, w) < s1; ++w) {
+#pragma unroll 2
+    for (uint32_t w = first; w <= last; ++w) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
