@@ -171,7 +171,7 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     EDGC_HIP_TRY(ctx, hipGetLastError());
     if (a.rest) {
         EDGC_LAUNCH(ctx, st, KID_FF_JOIN, 4.0 * BM * BN * (a.workers + a.rest), 0.0,
-                    k_ff_join<BM, BN, T, EPI><<<a.rest * (BM / 64) * (BN / 128), 256, 0, st>>>(a));
+                    k_ff_join<BM, BN, T, EPI><<<a.rest * (BM / 64) * (BN / (EPI == kFfGate ? 128 : 64)), 256, 0, st>>>(a));
         EDGC_HIP_TRY(ctx, hipGetLastError());
     }
     return EDGC_OK;

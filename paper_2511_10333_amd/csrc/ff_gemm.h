@@ -269,26 +269,30 @@ __device__ __forceinline__ void ff_each(F&& f)
 // The sums of 32 rows and 2 x 32 columns (gated: of either projection), of which a lane holds row lane % 32 and of either half the
 // columns 8 (v / 4) + 4 (lane / 32) + v % 4: through LDS (the wave's own part of it), so that a row's columns are loaded and stored together.
 constexpr uint32_t kFfRow = 68;         // floats: 64 and a pad that spreads the rows over the banks
-template <int EPI> constexpr uint32_t kFfLanes = EPI == kFfGate ? 8 : 16;       // per row, four columns each
-template <int EPI> constexpr int kFfPasses = 32 * kFfLanes<EPI> / 64;           // over the rows
+// SINGLE: of one square of 32 columns alone
+template <int EPI, bool SINGLE> constexpr uint32_t kFfLanes = EPI == kFfGate || SINGLE ? 8 : 16;   // per row, four columns each
+template <int EPI, bool SINGLE> constexpr int kFfPasses = 32 * kFfLanes<EPI, SINGLE> / 64;         // over the rows
 
+// whether all of it lies inside the output
+template <int EPI, bool SINGLE>
+__device__ __forceinline__ bool ff_inside(const FfProblem& p, uint32_t m0, uint32_t n0) { return m0 + 32 <= p.M && n0 + kFfLanes<EPI, SINGLE> * 4 <= p.N; }
 // what the epilogue of such a square loads, asked for ahead of it
-template <typename T, int EPI>
-__device__ __forceinline__ void ff_ask(const FfProblem& p, FfLoaded (&x)[kFfPasses<EPI>], uint32_t lane, uint32_t m0, uint32_t n0)
+template <typename T, int EPI, bool SINGLE>
+__device__ __forceinline__ void ff_ask(const FfProblem& p, FfLoaded (&x)[kFfPasses<EPI, SINGLE>], uint32_t lane, uint32_t m0, uint32_t n0)
 {
 #pragma unroll
-    for (int k = 0; k < kFfPasses<EPI>; ++k)
-        ff_load<T, EPI, true>(p, m0 + k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>, n0 + lane % kFfLanes<EPI> * 4, x[k]);
+    for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k)
+        ff_load<T, EPI, true>(p, m0 + k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>, n0 + lane % kFfLanes<EPI, SINGLE> * 4, x[k]);
 }
 // FULL: the square lies inside the output, and `x` holds what its epilogue loads
-template <typename T, int EPI, bool FULL>
+template <typename T, int EPI, bool SINGLE, bool FULL>
 __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left, const f32x16& right, float* mine, uint32_t lane, uint32_t m0,
-                                          uint32_t n0, const FfLoaded (&x)[kFfPasses<EPI>])
+                                          uint32_t n0, const FfLoaded (&x)[kFfPasses<EPI, SINGLE>])
 {
     constexpr bool GATED = EPI == kFfGate;
-    const uint32_t c4 = lane % kFfLanes<EPI> * 4, n = n0 + c4;
+    const uint32_t c4 = lane % kFfLanes<EPI, SINGLE> * 4, n = n0 + c4;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < (EPI != kFfGate && SINGLE ? 1 : 2); ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const f32x16& a = j ? right : left;
@@ -299,7 +303,7 @@ __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     auto row = [&](int k, const FfLoaded& loaded) {
-        const uint32_t r = k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>;
+        const uint32_t r = k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>;
         const float4 s = *reinterpret_cast<const float4*>(mine + r * kFfRow + c4);
         const float4 s2 = GATED ? *reinterpret_cast<const float4*>(mine + r * kFfRow + 32 + c4) : s;
         float v[4] = {s.x, s.y, s.z, s.w}, v2[4] = {s2.x, s2.y, s2.z, s2.w};
@@ -307,12 +311,12 @@ __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left
     };
     if constexpr (FULL) {
 #pragma unroll
-        for (int k = 0; k < kFfPasses<EPI>; ++k) row(k, x[k]);
+        for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k) row(k, x[k]);
     } else {
         const uint32_t n_end = EPI == kFfStore ? p.N : p.n_pad, m_end = EPI == kFfStore ? p.M : p.m_pad;
 #pragma unroll 1
-        for (int k = 0; k < kFfPasses<EPI>; ++k) {
-            const uint32_t m = m0 + k * (64 / kFfLanes<EPI>) + lane / kFfLanes<EPI>;
+        for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k) {
+            const uint32_t m = m0 + k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>;
             if (m >= m_end || n >= n_end) continue;
             FfLoaded loaded = {};
             if (m < p.M) ff_load<T, EPI, false>(p, m, n, loaded);
@@ -532,20 +536,16 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
             auto left_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][(GATED ? 1 : 2) * (s % (NI / 2))]; };
             auto right_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][GATED ? s % (NI / 2) + NI / 2 : 2 * (s % (NI / 2)) + 1]; };
             constexpr int SQUARES = MI * NI / 2;
-            FfLoaded x[2][kFfPasses<EPI>];
-            if (m0 + BM <= p.M && n0 + COLS <= p.N) {
-                ff_ask<T, EPI>(p, x[0], lane, m_of(0), n_of(0));
-                ff_each<SQUARES>([&](auto sq) {
-                    constexpr int s = decltype(sq)::value;
-                    if constexpr (s + 1 < SQUARES) ff_ask<T, EPI>(p, x[(s + 1) & 1], lane, m_of(s + 1), n_of(s + 1));
-                    ff_finish<T, EPI, true>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[s & 1]);
-                });
-            } else {
-                ff_each<SQUARES>([&](auto sq) {
-                    constexpr int s = decltype(sq)::value;
-                    ff_finish<T, EPI, false>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[0]);
-                });
-            }
+            FfLoaded x[2][kFfPasses<EPI, false>];
+            auto inside = [&](int s) { return ff_inside<EPI, false>(p, m_of(s), n_of(s)); };
+            if (inside(0)) ff_ask<T, EPI, false>(p, x[0], lane, m_of(0), n_of(0));
+            ff_each<SQUARES>([&](auto sq) {
+                constexpr int s = decltype(sq)::value;
+                if constexpr (s + 1 < SQUARES)
+                    if (inside(s + 1)) ff_ask<T, EPI, false>(p, x[(s + 1) & 1], lane, m_of(s + 1), n_of(s + 1));
+                if (inside(s)) ff_finish<T, EPI, false, true>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[s & 1]);
+                else ff_finish<T, EPI, false, false>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[0]);
+            });
         } else {
 #pragma unroll
             for (int i = 0; i < MI; ++i)
@@ -560,15 +560,15 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
     }
 }
 
-// Adds up the sums that several workers have of a tile, in the order of the workers: 32 rows and a pair of squares of every wave's
-// part per block
+// Adds up the sums that several workers have of a tile, in the order of the workers: one square (gated: of both projections) of every
+// wave's part per block
 template <int BM, int BN, typename T, int EPI>
 __global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
 {
-    constexpr int MI = BM / 64, NI = BN / 64;
     constexpr bool GATED = EPI == kFfGate;
+    constexpr int MI = BM / 64, NI = BN / 64, BOTH = GATED ? 2 : 1, ACROSS = NI / BOTH;
     __shared__ float stage[4 * 32 * kFfRow];
-    const uint32_t per = MI * NI / 2, at = blockIdx.x / per, i = blockIdx.x % per / (NI / 2), j = blockIdx.x % (NI / 2);
+    const uint32_t per = MI * ACROSS, at = blockIdx.x / per, i = blockIdx.x % per / ACROSS, j = blockIdx.x % ACROSS;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     const uint64_t s0 = static_cast<uint64_t>(at) * args.ksteps, s1 = s0 + args.ksteps, all = static_cast<uint64_t>(args.rest) * args.ksteps;
     // the workers that have a step of this tile
@@ -576,15 +576,14 @@ __global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
     while (ff_share(args, first + 1) <= s0) ++first;
     while (last + 1 < args.workers && ff_share(args, last + 1) < s1) ++last;
     if (first == last) return;                      // one, which has finished it
-    const uint32_t js[2] = {GATED ? j : 2 * j, GATED ? j + NI / 2 : 2 * j + 1};
-    f32x16 acc[2] = {};
-#pragma unroll 2
+    f32x16 acc[BOTH] = {};
+#pragma unroll 4
     for (uint32_t w = first; w <= last; ++w) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < BOTH; ++h)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float4 v = *ff_slot<BM, BN, NI>(args.part, w + at, i, js[h], q, tid);
+                const float4 v = *ff_slot<BM, BN, NI>(args.part, w + at, i, j + h * (NI / 2), q, tid);
                 acc[h][4 * q] += v.x; acc[h][4 * q + 1] += v.y; acc[h][4 * q + 2] += v.z; acc[h][4 * q + 3] += v.w;
             }
     }
@@ -592,10 +591,15 @@ __global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
     const FfProblem& p = ff_problem_of(args, tile);
     uint32_t tm, tn;
     ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
-    const uint32_t wm = wave / 2, wn = wave % 2;
-    const FfLoaded none[kFfPasses<EPI>] = {};
-    ff_finish<T, EPI, false>(p, acc[0], acc[1], stage + wave * (32 * kFfRow), lane, tm * BM + (wm * MI + i) * 32,
-                             tn * (GATED ? BN / 2 : BN) + (GATED ? wn * NI * 16 + j * 32 : wn * NI * 32 + j * 64), none);
+    const uint32_t m0 = tm * BM + (wave / 2 * MI + i) * 32, n0 = tn * (BN / BOTH) + (wave % 2 * ACROSS + j) * 32;
+    float* const mine = stage + wave * (32 * kFfRow);
+    FfLoaded x[kFfPasses<EPI, true>];
+    if (ff_inside<EPI, true>(p, m0, n0)) {
+        ff_ask<T, EPI, true>(p, x, lane, m0, n0);
+        ff_finish<T, EPI, true, true>(p, acc[0], acc[BOTH - 1], mine, lane, m0, n0, x);
+    } else {
+        ff_finish<T, EPI, true, false>(p, acc[0], acc[BOTH - 1], mine, lane, m0, n0, x);
+    }
 }
 
 }  // namespace edgc
