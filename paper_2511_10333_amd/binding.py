@@ -380,11 +380,15 @@ ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 def _rows(name, t, dtype, shape) -> int:
     """Leading dimension of a matrix of that dtype and shape whose rows are contiguous."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
-        raise ValueError(f"{name} must be of shape {shape} with contiguous rows that do not overlap")
-    return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+    rows, cols = shape
+    if t.shape != shape:
+        raise ValueError(f"{name} must be of shape {tuple(shape)}")
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return ld if rows > 1 else max(ld, cols)
 
 
 class FeedForward:
@@ -406,15 +410,19 @@ class FeedForward:
         self.c = _FF(*[w.data_ptr() for w in self.weights], *lds, self.hidden, self.ff, _dtype_code(w_gate), ACTIVATIONS[act])
 
 
-def _check_dense(dtype, shape, **tensors) -> None:
-    """Every given tensor is contiguous, of that dtype and of that shape."""
-    for name, t in tensors.items():
-        if t is None:
+def _bad_dense(names, tensors, dtype, shape):
+    """What is wrong with the first of the given tensors that is not contiguous, of that dtype and of that shape."""
+    for name, t in zip(names, tensors):
+        if t is None or (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()):
             continue
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}")
-        if tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous of shape {shape}")
+        raise (TypeError(f"{name} must be {dtype}") if t.dtype != dtype else
+               ValueError(f"{name} must be contiguous of shape {tuple(shape)}"))
+
+
+def _check_dense(names, tensors, dtype, shape) -> None:
+    for t in tensors:
+        if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
+            _bad_dense(names, tensors, dtype, shape)
 
 
 class PreparedBatch:
@@ -671,12 +679,16 @@ class Context:
         self._check(rc, "edgc_residual_materialize_batch")
 
     # -- the block around the compressor --------------------------------------
+    def _gradients(self, tensors):
+        """Descriptors for the calls that read gradients alone: a prepared batch's as they are, without its per-call flags."""
+        return (tensors.arr, tensors.code) if isinstance(tensors, PreparedBatch) else self._marshal(tensors)
+
     def grad_sumsq_batch(self, tensors: Sequence[Tensor], sumsq=None, accumulate: bool = False, stream=None) -> None:
         """edgc_grad_sumsq_batch: the sum of squares of the tensors' ``grad``, into ``sumsq`` (a float64 CUDA tensor of one
         element; None: the context's own place); ``accumulate`` adds to what is there."""
         if sumsq is not None and (sumsq.dtype != (_torch or _load_torch()).float64 or sumsq.numel() != 1):
             raise TypeError("sumsq must be one float64")
-        arr, code = self._marshal(tensors)
+        arr, code = self._gradients(tensors)
         rc = self._L.edgc_grad_sumsq_batch(self._h, arr, len(tensors), code, 1 if accumulate else 0, _ptr(sumsq),
                                            _stream_handle(stream))
         self._check(rc, "edgc_grad_sumsq_batch")
@@ -690,7 +702,7 @@ class Context:
             raise TypeError("sumsq must be one float64")
         if norm_coef is not None and (norm_coef.dtype != torch.float32 or norm_coef.numel() != 2 or not norm_coef.is_contiguous()):
             raise TypeError("norm_coef must be two float32")
-        arr, code = self._marshal(tensors)
+        arr, code = self._gradients(tensors)
         rc = self._L.edgc_clip_batch(self._h, arr, len(tensors), code, float(max_norm), _ptr(sumsq), _ptr(norm_coef),
                                      _stream_handle(stream))
         self._check(rc, "edgc_clip_batch")
@@ -700,42 +712,48 @@ class Context:
         self._check(self._L.edgc_reserve_block_norm(self._h, tokens, hidden), "edgc_reserve_block_norm")
 
     @staticmethod
-    def _norm_shapes(x, gate, rows_per_gate, dense, vectors):
-        if x.dim() != 2:
+    def _norm_shapes(of, gate, rows_per_gate, names, dense, vectors, stats):
+        """Tokens and hidden size of a pass whose tokens x hidden tensors are ``dense`` (and ``of``), whose vectors of hidden
+        elements and of tokens statistics are the others; all as they have to be."""
+        shape, dtype = of.shape, of.dtype
+        if len(shape) != 2:
             raise ValueError("activations must be tokens x hidden")
-        t, h = x.shape
-        _check_dense(x.dtype, (t, h), **dense)
-        _check_dense(x.dtype, (h,), **vectors)
+        t, h = shape
+        _check_dense(names[0], dense, dtype, shape)
+        _check_dense(names[1], vectors, dtype, (h,))
+        _check_dense(("rstd_post", "rstd_pre"), stats, _torch.float32, (t,))
         if gate is not None:
             if rows_per_gate < 1:
                 raise ValueError("rows_per_gate must be >= 1 with a gate")
-            _check_dense(x.dtype, (-(-t // rows_per_gate), h), gate=gate)
+            _check_dense(("gate",), (gate,), dtype, (-(-t // rows_per_gate), h))
         return t, h
 
     def block_norm_forward(self, x, y, w_post, gate, w_pre, x_out, n_out, rstd_post=None, rstd_pre=None, scale: float = 1.0,
                            eps: float = 1e-6, rows_per_gate: int = 0, stream=None) -> None:
         """edgc_block_norm_forward: x_out = x + scale * gate * (norm(y) * w_post), n_out = norm(x_out) * w_pre; tokens x hidden.
         ``y`` None: the norm before a block alone; ``w_pre`` None: the norm after it alone."""
-        t, h = self._norm_shapes(x, gate, rows_per_gate, dict(x=x, y=y, x_out=x_out, n_out=n_out), dict(w_post=w_post, w_pre=w_pre))
-        _check_dense((_torch or _load_torch()).float32, (t,), rstd_post=rstd_post, rstd_pre=rstd_pre)
-        rc = self._L.edgc_block_norm_forward(self._h, _dtype_code(x), t, h, x.data_ptr(), _ptr(y), _ptr(w_post), _ptr(gate),
-                                             rows_per_gate, _ptr(w_pre), scale, eps, _ptr(x_out), _ptr(n_out), _ptr(rstd_post),
-                                             _ptr(rstd_pre), _stream_handle(stream))
-        self._check(rc, "edgc_block_norm_forward")
+        code = _dtype_code(x)
+        t, h = self._norm_shapes(x, gate, rows_per_gate, (("x", "y", "x_out", "n_out"), ("w_post", "w_pre")), (x, y, x_out, n_out),
+                                 (w_post, w_pre), (rstd_post, rstd_pre))
+        rc = self._L.edgc_block_norm_forward(self._h, code, t, h, x.data_ptr(), _ptr(y), _ptr(w_post), _ptr(gate), rows_per_gate,
+                                             _ptr(w_pre), scale, eps, _ptr(x_out), _ptr(n_out), _ptr(rstd_post), _ptr(rstd_pre),
+                                             _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_block_norm_forward")
 
     def block_norm_backward(self, dx_out, dn, x_out, y, w_post, gate, w_pre, rstd_post, rstd_pre, dx, dy, dw_post, dgate, dw_pre,
                             scale: float = 1.0, rows_per_gate: int = 0, stream=None) -> None:
         """edgc_block_norm_backward: the gradients of what :meth:`block_norm_forward` computed, from those of x_out and n_out."""
-        t, h = self._norm_shapes(dx, gate, rows_per_gate, dict(dx_out=dx_out, dn=dn, x_out=x_out, y=y, dx=dx, dy=dy),
-                                 dict(w_post=w_post, w_pre=w_pre, dw_post=dw_post, dw_pre=dw_pre))
-        _check_dense((_torch or _load_torch()).float32, (t,), rstd_post=rstd_post, rstd_pre=rstd_pre)
+        code = _dtype_code(dx)
+        t, h = self._norm_shapes(dx, gate, rows_per_gate, (("dx_out", "dn", "x_out", "y", "dx", "dy"), ("w_post", "w_pre", "dw_post", "dw_pre")),
+                                 (dx_out, dn, x_out, y, dx, dy), (w_post, w_pre, dw_post, dw_pre), (rstd_post, rstd_pre))
         if gate is not None:
-            _check_dense(dx.dtype, tuple(gate.shape), dgate=dgate)
-        rc = self._L.edgc_block_norm_backward(self._h, _dtype_code(dx), t, h, _ptr(dx_out), _ptr(dn), _ptr(x_out), _ptr(y),
-                                              _ptr(w_post), _ptr(gate), rows_per_gate, _ptr(w_pre), _ptr(rstd_post),
-                                              _ptr(rstd_pre), scale, dx.data_ptr(), _ptr(dy), _ptr(dw_post), _ptr(dgate),
-                                              _ptr(dw_pre), _stream_handle(stream))
-        self._check(rc, "edgc_block_norm_backward")
+            _check_dense(("dgate",), (dgate,), dx.dtype, gate.shape)
+        rc = self._L.edgc_block_norm_backward(self._h, code, t, h, _ptr(dx_out), _ptr(dn), _ptr(x_out), _ptr(y), _ptr(w_post),
+                                              _ptr(gate), rows_per_gate, _ptr(w_pre), _ptr(rstd_post), _ptr(rstd_pre), scale,
+                                              dx.data_ptr(), _ptr(dy), _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_block_norm_backward")
 
     def reserve_ff(self, dtype, tokens: int, hidden: int, ff: int, backward: bool = False) -> None:
         """edgc_reserve_ff: scratch of :meth:`ff_forward` (and :meth:`ff_backward`) for up to that many tokens of that
