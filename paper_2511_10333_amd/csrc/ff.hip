@@ -269,7 +269,7 @@ int launch_few(edgc_ctx* ctx, FfFewArgs& a, int kid, hipStream_t st)
 {
     const uint32_t blocks = (a.N + 15) / 16, steps = (a.K + FfFew<T>::kStep - 1) / FfFew<T>::kStep, cu = static_cast<uint32_t>(ctx->num_cu);
     uint32_t waves = 4, splits = 1;
-    while (waves < (blocks < cu ? 8u : 16u) && blocks * waves < cu * 16 && steps >= waves * 16) waves *= 2;
+    while (waves < (blocks < cu || a.tokens > 32 ? 8u : 16u) && blocks * waves < cu * 16 && steps >= waves * 16) waves *= 2;
     while (splits < kFfFewSplits && blocks < cu && blocks * splits < cu * 2 && steps >= waves * splits * 16) splits *= 2;
     a.part = ctx->ff.part;
     a.tickets = ctx->ff.tickets;
@@ -284,16 +284,15 @@ int launch_few(edgc_ctx* ctx, FfFewArgs& a, int kid, hipStream_t st)
     };
     if (a.tokens <= 16) return go(std::integral_constant<int, 1>{});
     if (a.tokens <= 32) return go(std::integral_constant<int, 2>{});
-    return go(std::integral_constant<int, 4>{});
+    if constexpr (kFfFewTokens<T> > 32) return go(std::integral_constant<int, 4>{});
+    else return static_cast<int>(EDGC_EINVAL);      // (not reached)
 }
 
-template <typename T>
+template <typename T, int GROUPS>
 hipError_t prepare_few()
 {
-    for (const void* f : {reinterpret_cast<const void*>(&k_ff_few<T, 1, false>), reinterpret_cast<const void*>(&k_ff_few<T, 2, false>),
-                          reinterpret_cast<const void*>(&k_ff_few<T, 4, false>), reinterpret_cast<const void*>(&k_ff_few<T, 1, true>),
-                          reinterpret_cast<const void*>(&k_ff_few<T, 2, true>), reinterpret_cast<const void*>(&k_ff_few<T, 4, true>)})
-        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * 2 * 4 * 64 * 16)) return e;
+    for (const void* f : {reinterpret_cast<const void*>(&k_ff_few<T, GROUPS, false>), reinterpret_cast<const void*>(&k_ff_few<T, GROUPS, true>)})
+        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kFfFewWaves<GROUPS> * 2 * GROUPS * 1024)) return e;
     return hipSuccess;
 }
 
@@ -316,7 +315,7 @@ template <typename T>
 int ff_forward(edgc_ctx* ctx, const edgc_ff& w, const void* x, uint64_t ldx, uint64_t tokens, void* y, uint64_t ldy, void* gate, void* up,
                uint64_t ldg, hipStream_t st)
 {
-    if (tokens <= kFfFewTokens) return ff_forward_few<T>(ctx, w, x, ldx, static_cast<uint32_t>(tokens), y, ldy, gate, up, ldg, st);
+    if (tokens <= kFfFewTokens<T>) return ff_forward_few<T>(ctx, w, x, ldx, static_cast<uint32_t>(tokens), y, ldy, gate, up, ldg, st);
     constexpr int P = FfType<T>::kPlanes;
     const uint64_t H = w.hidden, F = w.ff;
     FfPlan plan(tokens, H, F, w.dtype);
@@ -433,8 +432,11 @@ int prepare_ff_kernels(edgc_ctx* ctx)
 {
     hipError_t e = prepare_tiles<256, 256, __bf16>();
     if (e == hipSuccess) e = prepare_tiles<256, 256, float>();
-    if (e == hipSuccess) e = prepare_few<__bf16>();
-    if (e == hipSuccess) e = prepare_few<float>();
+    if (e == hipSuccess) e = prepare_few<__bf16, 1>();
+    if (e == hipSuccess) e = prepare_few<__bf16, 2>();
+    if (e == hipSuccess) e = prepare_few<float, 1>();
+    if (e == hipSuccess) e = prepare_few<float, 2>();
+    if (e == hipSuccess) e = prepare_few<float, 4>();
     EDGC_HIP_TRY(ctx, e);
     return EDGC_OK;
 }

@@ -1,6 +1,6 @@
 // The feed-forward block's forward products for few tokens: bounded by reading the weights once.
 //
-// A wave has 16 rows of a weight matrix (gated: of both projections) and all tokens, up to 64 in groups of 16, and a share of k; the
+// A wave has 16 rows of a weight matrix (gated: of both projections) and all tokens, in groups of 16, and a share of k; the
 // waves of a block share k and are added up in LDS, in their order.  Where that makes too few waves for the memory, several blocks
 // (gridDim.y) share k, and the last of them to finish adds their sums up, in their order too.  The weights go from memory to the matrix instructions'
 // registers as they lie there, whatever their alignment: a lane brings 16 bytes of a row, 64 bytes of each row per load.  bf16:
@@ -11,7 +11,9 @@
 
 namespace edgc {
 
-constexpr uint32_t kFfFewTokens = 64;
+// Measured, weights of 4096 x 16384 in bf16 and of 2048 x 8192 in fp32, these kernels / the products of ff_gemm.h: bf16, 32 tokens
+// 137 / 133 us, 24 125 / 133; fp32, 64 tokens 98 / 230 us.
+template <typename T> constexpr uint32_t kFfFewTokens = sizeof(T) == 4 ? 64 : 32;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct FfFewArgs {
@@ -55,12 +57,15 @@ template <> struct FfFew<float> {
     }
 };
 
+// Waves of a block at most: with four groups of tokens a wave takes over 128 registers
+template <int GROUPS> constexpr uint32_t kFfFewWaves = GROUPS == 4 ? 8 : 16;
+
 // GROUPS: of 16 tokens
 template <typename T, int GROUPS, bool GATED>
-__global__ __launch_bounds__(1024) void k_ff_few(const FfFewArgs a)
+__global__ __launch_bounds__(64 * kFfFewWaves<GROUPS>) void k_ff_few(const FfFewArgs a)
 {
     using F = FfFew<T>;
-    constexpr int MATS = GATED ? 2 : 1, UNROLL = 4;       // steps whose loads are on their way together
+    constexpr int MATS = GATED ? 2 : 1, UNROLL = MATS + GROUPS <= 3 ? 4 : 2;
     extern __shared__ __align__(16) float red[];            // [waves][MATS * GROUPS][64 lanes][4]
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, waves = blockDim.x / 64, r = lane % 16, h = lane / 16;
     const uint32_t n0 = blockIdx.x * 16, row = min(n0 + r, a.N - 1);
@@ -75,22 +80,49 @@ __global__ __launch_bounds__(1024) void k_ff_few(const FfFewArgs a)
     for (int g = 0; g < GROUPS; ++g) x[g] = static_cast<const T*>(a.x) + min(g * 16 + r, a.tokens - 1) * a.ldx + h * F::kLane;
 
     f32x4 acc[MATS][GROUPS] = {};
-    uint32_t s = s0;
-    for (; s + UNROLL <= min(s1, whole); s += UNROLL) {
-        typename F::reg rw[UNROLL][MATS], rx[UNROLL][GROUPS];
+    // the loads of UNROLL steps are on their way while those before are multiplied
+    typename F::reg rw[2][UNROLL][MATS], rx[2][UNROLL][GROUPS];
+    auto ask = [&](auto to, uint32_t step) {
+        constexpr int b = decltype(to)::value;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
 #pragma unroll
-            for (int m = 0; m < MATS; ++m) rw[u][m] = F::load(w[m] + (s + u) * static_cast<uint64_t>(F::kStep));
+            for (int m = 0; m < MATS; ++m) rw[b][u][m] = F::load(w[m] + (step + u) * static_cast<uint64_t>(F::kStep));
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) rx[u][g] = F::load(x[g] + (s + u) * static_cast<uint64_t>(F::kStep));
+            for (int g = 0; g < GROUPS; ++g) rx[b][u][g] = F::load(x[g] + (step + u) * static_cast<uint64_t>(F::kStep));
         }
+    };
+    auto multiply = [&](auto from) {
+        constexpr int b = decltype(from)::value;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
             for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) acc[m][g] = F::mma(rw[u][m], rx[u][g], acc[m][g]);
+                for (int g = 0; g < GROUPS; ++g) acc[m][g] = F::mma(rw[b][u][m], rx[b][u][g], acc[m][g]);
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0> even;
+    constexpr integral_constant<int, 1> odd;
+    uint32_t s = s0;
+    const uint32_t whole_end = min(s1, whole);
+    if (s + UNROLL <= whole_end) {
+        ask(even, s);
+        for (; s + 3 * UNROLL <= whole_end; s += 2 * UNROLL) {
+            ask(odd, s + UNROLL);
+            multiply(even);
+            ask(even, s + 2 * UNROLL);
+            multiply(odd);
+        }
+        if (s + 2 * UNROLL <= whole_end) {
+            ask(odd, s + UNROLL);
+            multiply(even);
+            multiply(odd);
+            s += 2 * UNROLL;
+        } else {
+            multiply(even);
+            s += UNROLL;
+        }
     }
     for (; s < s1; ++s) {
         const uint64_t at = s * static_cast<uint64_t>(F::kStep);
