@@ -5,8 +5,12 @@
 //
 // Forward: one product whose tiles hold both projections and whose epilogue applies the activation and the product, and one for y.
 // Backward: dA, whose epilogue makes dG, dU and A from the kept projections (dA itself is never stored), dx over both halves in one
-// sum, and the three weight gradients in one launch.  Products: ff_gemm.h.  Operands that are not laid out for them (k contiguous
-// and a multiple of 64, 16-byte aligned, bf16) are first copied into the reserved scratch, transposed or split where needed.
+// sum, and the three weight gradients in one launch.  Products: ff_gemm.h, few tokens forward: ff_few.h.  Either takes the operands as
+// they lie in memory, transposed or not.  Where that cannot be (ff_gemm.h: rows that are not 16-byte aligned, k not a multiple of 64,
+// fp32) they are first copied into the reserved scratch, padded, and in fp32 split into planes.
+//
+// Measured, 4096 x 16384 bf16 with 8192 and 4096 tokens and 2048 x 8192 fp32 with 2048 tokens: the table at the foot of ff_gemm.h's
+// first comment; k_ff_pack, 335 MB of fp32 in and planes out: 101 us.
 #include "ff_few.h"
 
 #include <algorithm>
@@ -163,6 +167,9 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     a.whole = tiles / places * places;
     a.rest = tiles - a.whole;
     a.workers = static_cast<uint32_t>(std::min<uint64_t>(places, static_cast<uint64_t>(a.rest) * a.ksteps * kFfBk / kMinK));
+    // dgate: where there are few tiles the join, whose blocks have a square of four waves each, gets through the long epilogue sooner
+    // than the tile's four waves, and two workers a tile will do (841 x 279 of 320 bf16: @A us, one @B)
+    if (EPI == kFfDgate && a.ksteps >= 2 && a.rest * 2 <= places) a.workers = std::max(a.workers, a.rest * 2);
     // (a last round that is nearly full is not worth the sums' way through memory)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;

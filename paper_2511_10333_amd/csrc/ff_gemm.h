@@ -232,7 +232,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p)
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
 }
 // 16 bytes per lane from `base` + its offset to LDS, one lane's after the other's, from address `to` on.  An instruction of its own,
-// since the compiler would otherwise have every later read of LDS wait for it: wait_loads and a barrier stand before the reads.
+// since the compiler would otherwise have every later read of LDS wait for it: tile_barrier stands before the reads.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to)
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base));
@@ -284,13 +284,10 @@ __device__ __forceinline__ void ff_ask(const FfProblem& p, FfLoaded (&x)[kFfPass
     for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k)
         ff_load<T, EPI, true>(p, m0 + k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>, n0 + lane % kFfLanes<EPI, SINGLE> * 4, x[k]);
 }
-// FULL: the square lies inside the output, and `x` holds what its epilogue loads
-template <typename T, int EPI, bool SINGLE, bool FULL>
-__device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left, const f32x16& right, float* mine, uint32_t lane, uint32_t m0,
-                                          uint32_t n0, const FfLoaded (&x)[kFfPasses<EPI, SINGLE>])
+// the sums to the wave's part of LDS
+template <int EPI, bool SINGLE>
+__device__ __forceinline__ void ff_spread(const f32x16& left, const f32x16& right, float* mine, uint32_t lane)
 {
-    constexpr bool GATED = EPI == kFfGate;
-    const uint32_t c4 = lane % kFfLanes<EPI, SINGLE> * 4, n = n0 + c4;
 #pragma unroll
     for (int j = 0; j < (EPI != kFfGate && SINGLE ? 1 : 2); ++j)
 #pragma unroll
@@ -299,9 +296,20 @@ __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left
             const float4 v = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
             *reinterpret_cast<float4*>(mine + (lane & 31) * kFfRow + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
         }
+}
+__device__ __forceinline__ void ff_wave_sync()
+{
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// and from there through the epilogue.  FULL: the square lies inside the output, and `x` holds what its epilogue loads
+template <typename T, int EPI, bool SINGLE, bool FULL>
+__device__ __forceinline__ void ff_finish(const FfProblem& p, const float* mine, uint32_t lane, uint32_t m0, uint32_t n0,
+                                          const FfLoaded (&x)[kFfPasses<EPI, SINGLE>])
+{
+    constexpr bool GATED = EPI == kFfGate;
+    const uint32_t c4 = lane % kFfLanes<EPI, SINGLE> * 4, n = n0 + c4;
     auto row = [&](int k, const FfLoaded& loaded) {
         const uint32_t r = k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>;
         const float4 s = *reinterpret_cast<const float4*>(mine + r * kFfRow + c4);
@@ -314,18 +322,18 @@ __device__ __forceinline__ void ff_finish(const FfProblem& p, const f32x16& left
         for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k) row(k, x[k]);
     } else {
         const uint32_t n_end = EPI == kFfStore ? p.N : p.n_pad, m_end = EPI == kFfStore ? p.M : p.m_pad;
+        auto m_of = [&](int k) { return m0 + k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>; };
+        FfLoaded loaded = {}, next = {};
+        if (EPI == kFfDgate && m_of(0) < p.M) ff_load<T, EPI, false>(p, m_of(0), n, loaded);
 #pragma unroll 1
         for (int k = 0; k < kFfPasses<EPI, SINGLE>; ++k) {
-            const uint32_t m = m0 + k * (64 / kFfLanes<EPI, SINGLE>) + lane / kFfLanes<EPI, SINGLE>;
-            if (m >= m_end || n >= n_end) continue;
-            FfLoaded loaded = {};
-            if (m < p.M) ff_load<T, EPI, false>(p, m, n, loaded);
+            if (EPI == kFfDgate && k + 1 < kFfPasses<EPI, SINGLE> && m_of(k + 1) < p.M) ff_load<T, EPI, false>(p, m_of(k + 1), n, next);
+            if (m_of(k) >= m_end || n >= n_end) continue;
+            if (EPI != kFfDgate && m_of(k) < p.M) ff_load<T, EPI, false>(p, m_of(k), n, loaded);
             row(k, loaded);
+            if constexpr (EPI == kFfDgate) loaded = next;
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // Where a worker leaves the sums of a tile: in the order of its registers, NI squares of 32 x 32 in a row of them
@@ -533,19 +541,31 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
             float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);
             auto m_of = [&](int s) { return m0 + (wm * MI + s / (NI / 2)) * 32; };
             auto n_of = [&](int s) { return n0 + (GATED ? wn * NI * 16 + s % (NI / 2) * 32 : wn * NI * 32 + s % (NI / 2) * 64); };
-            auto left_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][(GATED ? 1 : 2) * (s % (NI / 2))]; };
-            auto right_of = [&](int s) -> const f32x16& { return acc[s / (NI / 2)][GATED ? s % (NI / 2) + NI / 2 : 2 * (s % (NI / 2)) + 1]; };
             constexpr int SQUARES = MI * NI / 2;
-            FfLoaded x[2][kFfPasses<EPI, false>];
+            FfLoaded x[kFfPasses<EPI, false>], next[kFfPasses<EPI, false>];
             auto inside = [&](int s) { return ff_inside<EPI, false>(p, m_of(s), n_of(s)); };
-            if (inside(0)) ff_ask<T, EPI, false>(p, x[0], lane, m_of(0), n_of(0));
-            ff_each<SQUARES>([&](auto sq) {
-                constexpr int s = decltype(sq)::value;
-                if constexpr (s + 1 < SQUARES)
-                    if (inside(s + 1)) ff_ask<T, EPI, false>(p, x[(s + 1) & 1], lane, m_of(s + 1), n_of(s + 1));
-                if (inside(s)) ff_finish<T, EPI, false, true>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[s & 1]);
-                else ff_finish<T, EPI, false, false>(p, left_of(s), right_of(s), mine, lane, m_of(s), n_of(s), x[0]);
-            });
+            if (inside(0)) ff_ask<T, EPI, false>(p, x, lane, m_of(0), n_of(0));
+            auto square = [&](auto s) {
+                if (s + 1 < SQUARES && inside(s + 1)) ff_ask<T, EPI, false>(p, next, lane, m_of(s + 1), n_of(s + 1));
+                ff_each<SQUARES>([&](auto sq) {
+                    constexpr int k = decltype(sq)::value, i = k / (NI / 2), j = k % (NI / 2);
+                    if (s == k) ff_spread<EPI, false>(acc[i][(GATED ? 1 : 2) * j], acc[i][GATED ? j + NI / 2 : 2 * j + 1], mine, lane);
+                });
+                ff_wave_sync();
+                if (inside(s)) ff_finish<T, EPI, false, true>(p, mine, lane, m_of(s), n_of(s), x);
+                else ff_finish<T, EPI, false, false>(p, mine, lane, m_of(s), n_of(s), x);
+                ff_wave_sync();
+#pragma unroll
+                for (int k = 0; k < kFfPasses<EPI, false>; ++k) x[k] = next[k];
+            };
+            // Long epilogues as a loop, whose code stays in the instruction cache (256 x 256, dgate / gate / dw of 4096 x 16384, unrolled
+            // and not: 674 and 641 us / 2975 and 2920 / 1368 and 1380)
+            if constexpr (EPI == kFfStore) {
+                ff_each<SQUARES>(square);
+            } else {
+#pragma unroll 1
+                for (int s = 0; s < SQUARES; ++s) square(s);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < MI; ++i)
@@ -594,12 +614,12 @@ __global__ __launch_bounds__(256) void k_ff_join(const FfArgs args)
     const uint32_t m0 = tm * BM + (wave / 2 * MI + i) * 32, n0 = tn * (BN / BOTH) + (wave % 2 * ACROSS + j) * 32;
     float* const mine = stage + wave * (32 * kFfRow);
     FfLoaded x[kFfPasses<EPI, true>];
-    if (ff_inside<EPI, true>(p, m0, n0)) {
-        ff_ask<T, EPI, true>(p, x, lane, m0, n0);
-        ff_finish<T, EPI, true, true>(p, acc[0], acc[BOTH - 1], mine, lane, m0, n0, x);
-    } else {
-        ff_finish<T, EPI, true, false>(p, acc[0], acc[BOTH - 1], mine, lane, m0, n0, x);
-    }
+    const bool inside = ff_inside<EPI, true>(p, m0, n0);
+    if (inside) ff_ask<T, EPI, true>(p, x, lane, m0, n0);
+    ff_spread<EPI, true>(acc[0], acc[BOTH - 1], mine, lane);
+    ff_wave_sync();
+    if (inside) ff_finish<T, EPI, true, true>(p, mine, lane, m0, n0, x);
+    else ff_finish<T, EPI, true, false>(p, mine, lane, m0, n0, x);
 }
 
 }  // namespace edgc
