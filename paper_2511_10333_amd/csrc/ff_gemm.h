@@ -72,9 +72,20 @@ __device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
         a = z * s;
         da = s * (1.0f + z * (1.0f - s));
     } else if (act == EDGC_GELU) {
-        const float cdf = 0.5f * erfcf(z * -0.70710678118654752f);
+        // Phi(-|z|) = exp(-z^2 / 2) t p(t), t = 1 / (1 + |z| / sqrt 8): p by least squares of the relative error, weighted towards its
+        // peaks (4.4e-8 of the result up to |z| = 20; 1.2e-7 absolute with fp32's roundings).  The library's function took
+        // 3.23 ms instead of 3.09 in the projections of 8192 tokens, 5120 x 20480 (SiLU 2.97).
+        constexpr float p[9] = {1.410421729e-01f, 1.412060559e-01f, 1.214175522e-01f,
+                                1.018762514e-01f, -1.457415149e-02f, 1.408663541e-01f,
+                                -2.452028543e-01f, 1.430617869e-01f, -2.969318256e-02f};
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.35355339059327376f, 1.0f)), e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+        float q = p[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) q = fmaf(q, t, p[i]);
+        q *= t * e;
+        const float cdf = z < 0.f ? q : 1.0f - q;
         a = z * cdf;
-        da = cdf + z * __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z) * 0.39894228040143268f;
+        da = cdf + z * e * 0.39894228040143268f;
     } else {
         const float k = 0.79788456080286536f, c = 0.044715f;
         const float s = ff_sigmoid(2.0f * k * (z + c * z * z * z));
