@@ -563,9 +563,10 @@ int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, u
  * for the second.  tokens = 0 does nothing (backward without accumulate: the
  * weight gradients become zero).
  * Errors: EDGC_EINVAL for null or misaligned pointers (multiples of the
- * element's size are enough; 16-byte aligned rows of a multiple of 64 columns
- * save a copy), hidden or ff 0 or over 2^20, tokens over 2^21, leading
- * dimensions too small or over 2^40, or sizes over the reservation. */
+ * element's size are enough; with EDGC_BF16, 16-byte aligned rows and widths
+ * that are multiples of 64, backward tokens too, save copies), hidden or ff 0
+ * or over 2^20, tokens over 2^21, leading dimensions too small or over 2^40, or
+ * sizes over the reservation. */
 typedef enum { EDGC_SILU = 0, EDGC_GELU = 1, EDGC_GELU_TANH = 2 } edgc_act;
 typedef struct {
     const void *w_gate, *w_up, *w_down;

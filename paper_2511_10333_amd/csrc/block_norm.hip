@@ -8,6 +8,8 @@
 //
 // Either norm can be missing (y null: x' = x; w_pre null: no n).  Bounded by memory: a row is read once into registers, its sums
 // are taken across the threads that hold it, and what it gives is written once.  A row is held by a wave (no barrier) or by a block.
+// bf16: 16384 rows of 5120 forward, 671 MB, 150 us (4.5 TB/s); 8192 rows of 4096 backward, 403 MB, 94 us (4.3 TB/s) and 4 for the
+// column sums; one row 7 us, the launch.
 #include "edgc_internal.h"
 
 #include <algorithm>

@@ -3,7 +3,8 @@
 // A wave has 16 rows of a weight matrix (gated: of both projections) and all tokens, in groups of 16, and a share of k; the
 // waves of a block share k and are added up in LDS, in their order.  Where that makes too few waves for the memory, several blocks
 // (gridDim.y) share k, and the last of them to finish adds their sums up, in their order too.  The weights go from memory to the matrix instructions'
-// registers as they lie there, whatever their alignment: a lane brings 16 bytes of a row, 64 bytes of each row per load.  bf16:
+// registers as they lie there, whatever their alignment (one token, 403 MB of bf16 in two launches: 82 us, 4.9 TB/s; 24 tokens, 201 MB of
+// fp32: 58 us): a lane brings 16 bytes of a row, 64 bytes of each row per load.  bf16:
 // 16 x 16 x 32.  fp32: 16 x 16 x 4 in fp32, four for the four values of a lane; any order of k will do that both operands have.
 #pragma once
 
