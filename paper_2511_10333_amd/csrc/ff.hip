@@ -268,7 +268,7 @@ struct FfPass {
 
 // Few tokens.  About 16 waves on a compute unit, each with eight steps of k at least: 4 to 16 waves of a block share k, and where there
 // are fewer blocks than compute units eight waves and up to four blocks.  (24 tokens, fp32, 2048 rows of 8192: 128 blocks of 16 waves
-// 38.5 us, 512 of 8 22.6; one token, bf16, 4096 rows of 16384: 256 of 16 27.6 us, 512 of 8 31.3.)
+// 45 us, 512 of 8 28; one token, bf16, 4096 rows of 16384: 256 of 16 29.4 us, 512 of 8 30.8.)
 template <typename T, bool GATED>
 int launch_few(edgc_ctx* ctx, FfFewArgs& a, int kid, hipStream_t st)
 {

@@ -2,17 +2,20 @@
 //
 // A wave has 16 rows of a weight matrix (gated: of both projections) and all tokens, in groups of 16, and a share of k; the
 // waves of a block share k and are added up in LDS, in their order.  Where that makes too few waves for the memory, several blocks
-// (gridDim.y) share k, and the last of them to finish adds their sums up, in their order too.  The weights go from memory to the matrix instructions'
-// registers as they lie there, whatever their alignment (one token, 403 MB of bf16 in two launches: 82 us, 4.9 TB/s; 24 tokens, 201 MB of
-// fp32: 58 us): a lane brings 16 bytes of a row, 64 bytes of each row per load.  bf16:
-// 16 x 16 x 32.  fp32: 16 x 16 x 4 in fp32, four for the four values of a lane; any order of k will do that both operands have.
+// (gridDim.y) share k, and the last of them to finish adds their sums up, in their order too.  The weights go from memory to the matrix
+// instructions' registers as they lie there, whatever their alignment: a lane brings 16 bytes of a row, 64 bytes of each row per load.
+// bf16: 16 x 16 x 32.  fp32: 16 x 16 x 4 in fp32, four for the four values of a lane; any order of k will do that both operands have.
+//
+// Weights from memory, both launches: one token, 403 MB of bf16, 78 to 82 us (5.0 TB/s), 16 tokens 103, 32 133; 201 MB of fp32, one
+// token 44, 24 tokens 69.  What more tokens cost is x on its way into every compute unit: together with the weights 6 to 6.7 TB/s.
+// (Its rows at other strides, its loads behind all of the weights', four steps on their way instead of two: the same.)
 #pragma once
 
 #include "ff_gemm.h"
 
 namespace edgc {
 
-// Measured, weights of 4096 x 16384 in bf16 and of 2048 x 8192 in fp32, these kernels / the products of ff_gemm.h: bf16, 32 tokens
+// Measured, weights of 4096 x 16384 in bf16 and of 2048 x 8192 in fp32 call after call, these kernels / the products of ff_gemm.h: bf16, 32 tokens
 // 137 / 133 us, 24 125 / 133; fp32, 64 tokens 98 / 230 us.
 template <typename T> constexpr uint32_t kFfFewTokens = sizeof(T) == 4 ? 64 : 32;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
