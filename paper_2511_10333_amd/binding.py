@@ -172,7 +172,8 @@ class _FF(C.Structure):
 @dataclass
 class Tensor:
     """One entry of a batch: torch CUDA tensors (``residual``, ``Q``, ``P`` may be None for a
-    tensor that is sent as it stands; 1-D gradients are taken as one row)."""
+    tensor that is sent as it stands; 1-D gradients are taken as one row).  Rows and columns are below 2^32
+    each: a longer flat gradient is given in parts."""
     grad: object
     grad_out: object
     residual: object = None
@@ -630,6 +631,8 @@ class Context:
         for i, t in enumerate(tensors):
             g = t.grad if t.grad is not None else t.grad_out
             m, n = (1, g.numel()) if g.dim() == 1 else g.shape
+            if m >> 32 or n >> 32:
+                raise ValueError("a gradient has fewer than 2^32 rows and columns: give a longer one in parts")
             ld = lambda x: (x.stride(0) if x.dim() == 2 else x.numel()) if x is not None else 0
             ptr = lambda x: x.data_ptr() if x is not None else None
             arr[i] = _Tensor(ptr(t.grad), ptr(t.grad_out), ptr(t.residual), ptr(t.Q), ptr(t.P),
