@@ -172,8 +172,8 @@ class _FF(C.Structure):
 @dataclass
 class Tensor:
     """One entry of a batch: torch CUDA tensors (``residual``, ``Q``, ``P`` may be None for a
-    tensor that is sent as it stands; 1-D gradients are taken as one row).  Rows and columns are below 2^32
-    each: a longer flat gradient is given in parts."""
+    tensor that is sent as it stands; 1-D gradients are taken as one row).  Gradients have contiguous rows
+    (of any row stride), and rows and columns are below 2^32 each: a longer flat gradient is given in parts."""
     grad: object
     grad_out: object
     residual: object = None
@@ -390,6 +390,20 @@ def _rows(name, t, dtype, shape) -> int:
     if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
     return ld if rows > 1 else max(ld, cols)
+
+
+def _gradient_ld(t) -> int:
+    """Leading dimension of a gradient, a matrix of contiguous rows or a contiguous vector (one row)."""
+    if t.dim() == 1:
+        if t.numel() > 1 and t.stride(0) != 1:
+            raise ValueError("a gradient must have contiguous rows: this vector's elements are not adjacent")
+        return t.numel()
+    if t.dim() != 2:
+        raise ValueError("a gradient must be a vector or a matrix")
+    ld, step = t.stride()
+    if t.shape[1] > 1 and step != 1:
+        raise ValueError("a gradient must have contiguous rows: this matrix's columns are not adjacent")
+    return ld
 
 
 class FeedForward:
@@ -633,7 +647,7 @@ class Context:
             m, n = (1, g.numel()) if g.dim() == 1 else g.shape
             if m >> 32 or n >> 32:
                 raise ValueError("a gradient has fewer than 2^32 rows and columns: give a longer one in parts")
-            ld = lambda x: (x.stride(0) if x.dim() == 2 else x.numel()) if x is not None else 0
+            ld = lambda x: _gradient_ld(x) if x is not None else 0
             ptr = lambda x: x.data_ptr() if x is not None else None
             arr[i] = _Tensor(ptr(t.grad), ptr(t.grad_out), ptr(t.residual), ptr(t.Q), ptr(t.P),
                              ld(t.grad), ld(t.grad_out), m, n,

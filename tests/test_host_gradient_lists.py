@@ -21,3 +21,26 @@ def test_sizes_beyond_the_descriptors_fields_are_refused_not_cut():
     assert (d.m, d.n) == (1, 2 ** 32 - 1)
     d = _one(torch.empty((2 ** 20, 2 ** 13), device="meta"))
     assert (d.m, d.n, d.ld) == (2 ** 20, 2 ** 13, 2 ** 13)
+
+
+def test_views_whose_neighbours_are_not_neighbours_in_memory_are_refused():
+    """The library reads rows of adjacent elements: a column of a matrix, or a transposed one, is not that."""
+    g = torch.zeros(10, 4)
+    for bad in (g[:, 0], g.t(), g[:, ::2], g.view(-1)[::2], torch.zeros(1).expand(10), g.t()[:1]):
+        with pytest.raises(ValueError, match="contiguous rows"):
+            _one(bad)
+        with pytest.raises(ValueError, match="contiguous rows"):
+            _one(torch.zeros(bad.shape), bad)
+    for bad in (g.view(2, 5, 4), torch.zeros(())):
+        with pytest.raises(ValueError):
+            _one(bad)
+    d = _one(g[:, 1:3])                                     # columns of a wider buffer
+    assert (d.m, d.n, d.ld, d.ld_out) == (10, 2, 4, 4)
+    d = _one(g[:, :1], g[:, 1:2])
+    assert (d.m, d.n, d.ld) == (10, 1, 4)
+    d = _one(g.t()[:, :1])                                  # a column as a matrix: nothing lies beside its elements' rows
+    assert (d.m, d.n, d.ld) == (4, 1, 1)
+    d = _one(g[3], g[4])
+    assert (d.m, d.n) == (1, 4)
+    d = _one(g.view(-1)[5:6:3])                             # one element
+    assert (d.m, d.n) == (1, 1)
