@@ -173,7 +173,8 @@ class _FF(C.Structure):
 class Tensor:
     """One entry of a batch: torch CUDA tensors (``residual``, ``Q``, ``P`` may be None for a
     tensor that is sent as it stands; 1-D gradients are taken as one row).  Gradients have contiguous rows
-    (of any row stride), and rows and columns are below 2^32 each: a longer flat gradient is given in parts."""
+    (of any row stride), ``grad`` and ``grad_out`` one type and shape, and rows and columns are below
+    2^32 each: a longer flat gradient is given in parts."""
     grad: object
     grad_out: object
     residual: object = None
@@ -647,6 +648,12 @@ class Context:
             m, n = (1, g.numel()) if g.dim() == 1 else g.shape
             if m >> 32 or n >> 32:
                 raise ValueError("a gradient has fewer than 2^32 rows and columns: give a longer one in parts")
+            out = t.grad_out
+            if out is not None and out is not g and g.numel():      # (an empty one is the library's to refuse)
+                if out.dtype != g.dtype:
+                    raise TypeError("grad_out must be of its gradient's type")
+                if out.shape != g.shape and ((1, out.numel()) if out.dim() == 1 else tuple(out.shape)) != (m, n):
+                    raise ValueError("grad_out must be of its gradient's shape")
             ld = lambda x: _gradient_ld(x) if x is not None else 0
             ptr = lambda x: x.data_ptr() if x is not None else None
             arr[i] = _Tensor(ptr(t.grad), ptr(t.grad_out), ptr(t.residual), ptr(t.Q), ptr(t.P),

@@ -44,3 +44,23 @@ def test_views_whose_neighbours_are_not_neighbours_in_memory_are_refused():
     assert (d.m, d.n) == (1, 4)
     d = _one(g.view(-1)[5:6:3])                             # one element
     assert (d.m, d.n) == (1, 1)
+
+
+def test_an_output_of_another_type_or_size_is_refused():
+    """grad_out is written as a matrix of the gradient's type and shape: anything narrower or shorter would be written past its end."""
+    g = torch.zeros(6, 8)
+    for bad in (torch.zeros(6, 8).bfloat16(), torch.zeros(6, 8).double()):
+        with pytest.raises(TypeError, match="grad_out"):
+            _one(g, bad)
+    with pytest.raises(TypeError, match="grad_out"):
+        _one(g.bfloat16(), g)
+    for bad in (torch.zeros(5, 8), torch.zeros(6, 7), torch.zeros(8, 6), torch.zeros(48), torch.zeros(6), torch.zeros(0)):
+        with pytest.raises(ValueError, match="grad_out"):
+            _one(g, bad)
+    with pytest.raises(ValueError, match="grad_out"):
+        _one(torch.zeros(9), torch.zeros(8))
+    with pytest.raises(ValueError, match="grad_out"):
+        _one(torch.zeros(9), torch.zeros(9, 1))
+    assert _one(torch.zeros(9), torch.zeros(1, 9)).n == 9           # one row either way
+    assert edgc.PreparedBatch([edgc.Tensor(None, g)]).arr[0].m == 6
+    assert edgc.PreparedBatch([edgc.Tensor(g, None)]).arr[0].grad_out is None
