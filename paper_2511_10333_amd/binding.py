@@ -393,6 +393,13 @@ def _rows(name, t, dtype, shape) -> int:
     return ld if rows > 1 else max(ld, cols)
 
 
+def _check_u32(*sizes) -> None:
+    """Sizes that travel in 32 bits."""
+    for n in sizes:
+        if n >> 32:
+            raise ValueError("tokens and widths must be 0 or more and below 2^32")
+
+
 def _gradient_ld(t) -> int:
     """Leading dimension of a gradient, a matrix of contiguous rows or a contiguous vector (one row)."""
     if t.dim() == 1:
@@ -418,6 +425,7 @@ class FeedForward:
         if w_gate.dim() != 2:
             raise ValueError("w_gate must be ff x hidden")
         self.ff, self.hidden = (int(d) for d in w_gate.shape)
+        _check_u32(self.ff, self.hidden)
         self.dtype, self.act = w_gate.dtype, act
         self.weights = (w_gate, w_up, w_down)
         lds = [_rows(n, w, self.dtype, s) for n, w, s in (("w_gate", w_gate, (self.ff, self.hidden)),
@@ -733,6 +741,7 @@ class Context:
 
     def reserve_block_norm(self, tokens: int, hidden: int) -> None:
         """edgc_reserve_block_norm: scratch of :meth:`block_norm_backward` for up to that many tokens and hidden units."""
+        _check_u32(tokens, hidden)
         self._check(self._L.edgc_reserve_block_norm(self._h, tokens, hidden), "edgc_reserve_block_norm")
 
     @staticmethod
@@ -786,12 +795,14 @@ class Context:
             _load_torch()
         if dtype not in _codes:
             raise TypeError("dtype must be float32 or bfloat16")
+        _check_u32(tokens, hidden, ff)
         self._check(self._L.edgc_reserve_ff(self._h, _codes[dtype], tokens, hidden, ff, 1 if backward else 0), "edgc_reserve_ff")
 
     def ff_forward(self, ff: FeedForward, x, y, gate=None, up=None, stream=None) -> None:
         """edgc_ff_forward: y = (act(x w_gate^T) * (x w_up^T)) w_down^T; x, y tokens x hidden.  ``gate``, ``up`` (tokens x ff)
         keep the two projections for :meth:`ff_backward`."""
         t = x.shape[0]
+        _check_u32(t)
         ldx, ldy = _rows("x", x, ff.dtype, (t, ff.hidden)), _rows("y", y, ff.dtype, (t, ff.hidden))
         ldk = 0
         if gate is not None and up is not None:
@@ -807,6 +818,7 @@ class Context:
         """edgc_ff_backward: the gradients of x and of the three weights from dy, x and the kept projections; ``accumulate``
         adds the weights' gradients to what is there."""
         t, dt, th, tf = x.shape[0], ff.dtype, (x.shape[0], ff.hidden), (x.shape[0], ff.ff)
+        _check_u32(t)
         ldk = _rows("gate", gate, dt, tf)
         if _rows("up", up, dt, tf) != ldk:
             raise ValueError("gate and up must have one row stride")

@@ -1,0 +1,40 @@
+"""Arguments of the block operators that the binding has to refuse or take before the library sees them (no GPU is needed)."""
+import types
+
+import pytest
+import torch
+
+import paper_2511_10333_amd as edgc
+
+STREAM = types.SimpleNamespace(cuda_stream=0)
+
+
+def _no_context():
+    """A Context whose library calls all answer EDGC_EINVAL, since it has no handle."""
+    c = object.__new__(edgc.Context)
+    c._L, c._h = edgc.load_library(), None
+    return c
+
+
+def test_tokens_and_widths_beyond_32_bits_are_refused_not_cut():
+    """The library's own limits come after the arguments' 32 bits: 2^32 + 16 tokens are not 16."""
+    c, many = _no_context(), 2 ** 32 + 16
+    w = edgc.FeedForward(torch.zeros(8, 8), torch.zeros(8, 8), torch.zeros(8, 8))
+    m = lambda rows, cols: torch.empty((rows, cols), device="meta")
+    x, k = m(many, 8), m(many, 8)
+    with pytest.raises(ValueError, match="2\\^32"):
+        c.ff_forward(w, x, x, stream=STREAM)
+    with pytest.raises(ValueError, match="2\\^32"):
+        c.ff_backward(w, x, k, k, x, x, *w.weights, stream=STREAM)
+    for reserve in ((many, 8, 8), (8, many, 8), (8, 8, many), (-1, 8, 8)):
+        with pytest.raises(ValueError, match="2\\^32"):
+            c.reserve_ff(torch.float32, *reserve)
+    for reserve in ((many, 8), (8, many), (-1, 8)):
+        with pytest.raises(ValueError, match="2\\^32"):
+            c.reserve_block_norm(*reserve)
+    with pytest.raises(ValueError, match="2\\^32"):
+        edgc.FeedForward(m(many, 8), m(many, 8), m(8, many))
+    with pytest.raises(ValueError, match="2\\^32"):
+        edgc.FeedForward(m(8, many), m(8, many), m(many, 8))
+    with pytest.raises(edgc.EdgcError):                     # what fits is handed on
+        c.ff_forward(w, torch.zeros(4, 8), torch.zeros(4, 8), stream=STREAM)
