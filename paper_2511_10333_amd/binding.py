@@ -756,8 +756,8 @@ class Context:
         _check_dense(names[1], vectors, dtype, (h,))
         _check_dense(("rstd_post", "rstd_pre"), stats, _torch.float32, (t,))
         if gate is not None:
-            if rows_per_gate < 1:
-                raise ValueError("rows_per_gate must be >= 1 with a gate")
+            if rows_per_gate < 1 or rows_per_gate >> 64:
+                raise ValueError("rows_per_gate must be >= 1 with a gate, and below 2^64")
             _check_dense(("gate",), (gate,), dtype, (-(-t // rows_per_gate), h))
         return t, h
 

@@ -38,3 +38,16 @@ def test_tokens_and_widths_beyond_32_bits_are_refused_not_cut():
         edgc.FeedForward(m(8, many), m(8, many), m(many, 8))
     with pytest.raises(edgc.EdgcError):                     # what fits is handed on
         c.ff_forward(w, torch.zeros(4, 8), torch.zeros(4, 8), stream=STREAM)
+
+
+def test_rows_per_gate_beyond_64_bits_is_refused_not_cut():
+    """2^64 + 3 tokens per row of the gate are one row for all of them, and not one for every three."""
+    c = _no_context()
+    x, v, g = torch.zeros(9, 8), torch.zeros(8), torch.zeros(1, 8)
+    r = torch.zeros(9)
+    with pytest.raises(ValueError, match="rows_per_gate"):
+        c.block_norm_forward(x, x, v, g, v, x, x, rows_per_gate=2 ** 64 + 3, stream=STREAM)
+    with pytest.raises(ValueError, match="rows_per_gate"):
+        c.block_norm_backward(x, x, x, x, v, g, v, r, r, x, x, v, g, v, rows_per_gate=2 ** 64 + 3, stream=STREAM)
+    with pytest.raises(edgc.EdgcError):                     # what fits is handed on
+        c.block_norm_forward(x, x, v, g, v, x, x, rows_per_gate=2 ** 64 - 1, stream=STREAM)
