@@ -390,7 +390,7 @@ def _rows(name, t, dtype, shape) -> int:
     ld, step = t.stride()
     if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return ld if rows > 1 else max(ld, cols)
+    return ld if rows > 1 else cols
 
 
 def _check_u32(*sizes) -> None:

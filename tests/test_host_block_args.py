@@ -51,3 +51,20 @@ def test_rows_per_gate_beyond_64_bits_is_refused_not_cut():
         c.block_norm_backward(x, x, x, x, v, g, v, r, r, x, x, v, g, v, rows_per_gate=2 ** 64 + 3, stream=STREAM)
     with pytest.raises(edgc.EdgcError):                     # what fits is handed on
         c.block_norm_forward(x, x, v, g, v, x, x, rows_per_gate=2 ** 64 - 1, stream=STREAM)
+
+
+def test_the_row_stride_of_a_single_row_does_not_count():
+    """One token's projections may lie in buffers of different widths, and a single row may have any stride."""
+    c = _no_context()
+    w = edgc.FeedForward(torch.zeros(12, 8), torch.zeros(12, 8), torch.zeros(8, 12))
+    x, gate, up = torch.zeros(1, 8), torch.zeros(1, 12), torch.zeros(1, 20)[:, :12]
+    up = up.as_strided((1, 12), (20, 1))
+    with pytest.raises(edgc.EdgcError):                     # handed on, and refused for want of a context alone
+        c.ff_forward(w, x, x.clone(), gate, up, stream=STREAM)
+    with pytest.raises(edgc.EdgcError):
+        c.ff_backward(w, x, gate, up, x, x.clone(), *w.weights, stream=STREAM)
+    far = torch.zeros(12, dtype=torch.bfloat16).as_strided((1, 12), (2 ** 41, 1))
+    one = edgc.FeedForward(far, far, torch.zeros(12, 1, dtype=torch.bfloat16))
+    assert (one.c.ld_gate, one.c.ld_up, one.c.ld_down) == (12, 12, 1)
+    with pytest.raises(ValueError):                         # of two rows it does
+        c.ff_forward(w, torch.zeros(2, 8), torch.zeros(2, 8), torch.zeros(2, 12), torch.zeros(2, 20)[:, :12], stream=STREAM)
