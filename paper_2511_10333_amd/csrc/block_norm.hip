@@ -589,7 +589,7 @@ extern "C" int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_
             b.part = ctx->norm.part; b.w_post = w_post; b.dw_pre = w_pre ? dw_pre : nullptr; b.dw_post = w_post ? dw_post : nullptr; b.dgate = dgate;
             b.tokens = tokens; b.rows_per_gate = rows_per_gate; b.hidden = hidden; b.rows = a.rows; b.groups = groups; b.scale = scale;
             // gate rows that go over a group's end can only be where rows of the gate are longer than one token
-            const uint64_t gates = gate && groups > 1 && rows_per_gate > 1 ? (tokens + rows_per_gate - 1) / rows_per_gate : 0;
+            const uint64_t gates = gate && groups > 1 && rows_per_gate > 1 ? (tokens - 1) / rows_per_gate + 1 : 0;
             b.by_group = gates && gates >= groups;
             const uint32_t crossing = b.by_group ? groups - 1 : static_cast<uint32_t>(gates);
             const dim3 grid((hidden + kSumCols - 1) / kSumCols, 2 + crossing);
