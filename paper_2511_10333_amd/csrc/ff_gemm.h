@@ -94,8 +94,10 @@ __device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
     } else {
         const float k = 0.79788456080286536f, c = 0.044715f;
         const float s = ff_sigmoid(2.0f * k * (z + c * z * z * z));
+        // (from the middle outwards: t is zero long before z^2 overflows)
+        const float t = z * s * (1.0f - s);
         a = z * s;
-        da = s + 2.0f * k * z * s * (1.0f - s) * (1.0f + 3.0f * c * z * z);
+        da = s + 2.0f * k * (t + 3.0f * c * (t * z) * z);
     }
 }
 
