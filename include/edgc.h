@@ -492,7 +492,8 @@ int edgc_entropy_estimate_noalloc(edgc_ctx* ctx, const void* grad, edgc_dtype dt
  *   edgc_clip_batch: reads S from where the first call put it, clips, and
  *     writes {norm, c} to norm_coef (device float[2], or NULL).  A norm that is
  *     not finite (an element was Inf or NaN) hands the gradients on as they
- *     are: the caller sees it in norm_coef[0].
+ *     are: the caller sees it in norm_coef[0].  (A finite norm beyond fp32 clips,
+ *     and is written there as fp32's largest number.)
  * Errors: EDGC_EINVAL for a null or misaligned pointer, an empty tensor, a
  * leading dimension below n or over 2^40, two leading dimensions for a
  * gradient clipped in place, max_norm that is not positive and finite.

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void k_clip(const GradList list, const do
     const double norm = sqrt(*sumsq);
     const float coef = isfinite(norm) ? static_cast<float>(fmin(1.0, max_norm / (norm + kClipEps))) : 1.0f;
     if (norm_coef && blockIdx.x == 0 && threadIdx.x == 0) {
-        norm_coef[0] = static_cast<float>(norm);
+        norm_coef[0] = static_cast<float>(isfinite(norm) ? fmin(norm, 3.4028234663852886e38) : norm);
         norm_coef[1] = coef;
     }
     const uint64_t lane_first = list.first[threadIdx.x & 63];
