@@ -22,6 +22,14 @@ RANKS = [4, 8, 16, 32, 64]
 CHUNK, STRIDE, BINS = 64, 100, 1024
 
 
+def reference_shape(shapes):
+    """The shape that the rank rule's error function is evaluated at: the smallest matrix that is compressed at every rank.  (Where a
+    model has none, a square of twice the largest rank, so that the rule still answers.)"""
+    r = max(RANKS)
+    matrices = [tuple(s) for s in shapes if len(s) == 2 and min(s) >= r and not tensor_bypassed(*s, r)]
+    return min(matrices, key=lambda s: s[0] * s[1], default=(2 * r, 2 * r))
+
+
 class Model:
     """Weights of ``layers`` blocks, their gradients, and the two passes through them."""
 
@@ -142,7 +150,7 @@ def train(layers=4, hidden=512, ff=2048, tokens=1024, sequence=256, steps=40, wi
     model = Model(ctx, layers, hidden, ff, tokens, sequence, dtype, seed=seed + 2)
     step = Step(model, max_norm, lr, momentum)
     state = RankState()
-    prm = RankParams(128, 128, min(RANKS), max(RANKS), allowed=RANKS, total_iters=steps)
+    prm = RankParams(*reference_shape([w.shape for w, _ in step.pairs]), min(RANKS), max(RANKS), allowed=RANKS, total_iters=steps)
     g = torch.Generator(device="cuda").manual_seed(seed)
     losses, entropies, rank = [], [], 0
     for i in range(steps):
