@@ -52,7 +52,7 @@ typedef enum { EDGC_F32 = 0, EDGC_BF16 = 1 } edgc_dtype;
 typedef enum {
     EDGC_OK         =  0,
     EDGC_EINVAL     = -1,   /* bad argument (null / misaligned pointer, size out of range)  */
-    EDGC_ENOMEM     = -2,   /* allocation failed (edgc_create, edgc_reserve_batch)         */
+    EDGC_ENOMEM     = -2,   /* allocation failed (edgc_create, edgc_reserve_*)             */
     EDGC_EHIP       = -3,   /* a HIP call failed; see edgc_last_error                      */
     EDGC_ENOTIMPL   = -4,
     EDGC_ENONFINITE = -5    /* empty sample, or no finite value in it                      */
@@ -525,8 +525,12 @@ int edgc_clip_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, e
  * dx is also the gradient of x.  dx may be the same buffer as dx_out, dy the
  * same as dn or y.  dx_out may be NULL where y is (it then counts as zero).
  * Arithmetic and sums are fp32 for either dtype, in a fixed order; every
- * output is rounded once.  The backward pass needs scratch: reserve it for the
- * largest tokens and hidden (it synchronises the device; not a hot call).
+ * output is rounded once.
+ * The backward pass needs scratch: reserve it for the largest tokens and hidden
+ * (not a hot call).  A reservation replaces the limits of the one before.  It
+ * keeps the memory where that is enough; otherwise it synchronises the device,
+ * frees and allocates, and a graph captured before has to be captured again
+ * (tokens = 0 frees alone).
  * tokens = 0 does nothing (backward: the weight gradients become zero).
  * Errors: EDGC_EINVAL for null or misaligned pointers, hidden = 0 or over
  * 16384, tokens over 2^31, rows_per_gate = 0 with a gate, a scale that is not
@@ -559,10 +563,12 @@ int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, u
  *   edgc_ff_backward: from the kept G and U; the weight gradients are
  *     overwritten, or added to with accumulate != 0 (micro-batches).  They are
  *     matrices as the batched calls take them.  No output may overlap an input.
- * Both need scratch for the largest tokens and the widths at hand:
- * edgc_reserve_ff (synchronises the device; not a hot call), with backward != 0
- * for the second.  tokens = 0 does nothing (backward without accumulate: the
- * weight gradients become zero).
+ * Both need scratch for the largest tokens and the widths at hand (every operand
+ * counted as copied, and 512 KiB of partial sums per compute unit):
+ * edgc_reserve_ff, with backward != 0 for the second.  Not a hot call; what it
+ * replaces, keeps and frees is as for edgc_reserve_block_norm.  tokens = 0 in a
+ * pass does nothing (backward without accumulate: the weight gradients become
+ * zero).
  * Errors: EDGC_EINVAL for null or misaligned pointers (multiples of the
  * element's size are enough; with EDGC_BF16, 16-byte aligned rows and widths
  * that are multiples of 64, backward tokens too, save copies), hidden or ff 0

@@ -740,7 +740,8 @@ class Context:
         self._check(rc, "edgc_clip_batch")
 
     def reserve_block_norm(self, tokens: int, hidden: int) -> None:
-        """edgc_reserve_block_norm: scratch of :meth:`block_norm_backward` for up to that many tokens and hidden units."""
+        """edgc_reserve_block_norm: scratch of :meth:`block_norm_backward` for up to that many tokens and hidden units, in place
+        of an earlier reservation's limits.  Where its memory is not enough it is freed: capture graphs afterwards."""
         _check_u32(tokens, hidden)
         self._check(self._L.edgc_reserve_block_norm(self._h, tokens, hidden), "edgc_reserve_block_norm")
 
@@ -790,7 +791,7 @@ class Context:
 
     def reserve_ff(self, dtype, tokens: int, hidden: int, ff: int, backward: bool = False) -> None:
         """edgc_reserve_ff: scratch of :meth:`ff_forward` (and :meth:`ff_backward`) for up to that many tokens of that
-        width; ``dtype``: torch.float32 or torch.bfloat16."""
+        width, in place of an earlier reservation (see :meth:`reserve_block_norm`); ``dtype``: torch.float32 or torch.bfloat16."""
         if _torch is None:
             _load_torch()
         if dtype not in _codes:

@@ -486,15 +486,18 @@ extern "C" int edgc_reserve_block_norm(edgc_ctx* ctx, uint32_t tokens, uint32_t 
     if (!ctx) return EDGC_EINVAL;
     if (hidden == 0 || hidden > kMaxHidden) return fail(ctx, EDGC_EINVAL, "hidden must be 1 to 16384");
     EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
-    EDGC_HIP_TRY(ctx, hipDeviceSynchronize());          // nothing may still be using the old scratch
-    if (ctx->norm.part) (void)hipFree(ctx->norm.part);
-    ctx->norm = NormScratch{};
-    if (tokens == 0) return EDGC_OK;
-    const size_t groups = std::min(tokens, most_groups(ctx));
-    if (hipMalloc(reinterpret_cast<void**>(&ctx->norm.part), groups * kSums * hidden * sizeof(float)) != hipSuccess) {
-        (void)hipGetLastError();
+    const size_t need = static_cast<size_t>(std::min(tokens, most_groups(ctx))) * kSums * hidden;
+    if (need == 0 || need > ctx->norm.held) {
+        EDGC_HIP_TRY(ctx, hipDeviceSynchronize());      // nothing may still be using the old scratch
+        if (ctx->norm.part) (void)hipFree(ctx->norm.part);
         ctx->norm = NormScratch{};
-        return fail(ctx, EDGC_ENOMEM, "norm scratch allocation failed");
+        if (need == 0) return EDGC_OK;
+        if (hipMalloc(reinterpret_cast<void**>(&ctx->norm.part), need * sizeof(float)) != hipSuccess) {
+            (void)hipGetLastError();
+            ctx->norm = NormScratch{};
+            return fail(ctx, EDGC_ENOMEM, "norm scratch allocation failed");
+        }
+        ctx->norm.held = need;
     }
     ctx->norm.tokens = tokens;
     ctx->norm.hidden = hidden;

@@ -124,6 +124,7 @@ struct BatchSlot {
 // Scratch of the block operators, of the sizes that edgc_reserve_block_norm has seen.
 struct NormScratch {
     float*   part = nullptr;        // [blocks][4][hidden] column sums of the backward pass
+    size_t   held = 0;              // elements of it: what the limits below need, or more
     uint32_t tokens = 0, hidden = 0;
 };
 
@@ -132,7 +133,7 @@ struct FfScratch {
     void*    ws = nullptr;          // operands, 16 bits each
     float*   part = nullptr;        // partial sums of products that are split along k
     unsigned int* tickets = nullptr;    // of blocks that share k, zero between calls
-    uint64_t elems = 0;
+    uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
 };
 
 // Kernel ids for the optional per-kernel event timing (edgc_profile_begin/end).

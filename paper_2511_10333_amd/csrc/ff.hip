@@ -457,14 +457,18 @@ extern "C" int edgc_reserve_ff(edgc_ctx* ctx, edgc_dtype dtype, uint32_t tokens,
     if (hidden == 0 || ff == 0 || hidden > kFfMaxWidth || ff > kFfMaxWidth || tokens > kFfMaxTokens)
         return fail(ctx, EDGC_EINVAL, "hidden and ff must be 1 to 2^20, tokens at most 2^21");
     EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    FfPlan plan(tokens, hidden, ff, dtype);
+    uint64_t elems = tokens ? plan.forward() : 0;
+    if (tokens && backward) elems = std::max(elems, plan.backward());
+    if (elems && elems <= ctx->ff.held) {
+        ctx->ff.elems = elems;
+        return EDGC_OK;
+    }
     EDGC_HIP_TRY(ctx, hipDeviceSynchronize());          // nothing may still be using the old scratch
     if (ctx->ff.ws) (void)hipFree(ctx->ff.ws);
     if (ctx->ff.part) (void)hipFree(ctx->ff.part);
     ctx->ff = FfScratch{};
-    if (tokens == 0) return EDGC_OK;
-    FfPlan plan(tokens, hidden, ff, dtype);
-    uint64_t elems = plan.forward();
-    if (backward) elems = std::max(elems, plan.backward());
+    if (elems == 0) return EDGC_OK;
     const uint64_t part_bytes = part_elems(ctx) * sizeof(float);
     bool ok = hipMalloc(&ctx->ff.ws, elems * 2) == hipSuccess;
     // the tickets lie behind the sums
@@ -478,7 +482,7 @@ extern "C" int edgc_reserve_ff(edgc_ctx* ctx, edgc_dtype dtype, uint32_t tokens,
         ctx->ff = FfScratch{};
         return fail(ctx, EDGC_ENOMEM, "feed-forward scratch allocation failed");
     }
-    ctx->ff.elems = elems;
+    ctx->ff.elems = ctx->ff.held = elems;
     return EDGC_OK;
 }
 
