@@ -556,8 +556,10 @@ int edgc_block_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, u
  * w_down: hidden x ff; all row-major of one dtype, with leading dimensions.
  * Sums are in fp32.  With EDGC_BF16, A, dG and dU are rounded to bf16 once, as
  * operands of the next product.  With EDGC_F32 operands are split into three
- * bf16 planes that add up to them exactly, and six products are summed: the
- * accuracy of fp32 products (an infinity may come out as NaN).
+ * bf16 planes that add up to them exactly, and six products of planes are
+ * summed (less than 2^-21 of a product is left out: the accuracy of fp32 sums;
+ * an infinity may come out as NaN), or, forward with up to 64 tokens, fp32
+ * products are.
  *   edgc_ff_forward: gate and up (both or neither) keep G and U for the
  *     backward pass.
  *   edgc_ff_backward: from the kept G and U; the weight gradients are

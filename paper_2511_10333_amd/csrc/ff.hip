@@ -168,7 +168,9 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     // dgate: where there are few tiles the join, whose blocks have a square of four waves each, gets through the long epilogue sooner
     // than the tile's four waves, and two workers a tile will do (841 tokens, 320 x 279, bf16: 14 us, one worker 31)
     if (EPI == kFfDgate && a.ksteps >= 2 && a.rest * 2 <= places) a.workers = std::max(a.workers, a.rest * 2);
-    // (a last round that is nearly full is not worth the sums' way through memory)
+    // (A last round that is nearly full is not worth the sums' way through memory.  The rule does not know k: where a tile has few steps the sums
+    // cost more than the sharing saves.  1888 tokens, 704 x 6026, bf16, projections: 11 steps, 128 of 384 tiles shared by 176 workers, joins
+    // 27 us in a pass whose products take 63 and 28.)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;
     constexpr uint32_t lds = lds_bytes(BM, BN);

@@ -15,8 +15,10 @@
 
 namespace edgc {
 
-// Measured, weights of 4096 x 16384 in bf16 and of 2048 x 8192 in fp32 call after call, these kernels / the products of ff_gemm.h: bf16, 32 tokens
-// 137 / 133 us, 24 125 / 133; fp32, 64 tokens 98 / 230 us.
+// Measured, weights from memory, these kernels / the products of ff_gemm.h, in us: bf16, 32 tokens, 1024 x 4096 18 / 35, 704 x 6026 29 / 45,
+// 2048 x 8192 41 / 49, 8192 x 2048 43 / 51, 4096 x 16384 133 / 121 (24 tokens 120 / 121), 5120 x 20480 278 / 171 (16 tokens 202 / 168);
+// fp32, 64 tokens, 997 x 2731 43 / 71, 2048 x 8192 113 / 225, 4096 x 16384 401 / 829.  The limit is right for matrices
+// of up to 2^24 elements; of larger ones in bf16 the two cross at fewer tokens (x is fetched again for every 16 rows), which it does not know.
 template <typename T> constexpr uint32_t kFfFewTokens = sizeof(T) == 4 ? 64 : 32;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
