@@ -400,18 +400,20 @@ def _check_u32(*sizes) -> None:
             raise ValueError("tokens and widths must be 0 or more and below 2^32")
 
 
-def _gradient_ld(t) -> int:
-    """Leading dimension of a gradient, a matrix of contiguous rows or a contiguous vector (one row)."""
-    if t.dim() == 1:
-        if t.numel() > 1 and t.stride(0) != 1:
-            raise ValueError("a gradient must have contiguous rows: this vector's elements are not adjacent")
-        return t.numel()
-    if t.dim() != 2:
+def _gradient_rows(t):
+    """Rows, columns and leading dimension of a gradient, a matrix of contiguous rows or a contiguous vector (one row)."""
+    shape, st = t.shape, t.stride()
+    if len(shape) == 2:
+        (m, n), (ld, step) = shape, st
+    elif len(shape) == 1:
+        m, n, ld, step = 1, shape[0], shape[0], st[0]
+    else:
         raise ValueError("a gradient must be a vector or a matrix")
-    ld, step = t.stride()
-    if t.shape[1] > 1 and step != 1:
-        raise ValueError("a gradient must have contiguous rows: this matrix's columns are not adjacent")
-    return ld
+    if step != 1 and n > 1:
+        raise ValueError("a gradient must have contiguous rows: the neighbours in a row of this one are not adjacent")
+    if m >> 32 or n >> 32:
+        raise ValueError("a gradient has fewer than 2^32 rows and columns: give a longer one in parts")
+    return m, n, ld
 
 
 class FeedForward:
@@ -650,30 +652,29 @@ class Context:
         if isinstance(tensors, PreparedBatch):
             return tensors.refresh(deferred)
         arr = (_Tensor * max(len(tensors), 1))()
-        code = None
+        code, dtype, deferred = F32, None, 1 if deferred else 0
         for i, t in enumerate(tensors):
-            g = t.grad if t.grad is not None else t.grad_out
-            m, n = (1, g.numel()) if g.dim() == 1 else g.shape
-            if m >> 32 or n >> 32:
-                raise ValueError("a gradient has fewer than 2^32 rows and columns: give a longer one in parts")
-            out = t.grad_out
-            if out is not None and out is not g and g.numel():      # (an empty one is the library's to refuse)
-                if out.dtype != g.dtype:
-                    raise TypeError("grad_out must be of its gradient's type")
-                if out.shape != g.shape and ((1, out.numel()) if out.dim() == 1 else tuple(out.shape)) != (m, n):
-                    raise ValueError("grad_out must be of its gradient's shape")
-            ld = lambda x: _gradient_ld(x) if x is not None else 0
-            ptr = lambda x: x.data_ptr() if x is not None else None
-            arr[i] = _Tensor(ptr(t.grad), ptr(t.grad_out), ptr(t.residual), ptr(t.Q), ptr(t.P),
-                             ld(t.grad), ld(t.grad_out), m, n,
-                             t.Q.shape[1] if t.Q is not None else 0,
-                             t.P.shape[1] if t.P is not None else 0,
-                             1 if t.residual_is_zero else 0, 1 if deferred else 0)
-            c = _dtype_code(g)
-            if code is not None and c != code:
-                raise TypeError("all gradients of a batch must have one dtype")
-            code = c
-        return arr, (code if code is not None else F32)
+            grad, out, residual, Q, P = t.grad, t.grad_out, t.residual, t.Q, t.P
+            g = out if grad is None else grad
+            m, n, ld = _gradient_rows(g)
+            if g.dtype is not dtype:
+                code = _dtype_code(g)
+                if dtype is not None:
+                    raise TypeError("all gradients of a batch must have one dtype")
+                dtype = g.dtype
+            ld_out = 0 if out is None else ld
+            if out is not None and out is not g:
+                mo, no, ld_out = _gradient_rows(out)
+                if m and n:                                         # (an empty one is the library's to refuse)
+                    if out.dtype is not dtype:
+                        raise TypeError("grad_out must be of its gradient's type")
+                    if mo != m or no != n:
+                        raise ValueError("grad_out must be of its gradient's shape")
+            arr[i] = _Tensor(None if grad is None else grad.data_ptr(), None if out is None else out.data_ptr(),
+                             None if residual is None else residual.data_ptr(), None if Q is None else Q.data_ptr(),
+                             None if P is None else P.data_ptr(), 0 if grad is None else ld, ld_out, m, n,
+                             0 if Q is None else Q.shape[1], 0 if P is None else P.shape[1], 1 if t.residual_is_zero else 0, deferred)
+        return arr, code
 
     def compress_batch(self, tensors: Sequence[Tensor], r: int, power_iters: int = 1, stream=None,
                        deferred: bool = False) -> None:
