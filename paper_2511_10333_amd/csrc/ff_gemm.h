@@ -102,7 +102,7 @@ __device__ __forceinline__ void ff_act(int act, float z, float& a, float& da)
     }
 }
 
-// x = p[0] + p[1] + p[2] in bf16, exactly (unless its last bits lie below the smallest number).  What is not finite is plane 0 alone.
+// x = p[0] + p[1] + p[2] in bf16, exactly (unless its last bits lie below bf16's smallest number: |x| under 2^-110).  What is not finite is plane 0 alone.
 __device__ __forceinline__ void ff_planes(float x, uint16_t (&p)[3])
 {
     const uint32_t u = __float_as_uint(x);
