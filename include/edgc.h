@@ -20,6 +20,8 @@
  *      global norm of the gradients and their clipping, the norms before and
  *      after a block fused with its gate and residual scale, and the gated
  *      feed-forward block, with their backward passes
+ *   7. what stands before and after the stack of blocks: the orthogonalised
+ *      update of the weights from a list of gradients
  *
  * Conventions
  *   - Every function returns an edgc_status (0 = OK, < 0 = error).  No C++
@@ -594,6 +596,42 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
                      uint64_t ldy, void* dx, uint64_t lddx, void* dw_gate, uint64_t ld_dgate,
                      void* dw_up, uint64_t ld_dup, void* dw_down, uint64_t ld_ddown,
                      int accumulate, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * 7. Before and after the stack of blocks.
+ *
+ * The orthogonalised update of a list of gradients (of the descriptors grad,
+ * ld, grad_out, ld_out, m and n are read): every matrix G by itself becomes
+ *     X = G / (|G|_F + eps);   `steps` times:  A = X X^T,
+ *     X <- a X + (b A + c A^2) X;   grad_out = round_dtype(scale X)
+ * With a, b, c = 3.4445, -4.7750, 2.0315 and five steps all singular values
+ * that are not tiny come out between 0.7 and 1.2.  A vector is a matrix of one
+ * row.  After a decompress and clipping, grad and grad_out are both the
+ * decompressed gradient (in place); otherwise no output overlaps an input.
+ * All products are on the smaller side of a matrix, of fp16 planes that hold 22
+ * bits of every operand (bf16 gradients: all of theirs), summed in fp32; the
+ * norm's squares and sums are in 64 bits.  A step's error counts twelve times
+ * more after every further step on A instead of on X, so X is formed again after
+ * three steps with EDGC_F32, five with EDGC_BF16.  The same list, reservation
+ * and GPU give the same bits.  A gradient of zeros stays zeros; one with Inf or
+ * NaN comes out as NaN throughout, and no other one with it.
+ *   edgc_reserve_orthogonalize: scratch for lists of tensors none of which needs
+ *     more than these do (not a hot call; smaller side s, larger l, rounded up to
+ *     multiples of 64: 20 s^2 + 4 s l bytes for a matrix, with EDGC_BF16
+ *     20 s^2 + 2 s l, and 4 s l more where X is formed again; up to twelve
+ *     matrices are worked on together, as many as the scratch holds).  What it
+ *     replaces, keeps and frees is as for edgc_reserve_block_norm; count = 0
+ *     frees alone.
+ *   edgc_orthogonalize_batch: scales: host, one per tensor, or NULL for 1.
+ * Errors: EDGC_EINVAL as for edgc_clip_batch, and for a smaller side over 2^14
+ * or a larger one over 2^20, steps 0 or over 64, an eps that is negative or not
+ * finite, a scale that is not finite, coefficients that let a matrix of a step grow
+ * beyond 1e9, and tensors over the reservation. */
+int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const uint32_t* rows,
+                               const uint32_t* cols, uint32_t count, uint32_t steps);
+int edgc_orthogonalize_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count,
+                             edgc_dtype dtype, uint32_t steps, double a, double b, double c,
+                             double eps, const float* scales, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -147,6 +147,11 @@ def load_library() -> C.CDLL:
     L.edgc_ff_forward.argtypes = [vp, C.POINTER(_FF), vp, u64, u32, vp, u64, vp, vp, u64, vp]
     L.edgc_ff_backward.restype = i32
     L.edgc_ff_backward.argtypes = [vp, C.POINTER(_FF), vp, u64, u32, vp, vp, u64, vp, u64, vp, u64, vp, u64, vp, u64, vp, u64, i32, vp]
+    f64 = C.c_double
+    L.edgc_reserve_orthogonalize.restype = i32
+    L.edgc_reserve_orthogonalize.argtypes = [vp, i32, C.POINTER(u32), C.POINTER(u32), u32, u32]
+    L.edgc_orthogonalize_batch.restype = i32
+    L.edgc_orthogonalize_batch.argtypes = [vp, C.POINTER(_Tensor), u32, i32, u32, f64, f64, f64, f64, vp, vp]
     _lib = L
     return L
 
@@ -509,7 +514,7 @@ class Context:
 
     def profile_end(self) -> dict:
         """Stops the timing; returns {kernel: dict(launches, total_ms, bytes, flops)}."""
-        cap = 32
+        cap = 64
         arr = (_KernelStat * cap)()
         n = C.c_uint32(0)
         self._check(self._L.edgc_profile_end(self._h, arr, cap, C.byref(n)), "edgc_profile_end")
@@ -830,3 +835,35 @@ class Context:
             _rows("dw_gate", dw_gate, dt, (ff.ff, ff.hidden)), dw_up.data_ptr(), _rows("dw_up", dw_up, dt, (ff.ff, ff.hidden)),
             dw_down.data_ptr(), _rows("dw_down", dw_down, dt, (ff.hidden, ff.ff)), 1 if accumulate else 0, _stream_handle(stream))
         self._check(rc, "edgc_ff_backward")
+
+    # -- before and after the stack of blocks --------------------------------------
+    @staticmethod
+    def _code_of(dtype) -> int:
+        if _torch is None:
+            _load_torch()
+        if dtype not in _codes:
+            raise TypeError("dtype must be float32 or bfloat16")
+        return _codes[dtype]
+
+    def reserve_orthogonalize(self, dtype, shapes: Sequence[Sequence[int]], steps: int = 5) -> None:
+        """edgc_reserve_orthogonalize: scratch of :meth:`orthogonalize_batch` for lists of matrices none of which is larger than
+        these, (rows, cols) each, in place of an earlier reservation (see :meth:`reserve_block_norm`)."""
+        n, code = len(shapes), self._code_of(dtype)
+        _check_u32(steps, *(d for s in shapes for d in s))
+        rows = (C.c_uint32 * max(n, 1))(*[s[0] for s in shapes])
+        cols = (C.c_uint32 * max(n, 1))(*[s[1] for s in shapes])
+        self._check(self._L.edgc_reserve_orthogonalize(self._h, code, rows, cols, n, steps), "edgc_reserve_orthogonalize")
+
+    def orthogonalize_batch(self, tensors: Sequence[Tensor], steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                            scales: Optional[Sequence[float]] = None, stream=None) -> None:
+        """edgc_orthogonalize_batch: ``grad_out`` = scale * (``steps`` Newton-Schulz steps of ``grad`` / its norm), each matrix by
+        itself; ``scales``: one per tensor."""
+        arr, code = self._gradients(tensors)
+        n = len(tensors)
+        if scales is not None and len(scales) != n:
+            raise ValueError("scales must be one per tensor")
+        _check_u32(steps)
+        a, b, c = coefficients
+        s = (C.c_float * max(n, 1))(*scales) if scales is not None else None
+        rc = self._L.edgc_orthogonalize_batch(self._h, arr, n, code, steps, a, b, c, eps, s, _stream_handle(stream))
+        self._check(rc, "edgc_orthogonalize_batch")

@@ -14,7 +14,7 @@ const char* const kKernelNames[KID_COUNT] = {
     "k_reduce_gram", "k_gram_sum", "k_chol", "k_apply", "k_pass_q", "k_reduce_q", "k_decompress",
     "k_pass_p_deferred", "k_wide_hist", "k_wide_reduce", "k_estimate_one", "k_grad_sumsq", "k_clip",
     "k_norm_forward", "k_norm_backward", "k_norm_sum", "k_ff_pack", "k_ff_gate", "k_ff_down", "k_ff_dgate", "k_ff_dx",
-    "k_ff_dw", "k_ff_join"};
+    "k_ff_dw", "k_ff_join", "k_ortho_sumsq", "k_ortho_pack", "k_ortho_gram", "k_ortho_chain", "k_ortho_apply"};
 }
 
 namespace {
@@ -215,6 +215,7 @@ extern "C" int edgc_destroy(edgc_ctx* ctx)
     free_batch(ctx);
     for (void* p : {static_cast<void*>(ctx->norm.part), ctx->ff.ws, static_cast<void*>(ctx->ff.part)})
         if (p) (void)hipFree(p);
+    free_ortho(ctx);
     free_scratch(ctx->s);
     delete ctx;
     return EDGC_OK;

@@ -136,13 +136,22 @@ struct FfScratch {
     uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
 };
 
+// Scratch of the orthogonalised update (edgc_reserve_orthogonalize).
+struct OrthoScratch {
+    void*    ws = nullptr;          // the matrices' planes, 16 bits an element
+    double*  part = nullptr;        // sums of squares per block
+    float*   f = nullptr;           // a matrix's factor (behind the sums)
+    uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
+};
+
 // Kernel ids for the optional per-kernel event timing (edgc_profile_begin/end).
 enum KernelId {
     KID_SET_RANGE = 0, KID_MINMAX, KID_HIST, KID_SAMPLE_IDX, KID_INIT_Q, KID_PASS_P,
     KID_REDUCE_GRAM, KID_GRAM_SUM, KID_CHOL, KID_APPLY, KID_PASS_Q, KID_REDUCE_Q, KID_DECOMPRESS,
     KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
     KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_FF_PACK,
-    KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_JOIN, KID_COUNT
+    KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_JOIN,
+    KID_ORTHO_SUMSQ, KID_ORTHO_PACK, KID_ORTHO_GRAM, KID_ORTHO_CHAIN, KID_ORTHO_APPLY, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 
@@ -191,6 +200,7 @@ struct edgc_ctx {
     std::vector<edgc::BatchSlot> batch;
     edgc::NormScratch norm;
     edgc::FfScratch ff;
+    edgc::OrthoScratch ortho;
     edgc::Profiler prof;
     std::string last_error;
 };
@@ -339,6 +349,9 @@ int launch_decompress(edgc_ctx* ctx, Group& g, CopyList& copies, edgc_dtype dt, 
 int prepare_compress_kernels(edgc_ctx* ctx);
 int prepare_entropy_kernels(edgc_ctx* ctx);
 int prepare_ff_kernels(edgc_ctx* ctx);          // ff.hip
+void free_ortho(edgc_ctx* ctx);                 // ortho.hip
+// what the calls that read a list's gradients (and write grad_out) ask of it (grad_norm.hip)
+int check_gradients(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out);
 size_t compress_part_elems(uint64_t max_rows, uint64_t max_cols, uint32_t max_rank, int num_cu);
 
 // the P-pass of groups made of whole tiles only (pass_p_full.hip)

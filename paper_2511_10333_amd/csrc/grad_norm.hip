@@ -216,23 +216,6 @@ __global__ __launch_bounds__(kThreads) void k_clip(const GradList list, const do
     }
 }
 
-int check_grads(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out)
-{
-    if (count && !tensors) return fail(ctx, EDGC_EINVAL, "null tensor list");
-    if (dtype != EDGC_F32 && dtype != EDGC_BF16) return fail(ctx, EDGC_EINVAL, "unknown dtype");
-    const uint32_t esz = dtype == EDGC_F32 ? 4 : 2;
-    for (uint32_t i = 0; i < count; ++i) {
-        const edgc_tensor& d = tensors[i];
-        if (d.m == 0 || d.n == 0) return fail(ctx, EDGC_EINVAL, "empty tensor in list");
-        if (!d.grad || (with_out && !d.grad_out)) return fail(ctx, EDGC_EINVAL, "null gradient pointer in list");
-        if (!aligned_to(d.grad, esz) || (with_out && !aligned_to(d.grad_out, esz))) return fail(ctx, EDGC_EINVAL, "gradient misaligned in list");
-        if (d.m > 1 && (d.ld < d.n || (with_out && d.ld_out < d.n))) return fail(ctx, EDGC_EINVAL, "leading dimension too small in list");
-        if (d.m > 1 && (d.ld > kMaxSpan || (with_out && d.ld_out > kMaxSpan))) return fail(ctx, EDGC_EINVAL, "leading dimension over 2^40");
-        if (with_out && d.grad == d.grad_out && d.m > 1 && d.ld != d.ld_out) return fail(ctx, EDGC_EINVAL, "a gradient clipped in place has one leading dimension");
-    }
-    return EDGC_OK;
-}
-
 // launches `go` over the list, at most kMaxGrads tensors at a time; go(list, blocks, first tensor of the launch, bytes read)
 template <typename F>
 int over_list(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out, F&& go)
@@ -262,6 +245,24 @@ int over_list(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dt
 }
 
 }  // namespace
+
+int check_gradients(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out)
+{
+    if (count && !tensors) return fail(ctx, EDGC_EINVAL, "null tensor list");
+    if (dtype != EDGC_F32 && dtype != EDGC_BF16) return fail(ctx, EDGC_EINVAL, "unknown dtype");
+    const uint32_t esz = dtype == EDGC_F32 ? 4 : 2;
+    for (uint32_t i = 0; i < count; ++i) {
+        const edgc_tensor& d = tensors[i];
+        if (d.m == 0 || d.n == 0) return fail(ctx, EDGC_EINVAL, "empty tensor in list");
+        if (!d.grad || (with_out && !d.grad_out)) return fail(ctx, EDGC_EINVAL, "null gradient pointer in list");
+        if (!aligned_to(d.grad, esz) || (with_out && !aligned_to(d.grad_out, esz))) return fail(ctx, EDGC_EINVAL, "gradient misaligned in list");
+        if (d.m > 1 && (d.ld < d.n || (with_out && d.ld_out < d.n))) return fail(ctx, EDGC_EINVAL, "leading dimension too small in list");
+        if (d.m > 1 && (d.ld > kMaxSpan || (with_out && d.ld_out > kMaxSpan))) return fail(ctx, EDGC_EINVAL, "leading dimension over 2^40");
+        if (with_out && d.grad == d.grad_out && d.m > 1 && d.ld != d.ld_out) return fail(ctx, EDGC_EINVAL, "a gradient that is written in place has one leading dimension");
+    }
+    return EDGC_OK;
+}
+
 }  // namespace edgc
 
 using namespace edgc;
@@ -270,7 +271,7 @@ extern "C" int edgc_grad_sumsq_batch(edgc_ctx* ctx, const edgc_tensor* tensors, 
                                      double* sumsq, void* hip_stream)
 {
     if (!ctx) return EDGC_EINVAL;
-    if (int rc = check_grads(ctx, tensors, count, dtype, false)) return rc;
+    if (int rc = check_gradients(ctx, tensors, count, dtype, false)) return rc;
     if (sumsq && !aligned_to(sumsq, 8)) return fail(ctx, EDGC_EINVAL, "sumsq misaligned");
     double* const to = sumsq ? sumsq : ctx->s.sumsq;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -298,7 +299,7 @@ extern "C" int edgc_clip_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32
                                const double* sumsq, float* norm_coef, void* hip_stream)
 {
     if (!ctx) return EDGC_EINVAL;
-    if (int rc = check_grads(ctx, tensors, count, dtype, true)) return rc;
+    if (int rc = check_gradients(ctx, tensors, count, dtype, true)) return rc;
     if (!(max_norm > 0.0) || !std::isfinite(max_norm)) return fail(ctx, EDGC_EINVAL, "max_norm must be positive and finite");
     if (sumsq && !aligned_to(sumsq, 8)) return fail(ctx, EDGC_EINVAL, "sumsq misaligned");
     if (norm_coef && !aligned_to(norm_coef, 4)) return fail(ctx, EDGC_EINVAL, "norm_coef misaligned");

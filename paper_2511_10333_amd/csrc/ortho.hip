@@ -1,0 +1,521 @@
+// The orthogonalised update of a list of gradients: Newton-Schulz steps of the normalised matrix, on its smaller side.
+//
+//   X = G / (|G| + eps), s x l, s <= l (a tall matrix is transposed);  steps times:  A = X X^T,  W = a I + b A + c A^2,  X <- W X;  out = scale X
+//
+// All matrices on the smaller side are polynomials of the same A: they commute and are symmetric.  So a segment of steps needs X twice only,
+//
+//   A_0 = X X^T,  W_k = a I + b A_k + c A_k^2,  V_k = W_k A_k,  A_k+1 = V_k W_k,  Q_k+1 = W_k Q_k (Q_0 = I),  X <- Q X,
+//
+// and of the symmetric products half the tiles are made: of s^3 operations 4 a step, instead of 3 l / s + 1 in every step as written above.  A_k+1 by
+// products instead of from X carries its rounding errors on, a^2 = 12 times larger relative to the small singular values with each step, so segments are
+// bounded (kSegment).  Operands are fp16 planes (ortho_gemm.h); every sum is in fp32.
+#include "ortho_gemm.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace edgc {
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// the gradient's norm, and the gradient as planes
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kOrthoGroup = 12, kOrthoParts = 1024;    // matrices of a launch; blocks that one is spread over
+struct OrthoItem {
+    const void* src;
+    uint16_t* x;                        // planes, rows of ldx
+    double* part;                       // per block
+    float* f;
+    uint64_t ld, ldx;
+    uint32_t m, n, tiles_c, tiles, first, blocks, tall, _pad;
+};
+struct OrthoList {
+    OrthoItem t[kOrthoGroup];
+    uint32_t count, blocks;
+    double eps;
+};
+__device__ __forceinline__ const OrthoItem& ortho_item_of(const OrthoList& list)
+{
+    uint32_t k = 0;
+    while (k + 1 < list.count && blockIdx.x >= list.t[k + 1].first) ++k;
+    return list.t[k];
+}
+// Eight neighbours of row r of a tile of 64 x 64
+template <typename T>
+__device__ __forceinline__ void ortho_load8(const OrthoItem& t, uint32_t tile, uint32_t half, float (&v)[8])
+{
+    const uint32_t r = tile / t.tiles_c * 64 + half * 32 + threadIdx.x / 8, c = tile % t.tiles_c * 64 + threadIdx.x % 8 * 8;
+    if (r >= t.m) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        return;
+    }
+    const T* const row = static_cast<const T*>(t.src) + r * t.ld;
+    float a[4], b[4];
+    ff_load4<T, false>(row, c, t.n, a);
+    ff_load4<T, false>(row, c + 4, t.n, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+__device__ __forceinline__ double ortho_block_sum(double v)
+{
+    __shared__ double s[4];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+// Squares and sums in 64 bits, in a fixed order
+template <typename T>
+__global__ __launch_bounds__(256) void k_ortho_sumsq(const OrthoList list)
+{
+    const OrthoItem& t = ortho_item_of(list);
+    const uint32_t at = blockIdx.x - t.first;
+    double acc = 0.0;
+    for (uint32_t tile = at; tile < t.tiles; tile += t.blocks)
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) {
+            float v[8];
+            ortho_load8<T>(t, tile, half, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc = __builtin_fma(static_cast<double>(v[i]), static_cast<double>(v[i]), acc);
+        }
+    acc = ortho_block_sum(acc);
+    if (threadIdx.x == 0) t.part[at] = acc;
+}
+// X = f 2^k G: 2^k G, whose norm is in [2^14, 2^15), as planes (P of them), f = 1 / ((norm + eps) 2^k) beside them.  Of a gradient that has a value
+// that is not finite f is NaN, and so is the whole update.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
+{
+    __shared__ float turn[64 * 65];
+    const OrthoItem& t = ortho_item_of(list);
+    const uint32_t at = blockIdx.x - t.first;
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < t.blocks; i += 256) sum += t.part[i];
+    const double norm = sqrt(ortho_block_sum(sum));
+    int k = 0;
+    if (norm > 0.0 && norm < 1e300) {
+        (void)frexp(norm, &k);
+        k = 15 - k;
+    }
+    if (at == 0 && threadIdx.x == 0) *t.f = norm < 1e300 ? (norm > 0.0 ? static_cast<float>(ldexp(1.0 / (norm + list.eps), -k)) : 0.f) : __builtin_nanf("");
+    auto put = [&](uint32_t row, uint32_t col, float (&v)[8]) {         // of X
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], k);
+        u32x4 hi, lo;
+        ortho_planes(v, hi, lo);
+        uint16_t* const to = t.x + row * t.ldx + (P == 2 ? ortho_at(col) : col);
+        *reinterpret_cast<u32x4*>(to) = hi;
+        if constexpr (P == 2) *reinterpret_cast<u32x4*>(to + 32) = lo;
+    };
+    const uint32_t row = threadIdx.x / 8, col = threadIdx.x % 8 * 8;
+    for (uint32_t tile = at; tile < t.tiles; tile += t.blocks) {
+        const uint32_t r0 = tile / t.tiles_c * 64, c0 = tile % t.tiles_c * 64;
+        float v[2][8];
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) ortho_load8<T>(t, tile, half, v[half]);
+        if (!t.tall) {
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) put(r0 + half * 32 + row, c0 + col, v[half]);
+            continue;
+        }
+        __syncthreads();                // the last tile's reads are done
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turn[(half * 32 + row) * 65 + col + i] = v[half][i];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[half][i] = turn[(col + i) * 65 + half * 32 + row];
+            put(c0 + half * 32 + row, r0 + col, v[half]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kOrthoMaxSide = 1u << 14, kOrthoMaxLong = 1u << 20, kOrthoMaxSteps = 64;
+// Steps of a segment at most.  The rounding errors of A_0, 2^-24 of its largest value, are 12^(n - 1) times larger in A_n-1 relative to what comes of the
+// smallest singular values, 2 / sqrt s of that in the norm: with 3 steps they stay below the fp32 sums' own, with 5 below 1e-4, an eighth of what bf16
+// rounds.
+constexpr uint32_t segment_steps(edgc_dtype dt) { return dt == EDGC_F32 ? 3 : 5; }
+
+uint64_t pad64(uint64_t n) { return (n + 63) / 64 * 64; }
+
+struct OrthoShape {
+    uint64_t s, l, S, L;                // the smaller and the larger side, padded
+    bool tall;
+    OrthoShape() = default;
+    OrthoShape(uint64_t m, uint64_t n) : s(std::min(m, n)), l(std::max(m, n)), S(pad64(s)), L(pad64(l)), tall(m > n) {}
+    // 16-bit elements: X, the X of a later segment, five matrices of the smaller side
+    uint64_t x_elems(uint32_t planes) const { return S * L * planes; }
+    uint64_t side_elems() const { return S * S * 2; }
+    uint64_t elems(edgc_dtype dt, uint32_t segments) const
+    {
+        return x_elems(first_planes(dt, segments)) + (segments > 1 ? x_elems(2) : 0) + 5 * side_elems();
+    }
+    // (with three segments the second X comes where the first one was)
+    static uint32_t first_planes(edgc_dtype dt, uint32_t segments) { return dt == EDGC_F32 || segments > 2 ? 2 : 1; }
+    uint64_t tiles() const { const uint64_t t = (s + 255) / 256; return t * (t + 1) / 2; }
+};
+uint32_t segments_of(edgc_dtype dt, uint32_t steps) { return (steps + segment_steps(dt) - 1) / segment_steps(dt); }
+
+// Matrices i, i + 1, .. that are worked on together: as many as give the smaller side's products a few rounds of tiles, and fit
+template <typename F>
+uint32_t ortho_group(const edgc_ctx* ctx, edgc_dtype dt, uint32_t segments, uint32_t i, uint32_t count, uint64_t held, F&& shape_of, uint64_t* used)
+{
+    uint64_t elems = 0, tiles = 0;
+    uint32_t k = 0;
+    for (; i + k < count && k < kOrthoGroup; ++k) {
+        const OrthoShape sh = shape_of(i + k);
+        const uint64_t e = sh.elems(dt, segments);
+        if (k && (e > held - elems || tiles >= 4ull * ctx->num_cu)) break;
+        elems += e;
+        tiles += sh.tiles();
+    }
+    if (used) *used = elems;
+    return k;
+}
+
+// Powers of two that the matrices of a step are scaled by, so that none of their entries passes 2^15: an entry of a symmetric matrix is at
+// most its largest eigenvalue, a polynomial's largest value over the singular values that there can be.
+struct OrthoScale {
+    static int of(double most) { int e; (void)std::frexp(std::max(most * 1.1, 1e-6), &e); return 15 - e; }
+};
+
+struct OrthoCoefs {
+    double a, b, c;
+    // the largest |p0 + p1 u + p2 u^2| u^power over [0, top], of which the derivative's quadratic is d0 + d1 u + d2 u^2
+    double most_of(double top, double power, double d0, double d1, double d2) const
+    {
+        double best = 0.0;
+        auto look = [&](double u) {
+            if (u >= 0.0 && u <= top) best = std::max(best, std::fabs(a + u * (b + u * c)) * std::pow(u, power));
+        };
+        look(0.0);
+        look(top);
+        if (d2 == 0.0) {
+            if (d1 != 0.0) look(-d0 / d1);
+        } else if (const double disc = d1 * d1 - 4.0 * d2 * d0; disc >= 0.0) {
+            look((-d1 + std::sqrt(disc)) / (2.0 * d2));
+            look((-d1 - std::sqrt(disc)) / (2.0 * d2));
+        }
+        return best;
+    }
+    // the largest values of W, W A and W s over singular values s up to `top`: of a + b u + c u^2 and its products with u and sqrt u, u = s^2
+    void most(double top, double& w_top, double& v_top, double& s_top) const
+    {
+        const double u = top * top;
+        w_top = most_of(u, 0.0, b, 2.0 * c, 0.0);
+        v_top = most_of(u, 1.0, a, 2.0 * b, 3.0 * c);
+        s_top = most_of(u, 0.5, a, 3.0 * b, 5.0 * c);
+    }
+};
+constexpr double kOrthoMost = 1e9;      // beyond this the steps diverge
+
+// whether `steps` of them keep every matrix representable
+bool coefs_bounded(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps)
+{
+    double top = 1.0, q = 1.0;
+    const uint32_t segments = segments_of(dt, steps);
+    for (uint32_t seg = 0, done = 0; seg < segments; ++seg) {
+        q = 1.0;
+        for (const uint32_t end = steps * (seg + 1) / segments; done < end; ++done) {
+            double w, v, s;
+            co.most(top, w, v, s);
+            q *= w;
+            if (!(w <= kOrthoMost && v <= kOrthoMost && s <= kOrthoMost && s * s <= kOrthoMost && q <= kOrthoMost)) return false;
+            top = s;
+        }
+    }
+    return true;
+}
+
+struct OrthoPass {
+    edgc_ctx* ctx;
+    hipStream_t st;
+    edgc_dtype dt;
+    const edgc_tensor* tensors;
+    const float* scales;
+    uint32_t count, segments, steps;
+    double eps;
+    OrthoCoefs co;
+    struct Mat {
+        OrthoShape sh;
+        uint16_t *x[2], *a, *v, *w[3];
+        float* f;
+    };
+    Mat mats[kOrthoGroup] = {};
+    uint32_t n = 0;                             // of them
+
+    template <int BM, int PA, int PB, bool TB, typename T>
+    int launch(OrthoArgs& args, int kid)
+    {
+        uint32_t tiles = 0;
+        double flops = 0.0, bytes = 0.0;
+        for (uint32_t i = 0; i < args.count; ++i) {
+            OrthoProblem& p = args.p[i];
+            p.tiles_m = (p.M + BM - 1) / BM;
+            p.tiles_n = (p.N + BM - 1) / BM;
+            p.first = tiles;
+            tiles += TB ? p.tiles_m * p.tiles_n : p.tiles_m * (p.tiles_m + 1) / 2;
+            const double k = p.steps * (PA == 1 ? 64.0 : 32.0);
+            flops += (TB ? 2.0 : 1.0) * p.M * p.N * k * (PA + PB - 1);
+            bytes += 2.0 * k * (static_cast<double>(p.M) * PA + static_cast<double>(p.N) * PB);
+        }
+        args.tiles = tiles;
+        EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ortho_gemm<BM, PA, PB, TB, T><<<tiles, 256, kOrthoLds<BM, PA, PB, TB>, st>>>(args));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        return EDGC_OK;
+    }
+    template <int PA, int PB, bool TB, typename T>
+    int product(OrthoArgs& args, int kid)
+    {
+        return launch<128, PA, PB, TB, T>(args, kid);
+    }
+    // a product of two matrices of the smaller side, or the first of a segment
+    static OrthoProblem symmetric(const Mat& m, const uint16_t* a, const uint16_t* b, uint16_t* out, double alpha)
+    {
+        OrthoProblem p{};
+        p.a = a; p.b = b; p.out = out;
+        p.lda = p.ldb = p.ldo = static_cast<uint32_t>(2 * m.sh.S);
+        p.M = p.N = static_cast<uint32_t>(m.sh.s);
+        p.rows = p.cols = static_cast<uint32_t>(m.sh.S);
+        p.steps = static_cast<uint32_t>(m.sh.S / 32);
+        p.alpha = static_cast<float>(alpha);
+        return p;
+    }
+
+    int group(uint32_t i0, uint32_t many)
+    {
+        place(i0, many);
+        if (int rc = dt == EDGC_F32 ? pack<float>(i0) : pack<__bf16>(i0)) return rc;
+        double top = 1.0;
+        int x_scale = 0;                        // of X; the first one's is in f
+        for (uint32_t seg = 0, done = 0; seg < segments; ++seg) {
+            const uint32_t end = steps * (seg + 1) / segments, from = seg % 2;
+            const bool first = seg == 0, single = first && OrthoShape::first_planes(dt, segments) == 1;
+            // A = X X^T
+            int a_scale = OrthoScale::of(top * top), q_scale = 0;
+            {
+                OrthoArgs g{};
+                for (const Mat& m : these()) {
+                    OrthoProblem p = symmetric(m, m.x[from], m.x[from], m.a, std::ldexp(1.0, a_scale - (first ? 0 : 2 * x_scale)));
+                    p.lda = p.ldb = static_cast<uint32_t>(m.sh.L * (single ? 1 : 2));
+                    p.steps = static_cast<uint32_t>(m.sh.L / (single ? 64 : 32));
+                    if (first) p.f = m.f, p.power = 2;
+                    g.p[g.count++] = p;
+                }
+                if (int rc = single ? product<1, 1, false, void>(g, KID_ORTHO_GRAM) : product<2, 2, false, void>(g, KID_ORTHO_GRAM)) return rc;
+            }
+            double q = 1.0;
+            uint32_t at_q = 0;                  // which of w[] holds Q
+            for (bool begin = true; done < end; ++done, begin = false) {
+                const bool last = done + 1 == end;
+                double w_top, v_top, s_top;
+                co.most(top, w_top, v_top, s_top);
+                q *= w_top;
+                const int w_scale = OrthoScale::of(w_top), v_scale = OrthoScale::of(v_top), next_a = OrthoScale::of(s_top * s_top), next_q = OrthoScale::of(q);
+                const uint32_t at_w = begin ? 0 : (at_q + 1) % 3, at_new = (at_q + 2) % 3;
+                OrthoArgs g{};
+                for (const Mat& m : these()) {     // W
+                    OrthoProblem p = symmetric(m, m.a, m.a, m.w[at_w], std::ldexp(co.c, w_scale - 2 * a_scale));
+                    p.e = m.a;
+                    p.beta = static_cast<float>(std::ldexp(co.b, w_scale - a_scale));
+                    p.gamma = static_cast<float>(std::ldexp(co.a, w_scale));
+                    g.p[g.count++] = p;
+                }
+                if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                g = OrthoArgs{};
+                for (const Mat& m : these()) {     // V, and the next Q
+                    if (!last) g.p[g.count++] = symmetric(m, m.w[at_w], m.a, m.v, std::ldexp(1.0, v_scale - w_scale - a_scale));
+                    if (!begin) g.p[g.count++] = symmetric(m, m.w[at_w], m.w[at_q], m.w[at_new], std::ldexp(1.0, next_q - w_scale - q_scale));
+                }
+                if (g.count)
+                    if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                if (!last) {                    // the next A
+                    g = OrthoArgs{};
+                    for (const Mat& m : these()) g.p[g.count++] = symmetric(m, m.v, m.w[at_w], m.a, std::ldexp(1.0, next_a - v_scale - w_scale));
+                    if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                }
+                a_scale = next_a;
+                q_scale = begin ? w_scale : next_q;
+                at_q = begin ? 0 : at_new;
+                top = s_top;
+            }
+            // X <- Q X
+            const bool out = seg + 1 == segments;
+            const int next_x = OrthoScale::of(top);
+            OrthoArgs g{};
+            for (uint32_t i = 0; i < n; ++i) {
+                const Mat& m = mats[i];
+                const edgc_tensor& d = tensors[i0 + i];
+                OrthoProblem p{};
+                p.a = m.w[at_q]; p.b = m.x[from];
+                p.lda = static_cast<uint32_t>(2 * m.sh.S);
+                p.ldb = p.b_cols = static_cast<uint32_t>(m.sh.L * (single ? 1 : 2));
+                p.M = static_cast<uint32_t>(m.sh.s); p.N = static_cast<uint32_t>(m.sh.l);
+                p.steps = static_cast<uint32_t>(m.sh.S / 32);
+                const double scale = out ? (scales ? scales[i0 + i] : 1.0) : std::ldexp(1.0, next_x);
+                p.alpha = static_cast<float>(std::ldexp(scale, -q_scale - (first ? 0 : x_scale)));
+                if (first) p.f = m.f, p.power = 1;
+                if (out) {
+                    p.to = d.grad_out; p.ldto = d.ld_out; p.transposed = m.sh.tall;
+                } else {
+                    p.out = m.x[1 - from]; p.ldo = static_cast<uint32_t>(2 * m.sh.L);
+                    p.rows = static_cast<uint32_t>(m.sh.S); p.cols = static_cast<uint32_t>(m.sh.L);
+                }
+                g.p[g.count++] = p;
+            }
+            if (int rc = apply(g, single, out)) return rc;
+            x_scale = next_x;
+        }
+        return EDGC_OK;
+    }
+    int apply(OrthoArgs& g, bool single, bool out)
+    {
+        if (!out) return single ? product<2, 1, true, void>(g, KID_ORTHO_APPLY) : product<2, 2, true, void>(g, KID_ORTHO_APPLY);
+        if (dt == EDGC_F32) return product<2, 2, true, float>(g, KID_ORTHO_APPLY);
+        return single ? product<2, 1, true, __bf16>(g, KID_ORTHO_APPLY) : product<2, 2, true, __bf16>(g, KID_ORTHO_APPLY);
+    }
+
+    struct Some {
+        const Mat *from, *to;
+        const Mat* begin() const { return from; }
+        const Mat* end() const { return to; }
+    };
+    Some these() const { return {mats, mats + n}; }
+
+    void place(uint32_t i0, uint32_t many)
+    {
+        n = many;
+        uint16_t* at = static_cast<uint16_t*>(ctx->ortho.ws);
+        auto take = [&](uint64_t elems) { uint16_t* const p = at; at += elems; return p; };
+        for (uint32_t i = 0; i < n; ++i) {
+            Mat m{OrthoShape(tensors[i0 + i].m, tensors[i0 + i].n), {}, nullptr, nullptr, {}, nullptr};
+            m.x[0] = take(m.sh.x_elems(OrthoShape::first_planes(dt, segments)));
+            m.x[1] = segments > 1 ? take(m.sh.x_elems(2)) : nullptr;
+            m.a = take(m.sh.side_elems());
+            m.v = take(m.sh.side_elems());
+            for (uint16_t*& w : m.w) w = take(m.sh.side_elems());
+            m.f = ctx->ortho.f + i;
+            mats[i] = m;
+        }
+    }
+    template <typename T>
+    int pack(uint32_t i0)
+    {
+        OrthoList list{};
+        list.eps = eps;
+        const uint32_t planes = OrthoShape::first_planes(dt, segments);
+        double elems = 0.0;
+        for (uint32_t i = 0; i < n; ++i) {
+            const edgc_tensor& d = tensors[i0 + i];
+            OrthoItem& t = list.t[list.count++];
+            t.src = d.grad; t.ld = d.ld; t.m = d.m; t.n = d.n;
+            t.x = mats[i].x[0]; t.ldx = mats[i].sh.L * planes; t.tall = mats[i].sh.tall;
+            t.part = ctx->ortho.part + static_cast<size_t>(i) * kOrthoParts; t.f = mats[i].f;
+            t.tiles_c = (d.n + 63) / 64;
+            t.tiles = t.tiles_c * ((d.m + 63) / 64);
+            t.first = list.blocks;
+            t.blocks = std::min(t.tiles, kOrthoParts);
+            list.blocks += t.blocks;
+            elems += static_cast<double>(d.m) * d.n;
+        }
+        EDGC_LAUNCH(ctx, st, KID_ORTHO_SUMSQ, elems * sizeof(T), 0.0, k_ortho_sumsq<T><<<list.blocks, 256, 0, st>>>(list));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        if (planes == 2) EDGC_LAUNCH(ctx, st, KID_ORTHO_PACK, elems * (sizeof(T) + 4.0), 0.0, k_ortho_pack<T, 2><<<list.blocks, 256, 0, st>>>(list));
+        else EDGC_LAUNCH(ctx, st, KID_ORTHO_PACK, elems * (sizeof(T) + 2.0), 0.0, k_ortho_pack<T, 1><<<list.blocks, 256, 0, st>>>(list));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        return EDGC_OK;
+    }
+};
+
+int check_shape(edgc_ctx* ctx, uint64_t m, uint64_t n)
+{
+    if (m == 0 || n == 0) return fail(ctx, EDGC_EINVAL, "empty tensor in list");
+    if (std::min(m, n) > kOrthoMaxSide || std::max(m, n) > kOrthoMaxLong)
+        return fail(ctx, EDGC_EINVAL, "the smaller side of a matrix is at most 2^14, the larger 2^20");
+    return EDGC_OK;
+}
+
+}  // namespace
+
+void free_ortho(edgc_ctx* ctx)
+{
+    if (ctx->ortho.ws) (void)hipFree(ctx->ortho.ws);
+    if (ctx->ortho.part) (void)hipFree(ctx->ortho.part);
+    ctx->ortho = OrthoScratch{};
+}
+
+}  // namespace edgc
+
+using namespace edgc;
+
+extern "C" int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const uint32_t* rows, const uint32_t* cols, uint32_t count, uint32_t steps)
+{
+    if (!ctx) return EDGC_EINVAL;
+    if (dtype != EDGC_F32 && dtype != EDGC_BF16) return fail(ctx, EDGC_EINVAL, "unknown dtype");
+    if (count && (!rows || !cols)) return fail(ctx, EDGC_EINVAL, "null list of shapes");
+    if (count && (steps == 0 || steps > kOrthoMaxSteps)) return fail(ctx, EDGC_EINVAL, "steps must be 1 to 64");
+    for (uint32_t i = 0; i < count; ++i)
+        if (int rc = check_shape(ctx, rows[i], cols[i])) return rc;
+    EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    const uint32_t segments = count ? segments_of(dtype, steps) : 0;
+    uint64_t need = 0;
+    for (uint32_t i = 0; i < count;) {
+        uint64_t used = 0;
+        i += ortho_group(ctx, dtype, segments, i, count, ~0ull, [&](uint32_t k) { return OrthoShape(rows[k], cols[k]); }, &used);
+        need = std::max(need, used);
+    }
+    if (need && need <= ctx->ortho.held) {
+        ctx->ortho.elems = need;
+        return EDGC_OK;
+    }
+    EDGC_HIP_TRY(ctx, hipDeviceSynchronize());          // nothing may still be using the old scratch
+    free_ortho(ctx);
+    if (need == 0) return EDGC_OK;
+    const size_t parts = static_cast<size_t>(kOrthoGroup) * kOrthoParts;
+    bool ok = hipMalloc(&ctx->ortho.ws, need * 2) == hipSuccess;
+    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.part), parts * sizeof(double) + kOrthoGroup * sizeof(float)) == hipSuccess;
+    if (!ok) {
+        (void)hipGetLastError();
+        free_ortho(ctx);
+        return fail(ctx, EDGC_ENOMEM, "scratch allocation of the orthogonalised update failed");
+    }
+    ctx->ortho.f = reinterpret_cast<float*>(ctx->ortho.part + parts);
+    ctx->ortho.elems = ctx->ortho.held = need;
+    return EDGC_OK;
+}
+
+extern "C" int edgc_orthogonalize_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, uint32_t steps, double a, double b,
+                                        double c, double eps, const float* scales, void* hip_stream)
+{
+    if (!ctx) return EDGC_EINVAL;
+    if (int rc = check_gradients(ctx, tensors, count, dtype, true)) return rc;
+    if (steps == 0 || steps > kOrthoMaxSteps) return fail(ctx, EDGC_EINVAL, "steps must be 1 to 64");
+    if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(ctx, EDGC_EINVAL, "eps must be finite and not negative");
+    const OrthoCoefs co{a, b, c};
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c) || !coefs_bounded(co, dtype, steps))
+        return fail(ctx, EDGC_EINVAL, "coefficients must be finite, and so that the steps keep singular values bounded");
+    const uint32_t segments = segments_of(dtype, steps);
+    for (uint32_t i = 0; i < count; ++i) {
+        if (int rc = check_shape(ctx, tensors[i].m, tensors[i].n)) return rc;
+        if (scales && !std::isfinite(scales[i])) return fail(ctx, EDGC_EINVAL, "scales must be finite");
+        if (OrthoShape(tensors[i].m, tensors[i].n).elems(dtype, segments) > ctx->ortho.elems)
+            return fail(ctx, EDGC_EINVAL, "larger than what edgc_reserve_orthogonalize was called for");
+    }
+    EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    OrthoPass pass{ctx, static_cast<hipStream_t>(hip_stream), dtype, tensors, scales, count, segments, steps, eps, co};
+    for (uint32_t i = 0; i < count;) {
+        const uint32_t n = ortho_group(ctx, dtype, segments, i, count, ctx->ortho.elems, [&](uint32_t k) { return OrthoShape(tensors[k].m, tensors[k].n); }, nullptr);
+        if (int rc = pass.group(i, n)) return rc;
+        i += n;
+    }
+    return EDGC_OK;
+}
