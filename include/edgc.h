@@ -618,7 +618,7 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
  *   edgc_reserve_orthogonalize: scratch for lists of tensors none of which needs
  *     more than these do (not a hot call; smaller side s, larger l, rounded up to
  *     multiples of 64: 20 s^2 + 4 s l bytes for a matrix, with EDGC_BF16
- *     20 s^2 + 2 s l, and 4 s l more where X is formed again; up to twelve
+ *     20 s^2 + 2 s l, and 4 s l more where X is formed again; up to ten
  *     matrices are worked on together, as many as the scratch holds).  What it
  *     replaces, keeps and frees is as for edgc_reserve_block_norm; count = 0
  *     frees alone.

@@ -139,6 +139,7 @@ struct FfScratch {
 // Scratch of the orthogonalised update (edgc_reserve_orthogonalize).
 struct OrthoScratch {
     void*    ws = nullptr;          // the matrices' planes, 16 bits an element
+    float*   sums = nullptr;        // partial sums of tiles whose k is shared
     double*  part = nullptr;        // sums of squares per block
     float*   f = nullptr;           // a matrix's factor (behind the sums)
     uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
@@ -151,7 +152,7 @@ enum KernelId {
     KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
     KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_FF_PACK,
     KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_JOIN,
-    KID_ORTHO_SUMSQ, KID_ORTHO_PACK, KID_ORTHO_GRAM, KID_ORTHO_CHAIN, KID_ORTHO_APPLY, KID_COUNT
+    KID_ORTHO_SUMSQ, KID_ORTHO_PACK, KID_ORTHO_GRAM, KID_ORTHO_CHAIN, KID_ORTHO_APPLY, KID_ORTHO_JOIN, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 
@@ -349,7 +350,8 @@ int launch_decompress(edgc_ctx* ctx, Group& g, CopyList& copies, edgc_dtype dt, 
 int prepare_compress_kernels(edgc_ctx* ctx);
 int prepare_entropy_kernels(edgc_ctx* ctx);
 int prepare_ff_kernels(edgc_ctx* ctx);          // ff.hip
-void free_ortho(edgc_ctx* ctx);                 // ortho.hip
+int prepare_ortho_kernels(edgc_ctx* ctx);       // ortho.hip
+void free_ortho(edgc_ctx* ctx);
 // what the calls that read a list's gradients (and write grad_out) ask of it (grad_norm.hip)
 int check_gradients(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out);
 size_t compress_part_elems(uint64_t max_rows, uint64_t max_cols, uint32_t max_rank, int num_cu);
