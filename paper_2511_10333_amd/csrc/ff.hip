@@ -138,8 +138,9 @@ struct Packer {
     }
 };
 
-// blocks that share a compute unit's LDS
-constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / ff_lds_bytes(bm, bn); }
+// LDS of a tile shape: two buffers, of A three where there is room; blocks that share a compute unit's
+constexpr uint32_t lds_bytes(int bm, int bn) { return ((bm == 256 ? 3u : 2u) * bm + 2u * bn) * 128u; }
+constexpr uint32_t blocks_per_cu(int bm, int bn) { return 160u * 1024u / lds_bytes(bm, bn); }
 // The least k that is worth a worker, which then writes a tile's sums and has them read again
 constexpr uint64_t kMinK = 512;
 
@@ -172,7 +173,7 @@ int launch_tiles(edgc_ctx* ctx, FfArgs& a, int kid, hipStream_t st)
     // 27 us in a pass whose products take 63 and 28.)
     if (a.workers <= a.rest || a.rest * 10ull > places * 9ull) a.whole = tiles, a.rest = a.workers = 0;
     a.part = ctx->ff.part;
-    constexpr uint32_t lds = ff_lds_bytes(BM, BN);
+    constexpr uint32_t lds = lds_bytes(BM, BN);
     EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ff_gemm<BM, BN, TA, TB, T, EPI><<<a.whole + a.workers, 256, lds, st>>>(a));
     EDGC_HIP_TRY(ctx, hipGetLastError());
     if (a.rest) {
@@ -212,7 +213,7 @@ hipError_t prepare_tiles()
                           reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, true, true, T, kFfStore>),
                           reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, false, T, kFfGate>),
                           reinterpret_cast<const void*>(&k_ff_gemm<BM, BN, false, true, T, kFfDgate>)})
-        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, ff_lds_bytes(BM, BN))) return e;
+        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(BM, BN))) return e;
     return hipSuccess;
 }
 

@@ -411,165 +411,17 @@ struct FfFragments {
 template <bool GATED, int NI>
 __device__ __forceinline__ uint32_t ff_column(uint32_t row) { return GATED ? row / (NI * 32) * (NI * 16) + row % (NI * 16) : row; }
 
-// LDS of a tile shape: two buffers, of A three where there is room
-constexpr uint32_t ff_lds_bytes(int bm, int bn) { return ((bm == 256 ? 3u : 2u) * bm + 2u * bn) * 128u; }
-
-template <bool F16>
-__device__ __forceinline__ f32x16 ff_mfma(const bf16x8& a, const bf16x8& b, const f32x16& c)
-{
-    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-
-// the second matrix of the gated form, or the first
-template <bool GATED, typename P>
-__device__ __forceinline__ const uint16_t* ff_second(const P& p, uint32_t seg, uint64_t at, const uint16_t* first)
-{
-    if constexpr (GATED) return p.b2[seg] + at;
-    else return first;
-}
-
-// The sums of a tile over tiles kt0 to kt1 of 64 k, counted through the segments, in `acc`: of a wave, MI x NI squares of 32 x 32.
-// P: FfProblem, or what has its a, b, lda, ldb, M, N, ktiles and nseg (GATED: b2).  F16: the operands are fp16.
-template <int BM, int BN, bool TA, bool TB, bool GATED, bool F16, typename P>
-__device__ __forceinline__ void ff_sums(const P& p, unsigned char* lds, uint32_t lane, uint32_t wave, uint32_t m0, uint32_t n0, uint32_t kt0, uint32_t kt1,
-                                        f32x16 (&acc)[BM / 64][BN / 64])
-{
-    constexpr bool LARGE = BM == 256;
-    constexpr int MI = BM / 64, NI = BN / 64, LA = BM / 32, LB = BN / 32;       // squares of a wave; its loads per tile of 64 k
-    constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = BN * 128, kAtB = kBufsA * kBytesA;     // lds: [kBufsA][kBytesA], [2][kBytesB]
-    const uint32_t wm = wave / 2, wn = wave % 2;
-
-    // Bytes from the tile's first element to the units that this thread brings.  Load i of a wave fills 1 KB of LDS, from
-    // 1024 (4 i + wave) on: eight rows of an operand, or two or four rows of k of a transposed one.  What lies beyond the matrix
-    // is its last row or unit again.
-    uint32_t oa[LA], ob[LB];
-#pragma unroll
-    for (int i = 0; i < LA; ++i) oa[i] = ff_place<TA, BM>(wave, lane, i, [&](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
-#pragma unroll
-    for (int i = 0; i < LB; ++i)
-        ob[i] = ff_place<TB, BN>(wave, lane, i, [&](uint32_t r) { return ff_column<GATED, NI>(r); }, p.N - 1 - n0, static_cast<uint32_t>(p.ldb));
-
-    const uint32_t per_seg = p.ktiles;
-    // elements from an operand's first to the tile's, and from a tile of k to the next
-    const uint64_t a_first = TA ? m0 : m0 * p.lda, b_first = TB ? n0 : n0 * p.ldb;
-    const uint64_t a_step = TA ? kFfBk * p.lda : kFfBk, b_step = TB ? kFfBk * p.ldb : kFfBk;
-    // where the next tile of either operand is; B is asked for later than A, so each has a place of its own
-    struct Place {
-        uint32_t seg, left;
-    };
-    Place na{kt0 / per_seg, 0}, nb;
-    const uint32_t in_seg = kt0 - na.seg * per_seg;
-    na.left = per_seg - in_seg;
-    nb = na;
-    const uint16_t *pa = p.a[na.seg] + a_first + in_seg * a_step, *pb = p.b[nb.seg] + b_first + in_seg * b_step;
-    const uint16_t* pb2 = ff_second<GATED>(p, nb.seg, b_first + in_seg * b_step, pb);
-    auto next_a = [&]() {
-        pa += a_step;
-        if (--na.left == 0 && na.seg + 1 < p.nseg) {
-            pa = p.a[++na.seg] + a_first;
-            na.left = per_seg;
-        }
-    };
-    auto next_b = [&]() {
-        pb += b_step;
-        pb2 += b_step;
-        if (--nb.left == 0 && nb.seg + 1 < p.nseg) {
-            pb = p.b[++nb.seg] + b_first;
-            pb2 = ff_second<GATED>(p, nb.seg, b_first, pb);
-            nb.left = per_seg;
-        }
-    };
-    const uint32_t base = lds_address(lds) + wave * 1024;
-    auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa, oa[i], base + buf * kBytesA + i * 4096); };
-    auto bring_b = [&](uint32_t buf, int i) {
-        // gated: LB / 2 loads of either matrix for each wave of the tile's columns
-        const bool second = GATED && (i * 32) % (NI * 32) >= NI * 16;
-        load_to_lds(second ? pb2 : pb, ob[i], base + kAtB + buf * kBytesB + i * 4096);
-    };
-
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-
-    // A tile's four steps of 16 k: while one is multiplied, the fragments of the next are read (in the last one, the first of the
-    // next tile).  The barrier before the last step ends the reads of the tile: from there on B of tile t + 2 is asked for, into
-    // the place of tile t's.  A has three buffers where they fit (LARGE), and A of tile t + 2 is asked for in the first two
-    // steps of tile t.  Either has four steps at least to come: the barrier of tile t has to find tile t + 1 there, and after that
-    // tile was asked for came A of tile t + 2 only.
-    const FfFragments<TA, BM> frag_a(lane, wm * MI * 32);
-    const FfFragments<TB, BN> frag_b(lane, wn * NI * 32);
-    const uint32_t n = kt1 - kt0;
-    bf16x8 fa[2][MI], fb[2][NI];
-    auto read = [&](uint32_t buf_a, uint32_t buf_b, int kk, int f) {        // fragment f of the step: NI of B, MI of A, as they are used
-        const int to = kk & 1;
-        if (f < NI) fb[to][f] = frag_b.read(lds + kAtB + buf_b * kBytesB, kk, f);
-        else fa[to][f - NI] = frag_a.read(lds + buf_a * kBytesA, kk, f - NI);
-    };
-    for (uint32_t t = 0; t < 2 && t < n; ++t) {
-#pragma unroll
-        for (int i = 0; i < LA; ++i) bring_a(t, i);
-        next_a();
-#pragma unroll
-        for (int i = 0; i < LB; ++i) bring_b(t, i);
-        next_b();
-    }
-    if (n > 1) tile_barrier<LA + LB>();
-    else tile_barrier<0>();
-#pragma unroll
-    for (int f = 0; f < MI + NI; ++f) read(0, 0, 0, f);
-    uint32_t buf_a = 0, ask_a = kBufsA - 1;     // buffers of this tile's A and of the one asked for next
-    for (uint32_t t = 0; t < n; ++t) {
-        const uint32_t buf_b = t & 1, next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1;
-        const bool more_a = LARGE && t + 2 < n, more_b = t + 2 < n;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            if (kk == 3) {
-                if (more_a) tile_barrier<LA>();
-                else tile_barrier<0>();
-            }
-            const int from = kk & 1;
-#pragma unroll
-            for (int c = 0; c < MI + NI; ++c) {
-                if (kk < 3) read(buf_a, buf_b, kk + 1, c);
-                else read(next_buf_a, buf_b ^ 1, 0, c);
-                if (LARGE && kk < 2 && more_a && c % 2 == 0) bring_a(ask_a, kk * (LA / 2) + c / 2);
-                if (kk == 3 && more_b) {
-                    bring_b(buf_b, c);
-                    if (!LARGE) bring_a(buf_b, c);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int m = c * MI * NI / (MI + NI); m < (c + 1) * MI * NI / (MI + NI); ++m)
-                    acc[m / NI][m % NI] = ff_mfma<F16>(fb[from][m % NI], fa[from][m / NI], acc[m / NI][m % NI]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (LARGE && kk == 1 && more_a) next_a();
-        }
-        if (more_b) {
-            next_b();
-            if (!LARGE) next_a();
-        }
-        buf_a = next_buf_a;
-        ask_a = ask_a + 1 == kBufsA ? 0 : ask_a + 1;
-    }
-    tile_barrier<0>();
-}
-
 template <int BM, int BN, bool TA, bool TB, typename T, int EPI>
 __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
 {
-    constexpr bool GATED = EPI == kFfGate;
+    constexpr bool GATED = EPI == kFfGate, LARGE = BM == 256;
     static_assert(!GATED || !TB, "the projections' weights have k along their rows");
-    constexpr int MI = BM / 64, NI = BN / 64;                   // squares of a wave
+    constexpr int MI = BM / 64, NI = BN / 64, LA = BM / 32, LB = BN / 32;       // squares of a wave; its loads per tile of 64 k
     constexpr uint32_t COLS = GATED ? BN / 2 : BN;
+    constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = BN * 128, kAtB = kBufsA * kBytesA;
     static_assert(MI == NI, "");
-    extern __shared__ __align__(16) unsigned char lds[];        // ff_sums' tiles
-    static_assert(4 * 32 * kFfRow * 4 <= ff_lds_bytes(BM, BN), "the waves' parts of LDS in ff_finish fit where the tiles were");
+    extern __shared__ __align__(16) unsigned char lds[];        // [kBufsA][kBytesA], [2][kBytesB]
+    static_assert(4 * 32 * kFfRow * 4 <= kAtB + 2 * kBytesB, "the waves' parts of LDS in ff_finish fit where the tiles were");
 
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / 2, wn = wave % 2;
     const bool shares = blockIdx.x >= args.whole;
@@ -587,8 +439,124 @@ __global__ __launch_bounds__(256) void k_ff_gemm(const FfArgs args)
         ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
         const uint32_t m0 = tm * BM, n0 = tn * COLS;
 
+        // Bytes from the tile's first element to the units that this thread brings.  Load i of a wave fills 1 KB of LDS, from
+        // 1024 (4 i + wave) on: eight rows of an operand, or two or four rows of k of a transposed one.  What lies beyond the matrix
+        // is its last row or unit again.
+        uint32_t oa[LA], ob[LB];
+#pragma unroll
+        for (int i = 0; i < LA; ++i) oa[i] = ff_place<TA, BM>(wave, lane, i, [&](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
+#pragma unroll
+        for (int i = 0; i < LB; ++i)
+            ob[i] = ff_place<TB, BN>(wave, lane, i, [&](uint32_t r) { return ff_column<GATED, NI>(r); }, p.N - 1 - n0, static_cast<uint32_t>(p.ldb));
+
+        const uint32_t per_seg = p.ktiles;
+        // elements from an operand's first to the tile's, and from a tile of k to the next
+        const uint64_t a_first = TA ? m0 : m0 * p.lda, b_first = TB ? n0 : n0 * p.ldb;
+        const uint64_t a_step = TA ? kFfBk * p.lda : kFfBk, b_step = TB ? kFfBk * p.ldb : kFfBk;
+        // where the next tile of either operand is; B is asked for later than A, so each has a place of its own
+        struct Place {
+            uint32_t seg, left;
+        };
+        Place na{kt0 / per_seg, 0}, nb;
+        const uint32_t in_seg = kt0 - na.seg * per_seg;
+        na.left = per_seg - in_seg;
+        nb = na;
+        const uint16_t *pa = p.a[na.seg] + a_first + in_seg * a_step, *pb = p.b[nb.seg] + b_first + in_seg * b_step;
+        const uint16_t* pb2 = GATED ? p.b2[nb.seg] + b_first + in_seg * b_step : pb;
+        auto next_a = [&]() {
+            pa += a_step;
+            if (--na.left == 0 && na.seg + 1 < p.nseg) {
+                pa = p.a[++na.seg] + a_first;
+                na.left = per_seg;
+            }
+        };
+        auto next_b = [&]() {
+            pb += b_step;
+            pb2 += b_step;
+            if (--nb.left == 0 && nb.seg + 1 < p.nseg) {
+                pb = p.b[++nb.seg] + b_first;
+                pb2 = GATED ? p.b2[nb.seg] + b_first : pb;
+                nb.left = per_seg;
+            }
+        };
+        const uint32_t base = lds_address(lds) + wave * 1024;
+        auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa, oa[i], base + buf * kBytesA + i * 4096); };
+        auto bring_b = [&](uint32_t buf, int i) {
+            // gated: LB / 2 loads of either matrix for each wave of the tile's columns
+            const bool second = GATED && (i * 32) % (NI * 32) >= NI * 16;
+            load_to_lds(second ? pb2 : pb, ob[i], base + kAtB + buf * kBytesB + i * 4096);
+        };
+
         f32x16 acc[MI][NI];
-        ff_sums<BM, BN, TA, TB, GATED, false>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+        // A tile's four steps of 16 k: while one is multiplied, the fragments of the next are read (in the last one, the first of the
+        // next tile).  The barrier before the last step ends the reads of the tile: from there on B of tile t + 2 is asked for, into
+        // the place of tile t's.  A has three buffers where they fit (LARGE), and A of tile t + 2 is asked for in the first two
+        // steps of tile t.  Either has four steps at least to come: the barrier of tile t has to find tile t + 1 there, and after that
+        // tile was asked for came A of tile t + 2 only.
+        const FfFragments<TA, BM> frag_a(lane, wm * MI * 32);
+        const FfFragments<TB, BN> frag_b(lane, wn * NI * 32);
+        const uint32_t n = kt1 - kt0;
+        bf16x8 fa[2][MI], fb[2][NI];
+        auto read = [&](uint32_t buf_a, uint32_t buf_b, int kk, int f) {        // fragment f of the step: NI of B, MI of A, as they are used
+            const int to = kk & 1;
+            if (f < NI) fb[to][f] = frag_b.read(lds + kAtB + buf_b * kBytesB, kk, f);
+            else fa[to][f - NI] = frag_a.read(lds + buf_a * kBytesA, kk, f - NI);
+        };
+        for (uint32_t t = 0; t < 2 && t < n; ++t) {
+#pragma unroll
+            for (int i = 0; i < LA; ++i) bring_a(t, i);
+            next_a();
+#pragma unroll
+            for (int i = 0; i < LB; ++i) bring_b(t, i);
+            next_b();
+        }
+        if (n > 1) tile_barrier<LA + LB>();
+        else tile_barrier<0>();
+#pragma unroll
+        for (int f = 0; f < MI + NI; ++f) read(0, 0, 0, f);
+        uint32_t buf_a = 0, ask_a = kBufsA - 1;     // buffers of this tile's A and of the one asked for next
+        for (uint32_t t = 0; t < n; ++t) {
+            const uint32_t buf_b = t & 1, next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1;
+            const bool more_a = LARGE && t + 2 < n, more_b = t + 2 < n;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk == 3) {
+                    if (more_a) tile_barrier<LA>();
+                    else tile_barrier<0>();
+                }
+                const int from = kk & 1;
+#pragma unroll
+                for (int c = 0; c < MI + NI; ++c) {
+                    if (kk < 3) read(buf_a, buf_b, kk + 1, c);
+                    else read(next_buf_a, buf_b ^ 1, 0, c);
+                    if (LARGE && kk < 2 && more_a && c % 2 == 0) bring_a(ask_a, kk * (LA / 2) + c / 2);
+                    if (kk == 3 && more_b) {
+                        bring_b(buf_b, c);
+                        if (!LARGE) bring_a(buf_b, c);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int m = c * MI * NI / (MI + NI); m < (c + 1) * MI * NI / (MI + NI); ++m)
+                        acc[m / NI][m % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][m % NI], fa[from][m / NI], acc[m / NI][m % NI], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (LARGE && kk == 1 && more_a) next_a();
+            }
+            if (more_b) {
+                next_b();
+                if (!LARGE) next_a();
+            }
+            buf_a = next_buf_a;
+            ask_a = ask_a + 1 == kBufsA ? 0 : ask_a + 1;
+        }
+        tile_barrier<0>();
 
         if (kt1 - kt0 == args.ksteps) {
             float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kFfRow);

@@ -23,10 +23,10 @@ namespace {
 constexpr uint32_t kOrthoGroup = 10, kOrthoParts = 1024;    // matrices of a launch; blocks that one is spread over
 struct OrthoItem {
     const void* src;
-    uint16_t* x;                        // hi plane, its lo behind it
+    uint16_t* x;                        // planes
     double* part;                       // per block
     float* f;
-    uint64_t ld, ldx, plane;
+    uint64_t ld, ldx;
     uint32_t m, n, tiles_c, tiles, first, blocks, tall, _pad;
 };
 struct OrthoList {
@@ -104,13 +104,12 @@ __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
     auto put = [&](uint32_t row, uint32_t col, float (&v)[8]) {         // of X
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], k);
-        uint16_t* const to = t.x + row * t.ldx + col;
         if constexpr (P == 2) {
-            ortho_put(to, t.plane, v);
+            ortho_put(t.x + row * t.ldx, col, v);
         } else {
             u32x4 hi, lo;
             ortho_planes(v, hi, lo);
-            *reinterpret_cast<u32x4*>(to) = hi;
+            *reinterpret_cast<u32x4*>(t.x + row * t.ldx + col) = hi;
         }
     };
     const uint32_t row = threadIdx.x / 8, col = threadIdx.x % 8 * 8;
@@ -239,21 +238,20 @@ bool coefs_bounded(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps)
     return true;
 }
 
-// blocks that share a compute unit's LDS, and all there are at a time
-constexpr uint32_t ortho_blocks(int bm) { return 160u * 1024u / ff_lds_bytes(bm, bm); }
-uint32_t ortho_places(const edgc_ctx* ctx, int bm) { return static_cast<uint32_t>(ctx->num_cu) * ortho_blocks(bm); }
+// The tile shapes: blocks of 256 rows have a compute unit for themselves, of 128 x 128 two share it
+uint32_t ortho_places(const edgc_ctx* ctx, int bm) { return static_cast<uint32_t>(ctx->num_cu) * (bm == 256 ? 1 : 2); }
 // sums that workers can leave behind: at most two tiles per place
-uint64_t ortho_sums(const edgc_ctx* ctx) { return 2ull * std::max(256ull * 256 * ortho_places(ctx, 256), 128ull * 128 * ortho_places(ctx, 128)); }
-// the least steps of k that are worth a worker
-constexpr uint32_t kOrthoMinSteps = 8;
+uint64_t ortho_sums_elems(const edgc_ctx* ctx) { return 2ull * 256 * 256 * ctx->num_cu; }
+// the rate at which tiles of 128 x 128 get done, of that of the large ones
+template <int PA> constexpr double kOrthoLittle = PA == 1 ? 0.65 : 0.8;
+// the least tiles of k that are worth a worker
+constexpr uint32_t kOrthoMinTiles = 8;
 
-template <int BM>
+template <int BM, int BN, int PA, int PB, bool TB, typename T>
 hipError_t prepare_ortho_tiles()
 {
-    for (const void* f : {reinterpret_cast<const void*>(&k_ortho_gemm<BM, false, void>), reinterpret_cast<const void*>(&k_ortho_gemm<BM, true, void>),
-                          reinterpret_cast<const void*>(&k_ortho_gemm<BM, true, float>), reinterpret_cast<const void*>(&k_ortho_gemm<BM, true, __bf16>)})
-        if (hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, ff_lds_bytes(BM, BM))) return e;
-    return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ortho_gemm<BM, BN, PA, PB, TB, T>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               kOrthoLds<BM, BN, PB, TB>);
 }
 
 struct OrthoPass {
@@ -273,7 +271,7 @@ struct OrthoPass {
     Mat mats[kOrthoGroup] = {};
     uint32_t n = 0;                             // of them
 
-    template <int BM, bool TB, typename T>
+    template <int BM, int BN, int PA, int PB, bool TB, typename T>
     int launch(OrthoArgs& args, int kid)
     {
         uint32_t tiles = 0;
@@ -281,12 +279,12 @@ struct OrthoPass {
         for (uint32_t i = 0; i < args.count; ++i) {
             OrthoProblem& p = args.p[i];
             p.tiles_m = (p.M + BM - 1) / BM;
-            p.tiles_n = (p.N + BM - 1) / BM;
+            p.tiles_n = (p.N + BN - 1) / BN;
             p.first = tiles;
-            tiles += tiles_of<TB>(p, BM);
-            const double k = static_cast<double>(p.ktiles) * p.nseg * kFfBk;
-            flops += (TB ? 2.0 : 1.0) * p.M * p.N * k;
-            bytes += 2.0 * k * (static_cast<double>(p.M) + p.N);
+            tiles += tiles_of<BM, BN, TB>(p);
+            const double k = static_cast<double>(p.ktiles) * kOrthoK<PA, PB>;
+            flops += (TB ? 2.0 : 1.0) * p.M * p.N * k * (PA + PB - 1);
+            bytes += 2.0 * k * (static_cast<double>(p.M) * PA + static_cast<double>(p.N) * PB);
         }
         const uint32_t places = ortho_places(ctx, BM);
         args.whole = tiles / places * places;
@@ -297,11 +295,11 @@ struct OrthoPass {
                 OrthoProblem& p = args.p[i];
                 const uint32_t end = i + 1 < args.count ? args.p[i + 1].first : tiles;
                 p.begin = args.steps;
-                if (end > args.whole) args.steps += (end - std::max(p.first, args.whole)) * p.ktiles * p.nseg;
+                if (end > args.whole) args.steps += (end - std::max(p.first, args.whole)) * p.ktiles;
             }
         };
         count_rest();
-        args.workers = std::min(places, args.steps / kOrthoMinSteps);
+        args.workers = std::min(places, args.steps / kOrthoMinTiles);
         // (a last round that is nearly full is not worth the sums' way through memory)
         if (args.workers <= args.rest || args.rest * 10ull > places * 9ull) {
             args.whole = tiles;
@@ -309,64 +307,50 @@ struct OrthoPass {
             count_rest();
         }
         args.part = ctx->ortho.sums;
-        EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ortho_gemm<BM, TB, T><<<args.whole + args.workers, 256, ff_lds_bytes(BM, BM), st>>>(args));
+        EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ortho_gemm<BM, BN, PA, PB, TB, T><<<args.whole + args.workers, 256, kOrthoLds<BM, BN, PB, TB>, st>>>(args));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         if (args.rest) {
-            EDGC_LAUNCH(ctx, st, KID_ORTHO_JOIN, 4.0 * BM * BM * (args.workers + args.rest), 0.0,
-                        k_ortho_join<BM, TB, T><<<args.rest * (BM / 64) * (BM / 64), 256, 0, st>>>(args));
+            EDGC_LAUNCH(ctx, st, KID_ORTHO_JOIN, 4.0 * BM * BN * (args.workers + args.rest), 0.0,
+                        k_ortho_join<BM, BN, TB, T><<<args.rest * (BM / 64) * (BN / 64), 256, 0, st>>>(args));
             EDGC_HIP_TRY(ctx, hipGetLastError());
         }
         return EDGC_OK;
     }
-    template <bool TB>
-    static uint32_t tiles_of(const OrthoProblem& p, uint32_t bm)
+    template <int BM, int BN, bool TB>
+    static uint32_t tiles_of(const OrthoProblem& p)
     {
-        const uint32_t tm = (p.M + bm - 1) / bm, tn = (p.N + bm - 1) / bm;
-        return TB ? tm * tn : tm * (tm + 1) / 2;
+        const uint32_t tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
+        return TB ? tm * tn : ortho_tiles<BM / BN>(tm, tn);
     }
-    template <bool TB, typename T>
+    template <int PA, int PB, bool TB, typename T>
     int product(OrthoArgs& args, int kid)
     {
-        std::stable_sort(args.p, args.p + args.count, [](const OrthoProblem& x, const OrthoProblem& y) { return x.ktiles * x.nseg > y.ktiles * y.nseg; });
-        // The time that either tile shape would take, in steps of 64 k of a 256 x 256 tile on a compute unit (launch_product of the
-        // feed-forward block, whose loop this is)
-        auto time_of = [&](uint32_t bm, double step) {
+        constexpr int BN = PA == 1 ? 256 : 128;         // one plane: a wave has room for 128 x 128
+        std::stable_sort(args.p, args.p + args.count, [](const OrthoProblem& x, const OrthoProblem& y) { return x.ktiles > y.ktiles; });
+        // the time that either tile shape would take, in a tile of k of the large one on a compute unit; `alone`: of the little one without a second
+        auto time_of = [&](auto bm, auto bn, double step, double alone) {
             double steps = 0.0, least = 0.0;
             for (uint32_t i = 0; i < args.count; ++i) {
-                const double each = static_cast<double>(args.p[i].ktiles) * args.p[i].nseg;
-                steps += each * tiles_of<TB>(args.p[i], bm);
-                least = std::max(least, std::min(each, 1.0 * kOrthoMinSteps));
+                steps += static_cast<double>(args.p[i].ktiles) * tiles_of<bm, bn, TB>(args.p[i]);
+                least = std::max(least, 1.0 * std::min(args.p[i].ktiles, kOrthoMinTiles));
             }
-            return step * std::max(steps / ortho_places(ctx, bm), least);
+            return std::max(step * steps / ortho_places(ctx, bm), alone * least);
         };
-        if (time_of(256, 1.0) <= time_of(128, 0.25 * ortho_blocks(128) / 0.65)) return launch<256, TB, T>(args, kid);
-        return launch<128, TB, T>(args, kid);
-    }
-    // the products of an operand pair's planes, the small ones first
-    static void segments_in(OrthoProblem& p, const uint16_t* a, uint64_t plane_a, const uint16_t* b, uint64_t plane_b, uint32_t planes_a, uint32_t planes_b)
-    {
-        auto add = [&](const uint16_t* x, const uint16_t* y) { p.a[p.nseg] = x; p.b[p.nseg++] = y; };
-        if (planes_a == 2) add(a + plane_a, b);
-        if (planes_b == 2) add(a, b + plane_b);
-        add(a, b);
+        using std::integral_constant;
+        const double large = time_of(integral_constant<int, 256>{}, integral_constant<int, BN>{}, 1.0, 1.0),
+                     little = time_of(integral_constant<int, 128>{}, integral_constant<int, 128>{}, 2.0 * 64 / BN / kOrthoLittle<PA>, 0.75);
+        if (large <= little) return launch<256, BN, PA, PB, TB, T>(args, kid);
+        return launch<128, 128, PA, PB, TB, T>(args, kid);
     }
     // a product of two matrices of the smaller side, or the first of a segment
     static OrthoProblem symmetric(const Mat& m, const uint16_t* a, const uint16_t* b, uint16_t* out, double alpha)
     {
-        OrthoProblem p = symmetric_out(m, out, alpha);
-        segments_in(p, a, m.sh.S * m.sh.S, b, m.sh.S * m.sh.S, 2, 2);
-        p.lda = p.ldb = static_cast<uint32_t>(m.sh.S);
-        p.ktiles = static_cast<uint32_t>(m.sh.S / kFfBk);
-        return p;
-    }
-    static OrthoProblem symmetric_out(const Mat& m, uint16_t* out, double alpha)
-    {
         OrthoProblem p{};
-        p.out = out;
-        p.ldo = m.sh.S;
-        p.plane = m.sh.S * m.sh.S;
+        p.a = a; p.b = b; p.out = out;
+        p.lda = p.ldb = p.ldo = 2 * m.sh.S;
         p.M = p.N = static_cast<uint32_t>(m.sh.s);
         p.rows = p.cols = static_cast<uint32_t>(m.sh.S);
+        p.ktiles = static_cast<uint32_t>(m.sh.S / 32);
         p.alpha = static_cast<float>(alpha);
         return p;
     }
@@ -385,15 +369,13 @@ struct OrthoPass {
             {
                 OrthoArgs g{};
                 for (const Mat& m : these()) {
-                    OrthoProblem p = symmetric_out(m, m.a, std::ldexp(1.0, a_scale - (first ? 0 : 2 * x_scale)));
-                    const uint64_t plane = m.sh.S * m.sh.L;
-                    segments_in(p, m.x[from], plane, m.x[from], plane, single ? 1 : 2, single ? 1 : 2);
-                    p.lda = p.ldb = static_cast<uint32_t>(m.sh.L);
-                    p.ktiles = static_cast<uint32_t>(m.sh.L / kFfBk);
+                    OrthoProblem p = symmetric(m, m.x[from], m.x[from], m.a, std::ldexp(1.0, a_scale - (first ? 0 : 2 * x_scale)));
+                    p.lda = p.ldb = m.sh.L * (single ? 1 : 2);
+                    p.ktiles = static_cast<uint32_t>(m.sh.L / (single ? 64 : 32));
                     if (first) p.f = m.f, p.power = 2;
                     g.p[g.count++] = p;
                 }
-                if (int rc = product<false, void>(g, KID_ORTHO_GRAM)) return rc;
+                if (int rc = single ? product<1, 1, false, void>(g, KID_ORTHO_GRAM) : product<2, 2, false, void>(g, KID_ORTHO_GRAM)) return rc;
             }
             double q = 1.0;
             uint32_t at_q = 0;                  // which of w[] holds Q
@@ -412,18 +394,18 @@ struct OrthoPass {
                     p.gamma = static_cast<float>(std::ldexp(co.a, w_scale));
                     g.p[g.count++] = p;
                 }
-                if (int rc = product<false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
                 g = OrthoArgs{};
                 for (const Mat& m : these()) {     // V, and the next Q
                     if (!last) g.p[g.count++] = symmetric(m, m.w[at_w], m.a, m.v, std::ldexp(1.0, v_scale - w_scale - a_scale));
                     if (!begin) g.p[g.count++] = symmetric(m, m.w[at_w], m.w[at_q], m.w[at_new], std::ldexp(1.0, next_q - w_scale - q_scale));
                 }
                 if (g.count)
-                    if (int rc = product<false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                    if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
                 if (!last) {                    // the next A
                     g = OrthoArgs{};
                     for (const Mat& m : these()) g.p[g.count++] = symmetric(m, m.v, m.w[at_w], m.a, std::ldexp(1.0, next_a - v_scale - w_scale));
-                    if (int rc = product<false, void>(g, KID_ORTHO_CHAIN)) return rc;
+                    if (int rc = product<2, 2, false, void>(g, KID_ORTHO_CHAIN)) return rc;
                 }
                 a_scale = next_a;
                 q_scale = begin ? w_scale : next_q;
@@ -438,26 +420,33 @@ struct OrthoPass {
                 const Mat& m = mats[i];
                 const edgc_tensor& d = tensors[i0 + i];
                 OrthoProblem p{};
-                segments_in(p, m.w[at_q], m.sh.S * m.sh.S, m.x[from], m.sh.S * m.sh.L, 2, single ? 1 : 2);
-                p.lda = static_cast<uint32_t>(m.sh.S); p.ldb = static_cast<uint32_t>(m.sh.L);
+                p.a = m.w[at_q]; p.b = m.x[from];
+                p.lda = 2 * m.sh.S; p.ldb = m.sh.L * (single ? 1 : 2);
                 p.M = static_cast<uint32_t>(m.sh.s); p.N = static_cast<uint32_t>(m.sh.l);
-                p.ktiles = static_cast<uint32_t>(m.sh.S / kFfBk);
+                p.ktiles = static_cast<uint32_t>(m.sh.S / 32);
                 const double scale = out ? (scales ? scales[i0 + i] : 1.0) : std::ldexp(1.0, next_x);
                 p.alpha = static_cast<float>(std::ldexp(scale, -q_scale - (first ? 0 : x_scale)));
                 if (first) p.f = m.f, p.power = 1;
                 if (out) {
                     p.to = d.grad_out; p.ldo = d.ld_out; p.transposed = m.sh.tall;
                 } else {
-                    p.out = m.x[1 - from]; p.ldo = m.sh.L; p.plane = m.sh.S * m.sh.L;
+                    p.out = m.x[1 - from]; p.ldo = 2 * m.sh.L;
                     p.rows = static_cast<uint32_t>(m.sh.S); p.cols = static_cast<uint32_t>(m.sh.L);
                 }
                 g.p[g.count++] = p;
             }
-            if (int rc = !out ? product<true, void>(g, KID_ORTHO_APPLY) : dt == EDGC_F32 ? product<true, float>(g, KID_ORTHO_APPLY) : product<true, __bf16>(g, KID_ORTHO_APPLY)) return rc;
+            if (int rc = apply(g, single, out)) return rc;
             x_scale = next_x;
         }
         return EDGC_OK;
     }
+    int apply(OrthoArgs& g, bool single, bool out)
+    {
+        if (!out) return single ? product<2, 1, true, void>(g, KID_ORTHO_APPLY) : product<2, 2, true, void>(g, KID_ORTHO_APPLY);
+        if (dt == EDGC_F32) return product<2, 2, true, float>(g, KID_ORTHO_APPLY);
+        return single ? product<2, 1, true, __bf16>(g, KID_ORTHO_APPLY) : product<2, 2, true, __bf16>(g, KID_ORTHO_APPLY);
+    }
+
     struct Some {
         const Mat *from, *to;
         const Mat* begin() const { return from; }
@@ -492,7 +481,7 @@ struct OrthoPass {
             const edgc_tensor& d = tensors[i0 + i];
             OrthoItem& t = list.t[list.count++];
             t.src = d.grad; t.ld = d.ld; t.m = d.m; t.n = d.n;
-            t.x = mats[i].x[0]; t.ldx = mats[i].sh.L; t.plane = mats[i].sh.S * mats[i].sh.L; t.tall = mats[i].sh.tall;
+            t.x = mats[i].x[0]; t.ldx = mats[i].sh.L * planes; t.tall = mats[i].sh.tall;
             t.part = ctx->ortho.part + static_cast<size_t>(i) * kOrthoParts; t.f = mats[i].f;
             t.tiles_c = (d.n + 63) / 64;
             t.tiles = t.tiles_c * ((d.m + 63) / 64);
@@ -522,7 +511,11 @@ int check_shape(edgc_ctx* ctx, uint64_t m, uint64_t n)
 
 int prepare_ortho_kernels(edgc_ctx* ctx)
 {
-    EDGC_HIP_TRY(ctx, prepare_ortho_tiles<256>());
+    for (hipError_t e : {prepare_ortho_tiles<256, 256, 1, 1, false, void>(), prepare_ortho_tiles<256, 128, 2, 2, false, void>(),
+                         prepare_ortho_tiles<256, 128, 2, 1, true, void>(), prepare_ortho_tiles<256, 128, 2, 2, true, void>(),
+                         prepare_ortho_tiles<256, 128, 2, 2, true, float>(), prepare_ortho_tiles<256, 128, 2, 1, true, __bf16>(),
+                         prepare_ortho_tiles<256, 128, 2, 2, true, __bf16>()})
+        EDGC_HIP_TRY(ctx, e);
     return EDGC_OK;
 }
 
@@ -564,7 +557,7 @@ extern "C" int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const
     const size_t parts = static_cast<size_t>(kOrthoGroup) * kOrthoParts;
     bool ok = hipMalloc(&ctx->ortho.ws, need * 2) == hipSuccess;
     ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.part), parts * sizeof(double) + kOrthoGroup * sizeof(float)) == hipSuccess;
-    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.sums), ortho_sums(ctx) * sizeof(float)) == hipSuccess;
+    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.sums), ortho_sums_elems(ctx) * sizeof(float)) == hipSuccess;
     if (!ok) {
         (void)hipGetLastError();
         free_ortho(ctx);

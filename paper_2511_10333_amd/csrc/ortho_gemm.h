@@ -4,32 +4,37 @@
 // an absolute 2^-25 at least (the matrix instructions take subnormal numbers as they are).  Three products, lo hi, hi lo and hi hi, are summed in fp32;
 // the fourth is left out: below 2^-24 of the product, of either sign.  bf16 inputs are one plane, exactly.  (bf16 planes would take three and six.)
 //
-// The products are segments of one sum, the small ones first.  An MFMA adds its 16 k to the sum in several roundings, so that the errors of these
-// roundings, not of the planes, are what an update is off by: with the three products of every 16 k one after the other it was 3.4e-6 off for a
-// block of hidden 512 and 3.7e-6 for odd matrices up to 2731, where fp32 products are 2.5e-6 and 2.2e-6.
+// The planes lie next to each other: 32 neighbours of a row's hi, then their lo, 128 bytes.  A tile of 32 k of both is 64 columns of memory, and a
+// step's fragments are read from LDS once for its three products.  (As three sums over k, with each plane brought and read twice, tiles of 128 x 128
+// took 4.64 ms instead of 3.80 for a hidden-2048 block.)
+//
+// The two small products have a sum of their own.  An MFMA adds its 16 k to the sum in several roundings, and the errors of these, not of the planes, are
+// what an update is off by: with all three products in one sum it was 3.4e-6 off for a block of hidden 512 and 3.7e-6 for odd matrices up to 2731, where
+// fp32 products are 2.5e-6 and 2.2e-6; with two sums 2.1e-6 and 1.9e-6.  So a wave has 128 x 64 of a tile of 256 x 128.
 #pragma once
 
 #include "ff_gemm.h"
+#include "ortho_tiles.h"
 
 namespace edgc {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr uint32_t kOrthoSegs = 3;
 struct OrthoProblem {
-    const uint16_t *a[kOrthoSegs], *b[kOrthoSegs];      // operands, per segment (ff_sums)
-    uint64_t lda, ldb;                  // elements
+    const uint16_t *a, *b;              // operands
+    uint64_t lda, ldb;                  // 16-bit elements from row to row
     uint32_t M, N;                      // of the output
-    uint32_t ktiles, nseg;              // times 64 k of a segment; segments
+    uint32_t ktiles;                    // tiles of k
+    uint32_t spread;                    // one plane of an operand that has two is taken
     uint32_t tiles_m, tiles_n, first;   // tiles of the output; the first's number
     uint32_t begin;                     // the first of its steps of k among those that are shared
     uint32_t rows, cols;                // of `out`, with what is padding: zeros
-    uint16_t* out;                      // the output's hi plane, its lo `plane` elements behind it; or
+    uint16_t* out;                      // planes, or
     void* to;                           // the caller's matrix
     const uint16_t* e;                  // planes like `out`'s that are added, or null
     const float* f;                     // what the sums are multiplied by, to the power `power`
-    uint64_t ldo, plane;                // of out and e, or to
+    uint64_t ldo;                       // of out and e (16-bit elements), or to
     uint32_t power, transposed;         // transposed: to[n][m]
     float alpha, beta, gamma;           // alpha f^power sum + beta e + gamma I
 };
@@ -40,7 +45,7 @@ struct OrthoArgs {
     OrthoProblem p[kOrthoProblems];
     uint32_t count, whole, rest, workers;
     uint32_t steps;                     // of the other tiles, all together
-    float* part;                        // [workers + rest][BM * BM]
+    float* part;                        // [workers + rest][BM * BN]
 };
 static_assert(sizeof(OrthoArgs) <= 4032, "kernel arguments are limited to 4 KiB");
 
@@ -62,12 +67,15 @@ __device__ __forceinline__ void ortho_planes(const float (&v)[8], u32x4& hi, u32
         lo[i] = __builtin_bit_cast(uint32_t, l);
     }
 }
-__device__ __forceinline__ void ortho_put(uint16_t* to, uint64_t plane, const float (&v)[8])
+// where eight neighbours' hi are in a row of planes; lo: 32 further on
+__device__ __forceinline__ uint32_t ortho_at(uint32_t column) { return column / 32 * 64 + column % 32; }
+__device__ __forceinline__ void ortho_put(uint16_t* row, uint32_t column, const float (&v)[8])
 {
     u32x4 hi, lo;
     ortho_planes(v, hi, lo);
+    uint16_t* const to = row + ortho_at(column);
     *reinterpret_cast<u32x4*>(to) = hi;
-    *reinterpret_cast<u32x4*>(to + plane) = lo;
+    *reinterpret_cast<u32x4*>(to + 32) = lo;
 }
 
 // eight neighbours of a row of n columns, from column c on
@@ -95,33 +103,9 @@ __device__ __forceinline__ void ortho_store8(__bf16* row, uint32_t c, uint32_t n
     }
 }
 
-// Tile of a symmetric output of `tiles` x `tiles`: those on and below the diagonal, in bands of kFfBand rows, column by column, each XCD's
-// neighbours of each other (ff_tile_of)
-__device__ __forceinline__ void ortho_tile_of(uint32_t id, uint32_t tiles, uint32_t& tm, uint32_t& tn)
-{
-    constexpr uint32_t B = kFfBand;
-    const uint32_t total = tiles * (tiles + 1) / 2, per = total / 8, left = total % 8, xcd = id % 8, at = id / 8;
-    id = xcd * per + min(xcd, left) + at;
-    // band b begins after sum over the bands before it of B B b + B (B + 1) / 2
-    auto begin = [](uint32_t b) { return B * B * (b * (b - 1) / 2) + B * (B + 1) / 2 * b; };
-    uint32_t band = 0;
-    while ((band + 1) * B < tiles && begin(band + 1) <= id) ++band;
-    const uint32_t rows = min(B, tiles - band * B);
-    uint32_t in = id - begin(band);
-    if (in < rows * B * band) {             // left of the band's diagonal
-        tm = band * B + in % rows;
-        tn = in / rows;
-        return;
-    }
-    in -= rows * B * band;
-    uint32_t c = 0;
-    while (in >= rows - c) in -= rows - c++;
-    tm = band * B + c + in;
-    tn = band * B + c;
-}
-
 // The sums of a square of 32 rows and columns, of which a lane holds row lane % 32 and columns 8 (v / 4) + 4 (lane / 32) + v % 4: through the wave's
-// part of LDS, so that eight neighbours of a row are stored together, and of the square's transpose (SYM: where it is another square).
+// part of LDS, so that eight neighbours of a row are stored together.  SYM: a square below the diagonal is stored as its transpose above it too, and one
+// above it not at all.
 constexpr uint32_t kOrthoRow = 36;      // floats: 32 and a pad that spreads the rows over the banks
 __device__ __forceinline__ void ortho_spread(float factor, const f32x16& acc, float* mine, uint32_t lane)
 {
@@ -131,9 +115,10 @@ __device__ __forceinline__ void ortho_spread(float factor, const f32x16& acc, fl
             float4{factor * acc[4 * q], factor * acc[4 * q + 1], factor * acc[4 * q + 2], factor * acc[4 * q + 3]};
 }
 template <bool SYM, typename T>
-__device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine, uint32_t lane, uint32_t m0, uint32_t n0, bool mirror)
+__device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine, uint32_t lane, uint32_t m0, uint32_t n0)
 {
     constexpr bool PLANES = std::is_same<T, void>::value;
+    const bool mirror = SYM && m0 != n0;
     ff_wave_sync();
     const uint32_t c = lane % 4 * 8;
     const bool across = PLANES ? SYM && mirror : p.transposed != 0;
@@ -149,10 +134,10 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
             const float4 x = *reinterpret_cast<const float4*>(mine + r * kOrthoRow + c), y = *reinterpret_cast<const float4*>(mine + r * kOrthoRow + c + 4);
             float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
             if constexpr (PLANES) {
-                const uint64_t at = m * p.ldo + n;
+                const uint64_t at = m * p.ldo + ortho_at(n);
                 if (SYM && p.e) {
                     const f16x8 h = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(p.e + at)),
-                                l = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(p.e + at + p.plane));
+                                l = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(p.e + at + 32));
 #pragma unroll
                     for (uint32_t i = 0; i < 8; ++i) {
                         v[i] = fmaf(p.beta, static_cast<float>(h[i]) + static_cast<float>(l[i]), v[i]);
@@ -165,7 +150,7 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
                     *reinterpret_cast<float4*>(mine + r * kOrthoRow + c) = float4{v[0], v[1], v[2], v[3]};
                     *reinterpret_cast<float4*>(mine + r * kOrthoRow + c + 4) = float4{v[4], v[5], v[6], v[7]};
                 }
-                ortho_put(p.out + at, p.plane, v);
+                ortho_put(p.out + m * p.ldo, n, v);
             } else {
                 ortho_store8(static_cast<T*>(p.to) + m * p.ldo, n, p.N, v);
             }
@@ -184,17 +169,17 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = mine[(c + i) * kOrthoRow + r];
-            if constexpr (PLANES) ortho_put(p.out + n * p.ldo + m, p.plane, v);
+            if constexpr (PLANES) ortho_put(p.out + n * p.ldo, m, v);
             else ortho_store8(static_cast<T*>(p.to) + n * p.ldo, m, p.M, v);
         }
     }
     ff_wave_sync();
 }
 
-template <bool SYM>
+template <bool SYM, int BM, int BN>
 __device__ __forceinline__ void ortho_place(const OrthoProblem& p, uint32_t tile, uint32_t& tm, uint32_t& tn)
 {
-    if constexpr (SYM) ortho_tile_of(tile - p.first, p.tiles_m, tm, tn);
+    if constexpr (SYM) ortho_tile_of<BM / BN>(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
     else ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
 }
 __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
@@ -204,14 +189,158 @@ __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
     return factor;
 }
 
-// A block of 2 x 2 waves makes a BM x BM tile of the output.  !TB: the output is symmetric, M = N.  T: void, planes, or the caller's type.
-template <int BM, bool TB, typename T>
-__global__ __launch_bounds__(256) void k_ortho_gemm(const OrthoArgs args)
+// k of a tile, bytes of either operand's tile in LDS, all of LDS: two tiles of each, of A three where a block has the compute unit for itself
+template <int PA, int PB> constexpr int kOrthoK = PA == 1 && PB == 1 ? 64 : 32;
+template <int BN, int PB, bool TB> constexpr uint32_t kOrthoBytesB = TB ? 32u * BN * PB * 2u : BN * 128u;
+template <int BM, int BN, int PB, bool TB> constexpr uint32_t kOrthoLds = (BM == 256 ? 3u : 2u) * BM * 128u + 2u * kOrthoBytesB<BN, PB, TB>;
+
+// The sums of a tile over tiles kt0 to kt1 of k, by 2 x 2 waves: of a wave, I x J squares of 32 x 32.  The loop of ff_gemm.h: while a step of 16 k is
+// multiplied, the fragments of the next are read (in a tile's last step, the first of the next tile); the barrier before the last step ends the reads of the
+// tile, and from there on B of the tile after the next is asked for, into its place.  A, in three buffers (LARGE), is asked for in the first half of
+// the steps: the barrier of tile t finds tile t + 1 there, after which A of tile t + 2 alone was asked for.
+template <int BM, int BN, int PA, int PB, bool TB>
+__device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char* lds, uint32_t lane, uint32_t wave, uint32_t m0, uint32_t n0, uint32_t kt0, uint32_t kt1,
+                                           f32x16 (&acc)[BM / 64][BN / 64])
+{
+    constexpr bool LARGE = BM == 256, SMALL = PA + PB > 2;                          // SMALL: there are small products
+    constexpr int I = BM / 64, J = BN / 64, BK = kOrthoK<PA, PB>, KK = BK / 16;     // squares of a wave; k of a tile; steps of 16 k
+    constexpr int WIDTH = BN * PB;                                                 // TB: elements of a tile's row of k
+    constexpr int LA = BM / 32, LB = TB ? WIDTH / 64 : BN / 32;                    // a wave's loads of a tile
+    constexpr int FA = I * PA, FB = J * PB, F = FA + FB, MM = I * J * (PA + PB - 1);    // fragments and products of a step
+    constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = kOrthoBytesB<BN, PB, TB>, kAtB = kBufsA * kBytesA;    // lds: [kBufsA][kBytesA], [2][kBytesB]
+    static_assert(!TB || PA == 2, "the transposed operand is the gradient, multiplied by two planes");
+    static_assert(PA == PB || (PB == 1 && TB), "");
+    const uint32_t wm = wave / 2, wn = wave % 2;
+
+    // Bytes from the tile's first element to the units of 16 that this thread brings (ff_place).  One plane of two: every other four units of a row.
+    const uint32_t spread = PA == 1 ? p.spread : 0u;
+    uint32_t oa[LA], ob[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        oa[i] = ff_place<false, BM>(wave, lane, i, [](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
+        if constexpr (PA == 1) oa[i] += spread * (oa[i] & 64u);
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        ob[i] = ff_place<TB, WIDTH>(wave, lane, i, [](uint32_t r) { return r; }, TB ? static_cast<uint32_t>(p.ldb) - 1 - n0 * PB : p.N - 1 - n0, static_cast<uint32_t>(p.ldb));
+        if constexpr (PA == 1) ob[i] += spread * (ob[i] & 64u);
+    }
+    const uint64_t a_step = 64u << spread, b_step = TB ? BK * p.ldb : a_step;
+    const uint16_t *pa = p.a + m0 * p.lda + kt0 * a_step, *pb = p.b + (TB ? static_cast<uint64_t>(n0) * PB : n0 * p.ldb) + kt0 * b_step;
+    const uint32_t base = lds_address(lds) + wave * 1024;
+    auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa, oa[i], base + buf * kBytesA + i * 4096); };
+    auto bring_b = [&](uint32_t buf, int i) { load_to_lds(pb, ob[i], base + kAtB + buf * kBytesB + i * 4096); };
+
+    f32x16 small[SMALL ? I : 1][SMALL ? J : 1];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                acc[i][j][v] = 0.f;
+                if constexpr (SMALL) small[i][j][v] = 0.f;
+            }
+
+    const FfFragments<false, BM> frag_a(lane, wm * I * 32);
+    const FfFragments<TB, WIDTH> frag_b(lane, wn * J * 32 * (TB ? PB : 1));
+    const uint32_t n = kt1 - kt0;
+    f16x8 fa[2][FA], fb[2][FB];
+    // fragment f of a step: first B's, then A's; of a square its planes one after the other
+    auto read = [&](uint32_t buf_a, uint32_t buf_b, int kk, int f) {
+        const int to = kk & 1;
+        if (f < FB) {
+            const unsigned char* const at = lds + kAtB + buf_b * kBytesB;
+            fb[to][f] = __builtin_bit_cast(f16x8, TB ? frag_b.read(at, kk, f) : frag_b.read(at, f % PB * 2 + kk, f / PB));
+        } else {
+            fa[to][f - FB] = __builtin_bit_cast(f16x8, frag_a.read(lds + buf_a * kBytesA, (f - FB) % PA * 2 + kk, (f - FB) / PA));
+        }
+    };
+    for (uint32_t t = 0; t < 2 && t < n; ++t) {
+#pragma unroll
+        for (int i = 0; i < LA; ++i) bring_a(t, i);
+        pa += a_step;
+#pragma unroll
+        for (int i = 0; i < LB; ++i) bring_b(t, i);
+        pb += b_step;
+    }
+    if (n > 1) tile_barrier<LA + LB>();
+    else tile_barrier<0>();
+#pragma unroll
+    for (int f = 0; f < F; ++f) read(0, 0, 0, f);
+    uint32_t buf_a = 0, ask_a = kBufsA - 1;     // buffers of this tile's A and of the one asked for next
+    for (uint32_t t = 0; t < n; ++t) {
+        const uint32_t buf_b = t & 1, next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1;
+        const bool more_a = LARGE && t + 2 < n, more_b = t + 2 < n;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kk == KK - 1) {
+                if (more_a) tile_barrier<LA>();
+                else tile_barrier<0>();
+            }
+            const int from = kk & 1;
+#pragma unroll
+            for (int c = 0; c < F; ++c) {
+                if (kk < KK - 1) read(buf_a, buf_b, kk + 1, c);
+                else read(next_buf_a, buf_b ^ 1, 0, c);
+                if (LARGE && kk < KK / 2 && more_a) {
+                    constexpr int SLOTS = KK / 2 * F;
+#pragma unroll
+                    for (int i = (kk * F + c) * LA / SLOTS; i < (kk * F + c + 1) * LA / SLOTS; ++i) bring_a(ask_a, i);
+                }
+                if (kk == KK - 1 && more_b) {
+#pragma unroll
+                    for (int i = c * LB / F; i < (c + 1) * LB / F; ++i) bring_b(buf_b, i);
+                    if constexpr (!LARGE) {
+#pragma unroll
+                        for (int i = c * LA / F; i < (c + 1) * LA / F; ++i) bring_a(buf_b, i);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // the products of the planes: lo hi, hi lo (of the first operand's and the second's), hi hi
+#pragma unroll
+                for (int m = c * MM / F; m < (c + 1) * MM / F; ++m) {
+                    const int which = m / (I * J), i = m % (I * J) / J, j = m % J;
+                    const int qa = PA == 2 && which == 0 ? 1 : 0, qb = PB == 2 && which == 1 ? 1 : 0;
+                    f32x16& sum = SMALL && which < PA + PB - 2 ? small[SMALL ? i : 0][SMALL ? j : 0] : acc[i][j];
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[from][j * PB + qb], fa[from][i * PA + qa], sum, 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (LARGE && kk == KK / 2 - 1 && more_a) pa += a_step;
+        }
+        if (more_b) {
+            pb += b_step;
+            if (!LARGE) pa += a_step;
+        }
+        buf_a = next_buf_a;
+        ask_a = ask_a + 1 == kBufsA ? 0 : ask_a + 1;
+    }
+    tile_barrier<0>();
+    if constexpr (SMALL) {
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) acc[i][j] += small[i][j];
+    }
+}
+
+// Where a worker leaves the sums of a tile: in the order of its registers
+template <int BM, int BN>
+__device__ __forceinline__ float4* ortho_slot(float* part, uint32_t slot, uint32_t i, uint32_t j, uint32_t q, uint32_t tid)
+{
+    return ff_slot<BM, BN, BN / 64>(part, slot, i, j, q, tid);
+}
+
+// A block of 2 x 2 waves makes a BM x BN tile of the output; PA, PB: planes of the operands.  !TB: the output is symmetric, M = N.  T: void, planes, or
+// the caller's type.
+template <int BM, int BN, int PA, int PB, bool TB, typename T>
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const OrthoArgs args)
 {
     constexpr bool SYM = !TB;
-    constexpr int I = BM / 64;                                  // squares of a wave, either way
-    extern __shared__ __align__(16) unsigned char lds[];        // ff_sums' tiles
-    static_assert(4 * 32 * kOrthoRow * 4 <= ff_lds_bytes(BM, BM), "the waves' parts of LDS in ortho_square fit where the tiles were");
+    constexpr int I = BM / 64, J = BN / 64;
+    extern __shared__ __align__(16) unsigned char lds[];        // ortho_sums' tiles
+    static_assert(4 * 32 * kOrthoRow * 4 <= kOrthoLds<BM, BN, PB, TB>, "the waves' parts of LDS in ortho_square fit where the tiles were");
 
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / 2, wn = wave % 2;
     const bool shares = blockIdx.x >= args.whole;
@@ -226,42 +355,43 @@ __global__ __launch_bounds__(256) void k_ortho_gemm(const OrthoArgs args)
             while (pi + 1 < args.count && tile >= args.p[pi + 1].first) ++pi;
         }
         const OrthoProblem& p = args.p[pi];
-        const uint32_t ksteps = p.ktiles * p.nseg;
-        kt1 = ksteps;
+        kt1 = p.ktiles;
         if (shares) {
-            const uint32_t in = (step - p.begin) / ksteps;
+            const uint32_t in = (step - p.begin) / p.ktiles;
             tile = max(p.first, args.whole) + in;
-            kt0 = step - p.begin - in * ksteps;
-            kt1 = min(ksteps, kt0 + (steps_end - step));
+            kt0 = step - p.begin - in * p.ktiles;
+            kt1 = min(p.ktiles, kt0 + (steps_end - step));
         }
         step += kt1 - kt0;
         uint32_t tm, tn;
-        ortho_place<SYM>(p, tile, tm, tn);
-        const uint32_t m0 = tm * BM, n0 = tn * BM;
+        ortho_place<SYM, BM, BN>(p, tile, tm, tn);
+        const uint32_t m0 = tm * BM, n0 = tn * BN;
 
-        f32x16 acc[I][I];
-        ff_sums<BM, BM, false, TB, false, true>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
+        f32x16 acc[I][J];
+        ortho_sums<BM, BN, PA, PB, TB>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
 
-        if (kt1 - kt0 == ksteps) {
+        if (kt1 - kt0 == p.ktiles) {
             const float factor = ortho_factor(p);
             float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kOrthoRow);
             // a loop, whose code stays in the instruction cache
 #pragma unroll 1
-            for (int s = 0; s < I * I; ++s) {
-                ff_each<I * I>([&](auto q) {
+            for (int s = 0; s < I * J; ++s) {
+                const uint32_t m = m0 + (wm * I + s / J) * 32, n = n0 + (wn * J + s % J) * 32;
+                if (SYM && n > m) continue;
+                ff_each<I * J>([&](auto q) {
                     constexpr int k = decltype(q)::value;
-                    if (s == k) ortho_spread(factor, acc[k / I][k % I], mine, lane);
+                    if (s == k) ortho_spread(factor, acc[k / J][k % J], mine, lane);
                 });
-                ortho_square<SYM, T>(p, mine, lane, m0 + (wm * I + s / I) * 32, n0 + (wn * I + s % I) * 32, SYM && tm != tn);
+                ortho_square<SYM, T>(p, mine, lane, m, n);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int j = 0; j < I; ++j)
+                for (int j = 0; j < J; ++j)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *ff_slot<BM, BM, I>(args.part, worker + tile - args.whole, i, j, q, tid) =
+                        *ortho_slot<BM, BN>(args.part, worker + tile - args.whole, i, j, q, tid) =
                             float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         }
         if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
@@ -269,35 +399,37 @@ __global__ __launch_bounds__(256) void k_ortho_gemm(const OrthoArgs args)
 }
 
 // Adds up the sums that several workers have of a tile, in the order of the workers: one square of every wave's part per block
-template <int BM, bool TB, typename T>
+template <int BM, int BN, bool TB, typename T>
 __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
 {
     constexpr bool SYM = !TB;
-    constexpr uint32_t I = BM / 64;
+    constexpr uint32_t I = BM / 64, J = BN / 64;
     __shared__ __align__(16) float stage[4 * 32 * kOrthoRow];
-    const uint32_t at = blockIdx.x / (I * I), i = blockIdx.x / I % I, j = blockIdx.x % I, tile = args.whole + at;
+    const uint32_t at = blockIdx.x / (I * J), i = blockIdx.x / J % I, j = blockIdx.x % J, tile = args.whole + at;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     const OrthoProblem& p = ortho_problem_of(args, tile);
-    const uint32_t ksteps = p.ktiles * p.nseg, s0 = p.begin + (tile - max(p.first, args.whole)) * ksteps, s1 = s0 + ksteps;
+    const uint32_t s0 = p.begin + (tile - max(p.first, args.whole)) * p.ktiles, s1 = s0 + p.ktiles;
     // the workers that have a step of this tile
     uint32_t first = static_cast<uint32_t>(static_cast<uint64_t>(s0) * args.workers / args.steps), last = static_cast<uint32_t>(static_cast<uint64_t>(s1 - 1) * args.workers / args.steps);
     while (ortho_share(args, first + 1) <= s0) ++first;
     while (last + 1 < args.workers && ortho_share(args, last + 1) < s1) ++last;
     if (first == last) return;                      // one, which has finished it
+    uint32_t tm, tn;
+    ortho_place<SYM, BM, BN>(p, tile, tm, tn);
+    const uint32_t m = tm * BM + (wave / 2 * I + i) * 32, n = tn * BN + (wave % 2 * J + j) * 32;
+    if (SYM && n > m) return;
     f32x16 acc = {};
 #pragma unroll 4
     for (uint32_t w = first; w <= last; ++w) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float4 v = *ff_slot<BM, BM, static_cast<int>(I)>(args.part, w + at, i, j, q, tid);
+            const float4 v = *ortho_slot<BM, BN>(args.part, w + at, i, j, q, tid);
             acc[4 * q] += v.x; acc[4 * q + 1] += v.y; acc[4 * q + 2] += v.z; acc[4 * q + 3] += v.w;
         }
     }
-    uint32_t tm, tn;
-    ortho_place<SYM>(p, tile, tm, tn);
     float* const mine = stage + wave * (32 * kOrthoRow);
     ortho_spread(ortho_factor(p), acc, mine, lane);
-    ortho_square<SYM, T>(p, mine, lane, tm * BM + (wave / 2 * I + i) * 32, tn * BM + (wave % 2 * I + j) * 32, SYM && tm != tn);
+    ortho_square<SYM, T>(p, mine, lane, m, n);
 }
 
 }  // namespace edgc
