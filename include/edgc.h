@@ -20,8 +20,10 @@
  *      global norm of the gradients and their clipping, the norms before and
  *      after a block fused with its gate and residual scale, and the gated
  *      feed-forward block, with their backward passes
- *   7. what stands before and after the stack of blocks: the orthogonalised
- *      update of the weights from a list of gradients
+ *   7. what stands before, in and after the stack of blocks: the embedding of
+ *      the tokens and its gradient, the norms of queries and keys with the
+ *      rotation by position and their gradients, and the orthogonalised update
+ *      of the weights from a list of gradients
  *
  * Conventions
  *   - Every function returns an edgc_status (0 = OK, < 0 = error).  No C++
@@ -598,7 +600,7 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
                      int accumulate, void* hip_stream);
 
 /* ------------------------------------------------------------------------
- * 7. Before and after the stack of blocks.
+ * 7. Before, in and after the stack of blocks.
  *
  * The orthogonalised update of a list of gradients (of the descriptors grad,
  * ld, grad_out, ld_out, m and n are read): every matrix G by itself becomes
@@ -632,6 +634,80 @@ int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const uint32_t* 
 int edgc_orthogonalize_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count,
                              edgc_dtype dtype, uint32_t steps, double a, double b, double c,
                              double eps, const float* scales, void* hip_stream);
+
+/* The embedding of tokens and its gradient:
+ *     out[t] = round_dtype(scale * table[ids[t] - first_id]), zeros for an id
+ *     that is not in first_id .. first_id + vocab - 1 (padding, or a row of
+ *     another rank's part of the table)
+ *     dtable[v] = round_dtype(scale * sum of dy[t] over ids[t] - first_id = v)
+ * table, dtable: vocab x hidden; out, dy: tokens x hidden; row-major of one dtype,
+ * with leading dimensions.  ids: device, int32 or int64 (id_bytes 4 or 8).
+ * Sums are in fp32 in the order of the tokens (in runs of 32 of a row's and
+ * those in order): the same tokens give the same bits.  A row without a token
+ * becomes zeros; accumulate != 0 adds to what is there, and leaves such a row.
+ * No output may overlap an input.  tokens = 0 does nothing (backward without
+ * accumulate: all rows become zeros).
+ * The backward pass needs scratch for the largest tokens, vocab and hidden at
+ * hand: edgc_reserve_embed, which replaces, keeps and frees as
+ * edgc_reserve_block_norm does.
+ * Errors: EDGC_EINVAL for null or misaligned pointers, vocab or hidden 0 or over
+ * 2^20, tokens over 2^26, first_id beyond 2^62 either way, a scale that is not
+ * finite, leading dimensions too small or over 2^40, or sizes over the
+ * reservation. */
+int edgc_embed_forward(edgc_ctx* ctx, edgc_dtype dtype, const void* table, uint64_t ld_table,
+                       uint32_t vocab, uint32_t hidden, const void* ids, int id_bytes,
+                       int64_t first_id, uint64_t tokens, float scale, void* out, uint64_t ld_out,
+                       void* hip_stream);
+int edgc_reserve_embed(edgc_ctx* ctx, uint32_t tokens, uint32_t vocab, uint32_t hidden);
+int edgc_embed_backward(edgc_ctx* ctx, edgc_dtype dtype, const void* ids, int id_bytes,
+                        int64_t first_id, uint64_t tokens, const void* dy, uint64_t ld_dy,
+                        uint32_t vocab, uint32_t hidden, float scale, void* dtable,
+                        uint64_t ld_dtable, int accumulate, void* hip_stream);
+
+/* The norms of queries and keys, each head by itself, with the rotation by
+ * position in the same pass:
+ *     forward:  r = (mean(x^2) + eps)^(-1/2),   y = R(x * r * w)
+ *     R: of the first `rot` dimensions pair i, which is (x[i], x[rot / 2 + i]), or
+ *     with interleaved != 0 (x[2 i], x[2 i + 1]), becomes
+ *     (a cos - b sin, b cos + a sin) of the angle position * inv_freq[i]; the other
+ *     dimensions stay.
+ *     backward: d = R^T(dy),  u = d * w,  xh = x * r
+ *               dx = r * (u - xh * mean(u * xh)),  dw = sum over tokens, heads of d * xh
+ * for queries (heads_q of them) and keys (heads_k, or 0 for none: k, w_k, k_out
+ * and the like are then NULL), tokens x heads x dim of one dtype, a head's
+ * dimensions adjacent, tokens and heads any strides apart (views of the product
+ * that gave queries, keys and values, or places in a cache).  w: dim.  positions:
+ * device, int32 or int64 (pos_bytes 4 or 8), one per token, of any sign; inv_freq:
+ * device, fp64[rot / 2]; with rot = 0 both may be NULL.  Angles are in 64 bits,
+ * everything else in fp32; every output is rounded once, and the same call gives
+ * the same bits.  q_out may be q, dq either of dq_out and q, with the same strides,
+ * and so for keys.  tokens = 0 does nothing (backward: the weights' gradients
+ * become zeros).
+ * The backward pass needs scratch for the largest tokens, heads and
+ * dim: edgc_reserve_qk_norm, which replaces, keeps and frees as
+ * edgc_reserve_block_norm does.
+ * Errors: EDGC_EINVAL for null or misaligned pointers, dim 0 or over 512, heads_q 0
+ * or heads over 2^16, tokens over 2^31, rot that is odd or over dim, strides over
+ * 2^40, outputs whose heads overlap, an eps that is negative or not finite, or
+ * sizes over the reservation. */
+typedef struct {
+    void*    p;
+    uint64_t token, head;       /* elements from a token, a head, to the next */
+} edgc_heads;
+int edgc_qk_norm_forward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, uint32_t heads_q,
+                         uint32_t heads_k, uint32_t dim, const edgc_heads* q, const edgc_heads* k,
+                         const void* w_q, const void* w_k, const void* positions, int pos_bytes,
+                         const double* inv_freq, uint32_t rot, int interleaved, float eps,
+                         const edgc_heads* q_out, const edgc_heads* k_out, void* hip_stream);
+int edgc_reserve_qk_norm(edgc_ctx* ctx, uint32_t tokens, uint32_t heads_q, uint32_t heads_k,
+                         uint32_t dim);
+int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t tokens, uint32_t heads_q,
+                          uint32_t heads_k, uint32_t dim, const edgc_heads* dq_out,
+                          const edgc_heads* dk_out, const edgc_heads* q, const edgc_heads* k,
+                          const void* w_q, const void* w_k, const void* positions, int pos_bytes,
+                          const double* inv_freq, uint32_t rot, int interleaved, float eps,
+                          const edgc_heads* dq, const edgc_heads* dk, void* dw_q, void* dw_k,
+                          void* hip_stream);
 
 #ifdef __cplusplus
 }

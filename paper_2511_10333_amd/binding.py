@@ -152,6 +152,20 @@ def load_library() -> C.CDLL:
     L.edgc_reserve_orthogonalize.argtypes = [vp, i32, C.POINTER(u32), C.POINTER(u32), u32, u32]
     L.edgc_orthogonalize_batch.restype = i32
     L.edgc_orthogonalize_batch.argtypes = [vp, C.POINTER(_Tensor), u32, i32, u32, f64, f64, f64, f64, vp, vp]
+    i64, heads = C.c_int64, C.POINTER(_Heads)
+    L.edgc_embed_forward.restype = i32
+    L.edgc_embed_forward.argtypes = [vp, i32, vp, u64, u32, u32, vp, i32, i64, u64, f32, vp, u64, vp]
+    L.edgc_reserve_embed.restype = i32
+    L.edgc_reserve_embed.argtypes = [vp, u32, u32, u32]
+    L.edgc_embed_backward.restype = i32
+    L.edgc_embed_backward.argtypes = [vp, i32, vp, i32, i64, u64, vp, u64, u32, u32, f32, vp, u64, i32, vp]
+    L.edgc_qk_norm_forward.restype = i32
+    L.edgc_qk_norm_forward.argtypes = [vp, i32, u64, u32, u32, u32, heads, heads, vp, vp, vp, i32, vp, u32, i32, f32, heads, heads, vp]
+    L.edgc_reserve_qk_norm.restype = i32
+    L.edgc_reserve_qk_norm.argtypes = [vp, u32, u32, u32, u32]
+    L.edgc_qk_norm_backward.restype = i32
+    L.edgc_qk_norm_backward.argtypes = [vp, i32, u64, u32, u32, u32, heads, heads, heads, heads, vp, vp, vp, i32, vp, u32, i32, f32, heads, heads,
+                                        vp, vp, vp]
     _lib = L
     return L
 
@@ -172,6 +186,10 @@ class _FF(C.Structure):
     _fields_ = [("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p), ("ld_gate", C.c_uint64),
                 ("ld_up", C.c_uint64), ("ld_down", C.c_uint64), ("hidden", C.c_uint32), ("ff", C.c_uint32),
                 ("dtype", C.c_int32), ("act", C.c_int32)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("token", C.c_uint64), ("head", C.c_uint64)]
 
 
 @dataclass
@@ -403,6 +421,28 @@ def _check_u32(*sizes) -> None:
     for n in sizes:
         if n >> 32:
             raise ValueError("tokens and widths must be 0 or more and below 2^32")
+
+
+def _head_views(name, t, dtype, shape) -> _Heads:
+    """Queries or keys (tokens x heads x dim) of that dtype and shape, the dimensions of a head adjacent."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be of shape {tuple(shape)}")
+    token, head, step = t.stride()
+    if step != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have the dimensions of a head next to each other")
+    return _Heads(t.data_ptr(), token, head)
+
+
+def _integers(name, t, shape) -> int:
+    """Bytes of an element of a contiguous vector of int32 or int64."""
+    torch = _torch or _load_torch()
+    if t.dtype is not torch.int64 and t.dtype is not torch.int32:
+        raise TypeError(f"{name} must be int32 or int64")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous of shape {tuple(shape)}")
+    return 8 if t.dtype is torch.int64 else 4
 
 
 def _gradient_rows(t):
@@ -867,3 +907,115 @@ class Context:
         s = (C.c_float * max(n, 1))(*scales) if scales is not None else None
         rc = self._L.edgc_orthogonalize_batch(self._h, arr, n, code, steps, a, b, c, eps, s, _stream_handle(stream))
         self._check(rc, "edgc_orthogonalize_batch")
+
+    def _on_device(self, *tensors) -> None:
+        """Every given tensor lies on the context's GPU: another address would be one for its kernels to fault on."""
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"tensors must be on the context's device, cuda:{self.device}")
+
+    def embed_forward(self, table, ids, out, scale: float = 1.0, first_id: int = 0, stream=None) -> None:
+        """edgc_embed_forward: out[t] = scale * table[ids[t] - first_id], zeros for an id that is not in the table; ``ids``: int32 or
+        int64, contiguous."""
+        if table.dim() != 2:
+            raise ValueError("table must be vocab x hidden")
+        (vocab, hidden), dtype = table.shape, table.dtype
+        _check_u32(vocab, hidden)
+        code, t = _dtype_code(table), ids.numel()
+        bytes_ = _integers("ids", ids, (t,))
+        ld, ldo = _rows("table", table, dtype, (vocab, hidden)), _rows("out", out, dtype, (t, hidden))
+        self._on_device(table, ids, out)
+        if first_id.bit_length() > 63:
+            raise ValueError("first_id beyond 2^62")
+        rc = self._L.edgc_embed_forward(self._h, code, table.data_ptr(), ld, vocab, hidden, ids.data_ptr(), bytes_, first_id, t, scale, out.data_ptr(),
+                                        ldo, _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_embed_forward")
+
+    def reserve_embed(self, tokens: int, vocab: int, hidden: int) -> None:
+        """edgc_reserve_embed: scratch of :meth:`embed_backward` for up to that many tokens, rows and columns, in place of an earlier reservation (see
+        :meth:`reserve_block_norm`)."""
+        _check_u32(tokens, vocab, hidden)
+        self._check(self._L.edgc_reserve_embed(self._h, tokens, vocab, hidden), "edgc_reserve_embed")
+
+    def embed_backward(self, ids, dy, dtable, scale: float = 1.0, first_id: int = 0, accumulate: bool = False, stream=None) -> None:
+        """edgc_embed_backward: dtable[v] = scale * the sum of dy[t] over ids[t] - first_id = v, zeros without a token; ``accumulate`` adds to what is
+        there."""
+        if dtable.dim() != 2:
+            raise ValueError("dtable must be vocab x hidden")
+        (vocab, hidden), dtype = dtable.shape, dtable.dtype
+        _check_u32(vocab, hidden)
+        code, t = _dtype_code(dtable), ids.numel()
+        bytes_ = _integers("ids", ids, (t,))
+        ldt, ldy = _rows("dtable", dtable, dtype, (vocab, hidden)), _rows("dy", dy, dtype, (t, hidden))
+        self._on_device(dtable, ids, dy)
+        if first_id.bit_length() > 63:
+            raise ValueError("first_id beyond 2^62")
+        rc = self._L.edgc_embed_backward(self._h, code, ids.data_ptr(), bytes_, first_id, t, dy.data_ptr(), ldy, vocab, hidden, scale,
+                                         dtable.data_ptr(), ldt, 1 if accumulate else 0, _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_embed_backward")
+
+    def _qk_args(self, q, k, w_q, w_k, positions, inv_freq):
+        """What the two passes have in common: type, sizes, positions and frequencies, all as they have to be."""
+        if len(q.shape) != 3 or (k is not None and len(k.shape) != 3):
+            raise ValueError("queries and keys must be tokens x heads x dim")
+        t, hq, dim = q.shape
+        hk = 0 if k is None else k.shape[1]
+        _check_u32(hq, hk, dim)
+        code, dtype = _dtype_code(q), q.dtype
+        _check_dense(("w_q", "w_k"), (w_q, w_k), dtype, (dim,))
+        if w_q is None or (k is not None and w_k is None):
+            raise ValueError("queries need w_q, and keys w_k")
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        bytes_ = 8
+        if rot:
+            if positions is None:
+                raise ValueError("inv_freq needs positions")
+            bytes_ = _integers("positions", positions, (t,))
+            _check_dense(("inv_freq",), (inv_freq,), _torch.float64, (rot // 2,))
+        self._on_device(q, k, w_q, w_k, positions, inv_freq)
+        return code, dtype, t, hq, hk, dim, rot, bytes_
+
+    @staticmethod
+    def _heads(name, t, like, dtype, shape):
+        """Descriptor of queries or keys of that shape, or None where the layer has none (``like`` is None)."""
+        if like is None:
+            if t is not None:
+                raise ValueError(f"{name} without keys")
+            return None
+        if t is None:
+            raise ValueError(f"{name} is missing")
+        return C.byref(_head_views(name, t, dtype, shape))
+
+    def qk_norm_forward(self, q, k, w_q, w_k, positions, inv_freq, q_out, k_out, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+        """edgc_qk_norm_forward: every head of ``q`` and ``k`` (tokens x heads x dim, any strides of tokens and heads; ``k`` may be None) normed, times
+        its weight, and the first 2 * len(inv_freq) dimensions rotated by positions * inv_freq (int32 or int64, and float64; None: none are)."""
+        code, dtype, t, hq, hk, dim, rot, bytes_ = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
+        sq, sk, h = (t, hq, dim), (t, hk, dim), self._heads
+        self._on_device(q_out, k_out)
+        rc = self._L.edgc_qk_norm_forward(self._h, code, t, hq, hk, dim, h("q", q, q, dtype, sq), h("k", k, k, dtype, sk), _ptr(w_q), _ptr(w_k),
+                                          _ptr(positions), bytes_, _ptr(inv_freq), rot, 1 if interleaved else 0, eps, h("q_out", q_out, q, dtype, sq),
+                                          h("k_out", k_out, k, dtype, sk), _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_qk_norm_forward")
+
+    def reserve_qk_norm(self, tokens: int, heads_q: int, heads_k: int, dim: int) -> None:
+        """edgc_reserve_qk_norm: scratch of :meth:`qk_norm_backward` for up to these sizes, in place of an earlier reservation (see
+        :meth:`reserve_block_norm`)."""
+        _check_u32(tokens, heads_q, heads_k, dim)
+        self._check(self._L.edgc_reserve_qk_norm(self._h, tokens, heads_q, heads_k, dim), "edgc_reserve_qk_norm")
+
+    def qk_norm_backward(self, dq_out, dk_out, q, k, w_q, w_k, positions, inv_freq, dq, dk, dw_q, dw_k, eps: float = 1e-6, interleaved: bool = False,
+                         stream=None) -> None:
+        """edgc_qk_norm_backward: the gradients of what :meth:`qk_norm_forward` read, from those of what it wrote."""
+        code, dtype, t, hq, hk, dim, rot, bytes_ = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
+        sq, sk, h = (t, hq, dim), (t, hk, dim), self._heads
+        _check_dense(("dw_q", "dw_k"), (dw_q, dw_k), dtype, (dim,))
+        self._on_device(dq_out, dk_out, dq, dk, dw_q, dw_k)
+        rc = self._L.edgc_qk_norm_backward(self._h, code, t, hq, hk, dim, h("dq_out", dq_out, q, dtype, sq), h("dk_out", dk_out, k, dtype, sk),
+                                           h("q", q, q, dtype, sq), h("k", k, k, dtype, sk), _ptr(w_q), _ptr(w_k), _ptr(positions), bytes_,
+                                           _ptr(inv_freq), rot, 1 if interleaved else 0, eps, h("dq", dq, q, dtype, sq), h("dk", dk, k, dtype, sk),
+                                           _ptr(dw_q), _ptr(dw_k), _stream_handle(stream))
+        if rc:
+            self._check(rc, "edgc_qk_norm_backward")

@@ -10,92 +10,13 @@
 // are taken across the threads that hold it, and what it gives is written once.  A row is held by a wave (no barrier) or by a block.
 // bf16: 16384 rows of 5120 forward, 671 MB, 150 us (4.5 TB/s); 8192 rows of 4096 backward, 403 MB, 94 us (4.3 TB/s) and 4 for the
 // column sums; one row 7 us, the launch.
-#include "edgc_internal.h"
+#include "row_pack.h"
 
 #include <algorithm>
 #include <cmath>
 
 namespace edgc {
 namespace {
-
-typedef float f32x4_at __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4_at __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x4r __attribute__((ext_vector_type(4)));
-
-// 16 bytes of a row in registers, as they stand in memory
-template <typename T> struct Pack;
-template <> struct Pack<float> {
-    static constexpr int N = 4;
-    u32x4r v;
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(v[i]); }
-    __device__ __forceinline__ void set(const float (&f)[N])
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __float_as_uint(f[i]);
-    }
-    __device__ __forceinline__ void load(const float* p, uint32_t len)
-    {
-        if (len == N) {
-            const f32x4_at x = *reinterpret_cast<const f32x4_at*>(p);
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = __float_as_uint(x[i]);
-            return;
-        }
-        v = u32x4r{0, 0, 0, 0};
-        for (int i = 0; i < N; ++i)
-            if (static_cast<uint32_t>(i) < len) v[i] = __float_as_uint(p[i]);
-    }
-    __device__ __forceinline__ void store(float* p, uint32_t len) const
-    {
-        if (len == N) {
-            f32x4_at x;
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v[i]);
-            *reinterpret_cast<f32x4_at*>(p) = x;
-            return;
-        }
-        for (int i = 0; i < N; ++i)
-            if (static_cast<uint32_t>(i) < len) p[i] = __uint_as_float(v[i]);
-    }
-};
-template <> struct Pack<__bf16> {
-    static constexpr int N = 8;
-    u32x4r v;
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); }
-    __device__ __forceinline__ void set(const float (&f)[N])
-    {
-        typedef float f2 __attribute__((ext_vector_type(2)));
-        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), b2));
-    }
-    __device__ __forceinline__ void load(const __bf16* p, uint32_t len)
-    {
-        if (len == N) {
-            const u32x4_at x = *reinterpret_cast<const u32x4_at*>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = x[i];
-            return;
-        }
-        v = u32x4r{0, 0, 0, 0};
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-        for (int i = 0; i < N; ++i)
-            if (static_cast<uint32_t>(i) < len) v[i / 2] |= static_cast<uint32_t>(q[i]) << (16 * (i & 1));
-    }
-    __device__ __forceinline__ void store(__bf16* p, uint32_t len) const
-    {
-        if (len == N) {
-            u32x4_at x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = v[i];
-            *reinterpret_cast<u32x4_at*>(p) = x;
-            return;
-        }
-        uint16_t* q = reinterpret_cast<uint16_t*>(p);
-        for (int i = 0; i < N; ++i)
-            if (static_cast<uint32_t>(i) < len) q[i] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
-    }
-};
 
 // A value's sum over the wave, in every lane: within rows of 16 lanes, then across them
 __device__ __forceinline__ float wave_sum(float v)

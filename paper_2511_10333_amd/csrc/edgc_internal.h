@@ -145,6 +145,17 @@ struct OrthoScratch {
     uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
 };
 
+// Scratch of the embedding's gradient (edgc_reserve_embed) and of that of the norms of queries and keys (edgc_reserve_qk_norm).
+struct EmbedScratch {
+    void*    ws = nullptr;          // the tokens' order, the rows' places in it, parts of sums
+    uint64_t bytes = 0, held = 0;   // reserved; of ws: that or more
+};
+struct QkScratch {
+    float*   part = nullptr;        // [blocks][2][dim] sums of the weights' gradients
+    size_t   held = 0;              // elements of it: what the limits below need, or more
+    uint32_t tokens = 0, heads_q = 0, heads_k = 0, dim = 0;
+};
+
 // Kernel ids for the optional per-kernel event timing (edgc_profile_begin/end).
 enum KernelId {
     KID_SET_RANGE = 0, KID_MINMAX, KID_HIST, KID_SAMPLE_IDX, KID_INIT_Q, KID_PASS_P,
@@ -152,7 +163,8 @@ enum KernelId {
     KID_PASS_P_DEFERRED, KID_WIDE_HIST, KID_WIDE_REDUCE, KID_ESTIMATE_ONE, KID_SUMSQ, KID_CLIP,
     KID_NORM_FORWARD, KID_NORM_BACKWARD, KID_NORM_SUM, KID_FF_PACK,
     KID_FF_GATE, KID_FF_DOWN, KID_FF_DGATE, KID_FF_DX, KID_FF_DW, KID_FF_JOIN,
-    KID_ORTHO_SUMSQ, KID_ORTHO_PACK, KID_ORTHO_GRAM, KID_ORTHO_CHAIN, KID_ORTHO_APPLY, KID_ORTHO_JOIN, KID_COUNT
+    KID_ORTHO_SUMSQ, KID_ORTHO_PACK, KID_ORTHO_GRAM, KID_ORTHO_CHAIN, KID_ORTHO_APPLY, KID_ORTHO_JOIN,
+    KID_EMBED_FORWARD, KID_EMBED_SORT, KID_EMBED_SUM, KID_EMBED_JOIN, KID_QK_FORWARD, KID_QK_BACKWARD, KID_QK_SUM, KID_COUNT
 };
 extern const char* const kKernelNames[KID_COUNT];
 
@@ -202,6 +214,8 @@ struct edgc_ctx {
     edgc::NormScratch norm;
     edgc::FfScratch ff;
     edgc::OrthoScratch ortho;
+    edgc::EmbedScratch embed;
+    edgc::QkScratch qk;
     edgc::Profiler prof;
     std::string last_error;
 };
@@ -352,6 +366,9 @@ int prepare_entropy_kernels(edgc_ctx* ctx);
 int prepare_ff_kernels(edgc_ctx* ctx);          // ff.hip
 int prepare_ortho_kernels(edgc_ctx* ctx);       // ortho.hip
 void free_ortho(edgc_ctx* ctx);
+int prepare_embed_kernels(edgc_ctx* ctx);       // embed.hip
+void free_embed(edgc_ctx* ctx);
+void free_qk(edgc_ctx* ctx);                    // qk_norm.hip
 // what the calls that read a list's gradients (and write grad_out) ask of it (grad_norm.hip)
 int check_gradients(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t count, edgc_dtype dtype, bool with_out);
 size_t compress_part_elems(uint64_t max_rows, uint64_t max_cols, uint32_t max_rank, int num_cu);

@@ -1,0 +1,411 @@
+// The embedding of tokens and its gradient.
+//
+//   forward   out[t] = scale table[ids[t] - first], zeros where that is no row of the table
+//   backward  dtable[v] = scale sum of dy[t] over the tokens t with ids[t] - first = v
+//
+// Bounded by memory.  The backward pass sorts the tokens by row, so that a row's gradient is the sum of neighbours, in the tokens' order, and is written
+// once: the same bits for the same tokens, whatever ran before.  k_embed_sort leaves the order and where each row's tokens begin in it, k_embed_sum adds up
+// chunks of the order (a row whose tokens lie in several leaves a part in each) and writes the rows without a token, and k_embed_join adds up the parts.
+#include "row_pack.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace edgc {
+namespace {
+
+constexpr uint32_t kEmbedMaxVocab = 1u << 20, kEmbedMaxHidden = 1u << 20, kEmbedMaxTokens = 1u << 26;
+constexpr int kEmbedUnroll = 4;                         // items of 16 bytes of a row that a lane has at a time
+template <typename T> constexpr uint32_t kEmbedCols = 64u * kEmbedUnroll * Pack<T>::N;      // columns of a wave
+
+struct EmbedArgs {
+    const void* ids;
+    int64_t first;
+    uint64_t tokens;
+    const void* table;                  // forward
+    const void* dy;                     // backward
+    void* out;                          // the tokens' rows, or the table's gradient
+    uint64_t ld_in, ld_out;
+    uint32_t vocab, hidden;
+    float scale;
+    int accumulate;
+};
+
+// Row of a token's id, or one that is not there (2^32 - 1)
+template <typename I>
+__device__ __forceinline__ uint32_t embed_row(const EmbedArgs& a, uint64_t token)
+{
+    const uint64_t r = static_cast<uint64_t>(static_cast<int64_t>(static_cast<const I*>(a.ids)[token])) - static_cast<uint64_t>(a.first);
+    return r < a.vocab ? static_cast<uint32_t>(r) : ~0u;
+}
+
+// A wave takes kEmbedCols columns of a token
+template <typename T, typename I>
+__global__ __launch_bounds__(256) void k_embed_forward(const EmbedArgs a, uint32_t parts)
+{
+    constexpr int N = Pack<T>::N;
+    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+    const uint64_t token = unit / parts;
+    if (token >= a.tokens) return;
+    const uint32_t c0 = static_cast<uint32_t>(unit - token * parts) * kEmbedCols<T> + threadIdx.x % 64 * N, row = embed_row<I>(a, token);
+    const T* const src = static_cast<const T*>(a.table) + row * a.ld_in;
+    T* const dst = static_cast<T*>(a.out) + token * a.ld_out;
+    Pack<T> v[kEmbedUnroll];
+    auto len = [&](int u) { const uint32_t c = c0 + u * 64 * N; return c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u; };
+#pragma unroll
+    for (int u = 0; u < kEmbedUnroll; ++u) {
+        v[u].v = u32x4r{0, 0, 0, 0};
+        if (row != ~0u) v[u].load(src + c0 + u * 64 * N, len(u));
+    }
+#pragma unroll
+    for (int u = 0; u < kEmbedUnroll; ++u) {
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = row != ~0u ? a.scale * v[u].get(i) : 0.f;
+        Pack<T> o;
+        o.set(f);
+        o.store(dst + c0 + u * 64 * N, len(u));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The tokens in the order of their rows
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 2048;      // keys: 128 KB of LDS
+
+// A block has `keys` neighbouring rows of the table and looks at all tokens twice: once to count those of its rows (and those of rows before them, which is
+// where its own begin), once to put them in their places.  A wave has a run of the tokens; the places of a row's tokens in it follow those in the waves
+// before it.
+template <typename I>
+__global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs a, uint32_t keys, uint32_t* order, uint32_t* starts)
+{
+    extern __shared__ uint32_t count[];                 // [kSortWaves][keys], then the first place of each
+    __shared__ uint32_t s_below[kSortWaves], s_scan[kSortWaves];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, row0 = blockIdx.x * keys;
+    const uint64_t per = ((a.tokens + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, t0 = wave * per, t1 = min(a.tokens, t0 + per);
+    for (uint32_t i = tid; i < kSortWaves * keys; i += 64 * kSortWaves) count[i] = 0;
+    __syncthreads();
+    uint32_t below = 0;
+    uint32_t* const mine = count + wave * keys;
+    for (uint64_t t = t0 + lane; t < t1; t += 64) {
+        const uint32_t r = embed_row<I>(a, t);
+        below += r < row0 ? 1u : 0u;
+        if (r != ~0u && r - row0 < keys) atomicAdd(mine + (r - row0), 1u);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
+    if (lane == 0) s_below[wave] = below;
+    __syncthreads();
+    uint32_t base = 0;
+    for (uint32_t w = 0; w < kSortWaves; ++w) base += s_below[w];
+    // first places, a row at a time per thread
+    for (uint32_t k0 = 0; k0 < keys; k0 += 64 * kSortWaves) {
+        const uint32_t k = k0 + tid;
+        uint32_t sum = 0;
+        if (k < keys)
+            for (uint32_t w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = count[w * keys + k];
+                count[w * keys + k] = sum;
+                sum += c;
+            }
+        uint32_t in = sum;                              // inclusive over the wave
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t v = __shfl_up(in, o, 64);
+            if (lane >= static_cast<uint32_t>(o)) in += v;
+        }
+        if (lane == 63) s_scan[wave] = in;
+        __syncthreads();
+        uint32_t before = base, all = 0;
+        for (uint32_t w = 0; w < kSortWaves; ++w) {
+            if (w < wave) before += s_scan[w];
+            all += s_scan[w];
+        }
+        const uint32_t at = before + in - sum;
+        if (k < keys) {
+            for (uint32_t w = 0; w < kSortWaves; ++w) count[w * keys + k] += at;
+            if (row0 + k <= a.vocab) starts[row0 + k] = at;
+        }
+        base += all;
+        __syncthreads();
+    }
+    if (tid == 0 && row0 + keys >= a.vocab && row0 < a.vocab) starts[a.vocab] = base;
+    for (uint64_t t = t0; t < t1; t += 64) {
+        const uint32_t r = t + lane < t1 ? embed_row<I>(a, t + lane) : ~0u, k = r - row0;
+        uint64_t left = __ballot(r != ~0u && k < keys);
+        while (left) {                                  // a row of those that these 64 tokens have at a time
+            const uint32_t key = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
+            const uint64_t same = __ballot(k == key) & left;
+            const uint32_t at = mine[key];
+            if (k == key && (same >> lane & 1)) order[at + __popcll(same & ((1ull << lane) - 1))] = static_cast<uint32_t>(t + lane);
+            __builtin_amdgcn_wave_barrier();
+            if (lane == 0) mine[key] = at + static_cast<uint32_t>(__popcll(same));
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            left &= ~same;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Their sums
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kSumAhead = 8, kZeroRows = 8;        // tokens on their way at a time; rows that a wave looks for tokens of
+enum { kPartHead = 0, kPartTail = 1 };                  // of a row begun in an earlier chunk; of one that goes on in the next
+
+template <typename T>
+__device__ __forceinline__ void embed_write(const EmbedArgs& a, uint32_t row, uint32_t c, uint32_t len, const float (&sum)[Pack<T>::N])
+{
+    constexpr int N = Pack<T>::N;
+    T* const to = static_cast<T*>(a.out) + row * a.ld_out + c;
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = a.scale * sum[i];
+    Pack<T> o;
+    if (a.accumulate) {
+        o.load(to, len);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] += o.get(i);
+    }
+    o.set(f);
+    o.store(to, len);
+}
+template <int N>
+__device__ __forceinline__ float* embed_part(float* part, uint32_t hidden, uint32_t chunk, int which, uint32_t c)
+{
+    const uint64_t ld = (static_cast<uint64_t>(hidden) + 7) / 8 * 8;
+    return part + (static_cast<uint64_t>(chunk) * 2 + which) * ld + c;
+}
+
+// A wave adds up `chunk` neighbours of the order, 64 items of 16 bytes of each; the blocks behind the chunks' write zeros to rows without tokens.
+template <typename T, typename I>
+__global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const uint32_t* order, const uint32_t* starts, float* part, uint32_t chunk, uint32_t chunks,
+                                                   uint32_t parts)
+{
+    constexpr int N = Pack<T>::N;
+    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+    const uint64_t which = unit / parts;
+    const uint32_t c = static_cast<uint32_t>(unit - which * parts) * (64 * N) + threadIdx.x % 64 * N;
+    const uint32_t len = c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u;
+    if (which >= chunks) {
+        if (a.accumulate) return;
+        const uint64_t r0 = (which - chunks) * kZeroRows;
+        const float none[N] = {};
+        for (uint64_t r = r0; r < min(r0 + kZeroRows, static_cast<uint64_t>(a.vocab)); ++r)
+            if (!starts || starts[r] == starts[r + 1]) embed_write<T>(a, static_cast<uint32_t>(r), c, len, none);
+        return;
+    }
+    const uint32_t all = starts[a.vocab], p0 = static_cast<uint32_t>(which) * chunk;
+    if (p0 >= all) return;
+    const uint32_t p1 = min(all, p0 + chunk);
+    uint32_t row = embed_row<I>(a, order[p0]);
+    float sum[N] = {};
+    auto done = [&]() {                                 // with the tokens of `row` in this chunk
+        const uint32_t s0 = starts[row], s1 = starts[row + 1];
+        if (s0 >= p0 && s1 <= p1) {
+            embed_write<T>(a, row, c, len, sum);
+        } else {
+            float* const to = embed_part<N>(part, a.hidden, static_cast<uint32_t>(which), s0 < p0 ? kPartHead : kPartTail, c);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (static_cast<uint32_t>(i) < len) to[i] = sum[i];
+        }
+    };
+    for (uint32_t p = p0; p < p1; p += kSumAhead) {
+        Pack<T> v[kSumAhead];
+        uint32_t rows[kSumAhead];
+#pragma unroll
+        for (uint32_t k = 0; k < kSumAhead; ++k) {
+            if (p + k < p1) {
+                const uint32_t t = order[p + k];
+                rows[k] = embed_row<I>(a, t);
+                v[k].load(static_cast<const T*>(a.dy) + t * a.ld_in + c, len);
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kSumAhead; ++k) {
+            if (p + k < p1) {
+                if (rows[k] != row) {
+                    done();
+                    row = rows[k];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) sum[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += v[k].get(i);
+            }
+        }
+    }
+    done();
+}
+
+// Adds up the parts of a row that begins in a chunk and goes on in the next: a block for every chunk and 64 items of 16 bytes
+template <typename T, typename I>
+__global__ __launch_bounds__(64) void k_embed_join(const EmbedArgs a, const uint32_t* order, const uint32_t* starts, float* part, uint32_t chunk)
+{
+    constexpr int N = Pack<T>::N;
+    const uint32_t k = blockIdx.x, all = starts[a.vocab];
+    if (static_cast<uint64_t>(k + 1) * chunk >= all) return;        // the last one, or none
+    const uint32_t p1 = (k + 1) * chunk, row = embed_row<I>(a, order[p1 - 1]), s0 = starts[row], s1 = starts[row + 1];
+    if (s0 < k * chunk || s1 <= p1) return;
+    const uint32_t c = blockIdx.y * (64 * N) + threadIdx.x * N, len = c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u;
+    float sum[N] = {};
+    auto add = [&](uint32_t at, int which) {
+        const float* const from = embed_part<N>(part, a.hidden, at, which, c);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (static_cast<uint32_t>(i) < len) sum[i] += from[i];
+    };
+    add(k, kPartTail);
+    const uint32_t last = (s1 - 1) / chunk;
+#pragma unroll 8
+    for (uint32_t j = k + 1; j <= last; ++j) add(j, kPartHead);
+    embed_write<T>(a, row, c, len, sum);
+}
+
+// Tokens of a chunk: a few waves for every SIMD of a large batch
+constexpr uint32_t kEmbedChunk = 32;
+
+uint64_t pad256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+struct EmbedPlan {
+    uint64_t order, starts, part, bytes;        // where each begins
+    EmbedPlan(uint64_t tokens, uint64_t vocab, uint64_t hidden)
+    {
+        order = 0;
+        starts = pad256(tokens * 4);
+        part = starts + pad256((vocab + 1) * 4);
+        bytes = part + (tokens + kEmbedChunk - 1) / kEmbedChunk * 2 * ((hidden + 7) / 8 * 8) * 4;
+    }
+};
+
+int check_embed(edgc_ctx* ctx, edgc_dtype dtype, const void* ids, int id_bytes, int64_t first, uint64_t tokens, uint32_t vocab, uint32_t hidden, float scale)
+{
+    if (dtype != EDGC_F32 && dtype != EDGC_BF16) return fail(ctx, EDGC_EINVAL, "unknown dtype");
+    if (id_bytes != 4 && id_bytes != 8) return fail(ctx, EDGC_EINVAL, "ids have 4 or 8 bytes");
+    if (vocab == 0 || hidden == 0 || vocab > kEmbedMaxVocab || hidden > kEmbedMaxHidden) return fail(ctx, EDGC_EINVAL, "vocab and hidden must be 1 to 2^20");
+    if (tokens > kEmbedMaxTokens) return fail(ctx, EDGC_EINVAL, "more than 2^26 tokens");
+    if (first > (1ll << 62) || first < -(1ll << 62)) return fail(ctx, EDGC_EINVAL, "first_id beyond 2^62");
+    if (!std::isfinite(scale)) return fail(ctx, EDGC_EINVAL, "scale must be finite");
+    if (tokens && (!ids || !aligned_to(ids, static_cast<size_t>(id_bytes)))) return fail(ctx, EDGC_EINVAL, "null or misaligned ids");
+    return EDGC_OK;
+}
+int check_embed_rows(edgc_ctx* ctx, edgc_dtype dtype, const void* p, uint64_t ld, uint32_t hidden)
+{
+    if (!p || !aligned_to(p, dtype == EDGC_F32 ? 4 : 2)) return fail(ctx, EDGC_EINVAL, "null or misaligned pointer");
+    if (ld < hidden || ld > kMaxSpan) return fail(ctx, EDGC_EINVAL, "leading dimension too small, or over 2^40");
+    return EDGC_OK;
+}
+
+}  // namespace
+
+int prepare_embed_kernels(edgc_ctx* ctx)
+{
+    for (const void* f : {reinterpret_cast<const void*>(&k_embed_sort<int32_t>), reinterpret_cast<const void*>(&k_embed_sort<int64_t>)})
+        EDGC_HIP_TRY(ctx, hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * kSortMaxKeys * 4));
+    return EDGC_OK;
+}
+
+void free_embed(edgc_ctx* ctx)
+{
+    if (ctx->embed.ws) (void)hipFree(ctx->embed.ws);
+    ctx->embed = EmbedScratch{};
+}
+
+}  // namespace edgc
+
+using namespace edgc;
+
+extern "C" int edgc_embed_forward(edgc_ctx* ctx, edgc_dtype dtype, const void* table, uint64_t ld_table, uint32_t vocab, uint32_t hidden, const void* ids,
+                                  int id_bytes, int64_t first_id, uint64_t tokens, float scale, void* out, uint64_t ld_out, void* hip_stream)
+{
+    if (!ctx) return EDGC_EINVAL;
+    if (int rc = check_embed(ctx, dtype, ids, id_bytes, first_id, tokens, vocab, hidden, scale)) return rc;
+    if (tokens == 0) return EDGC_OK;
+    if (int rc = check_embed_rows(ctx, dtype, table, ld_table, hidden)) return rc;
+    if (int rc = check_embed_rows(ctx, dtype, out, ld_out, hidden)) return rc;
+    EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    EmbedArgs a{};
+    a.ids = ids; a.first = first_id; a.tokens = tokens; a.table = table; a.out = out; a.ld_in = ld_table; a.ld_out = ld_out;
+    a.vocab = vocab; a.hidden = hidden; a.scale = scale;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    auto go = [&](auto type, auto id) -> int {
+        using T = decltype(type);
+        const uint32_t parts = (hidden + kEmbedCols<T> - 1) / kEmbedCols<T>;
+        const uint64_t blocks = (tokens * parts + 3) / 4;
+        if (blocks > 0x7fffffffull) return fail(ctx, EDGC_EINVAL, "tokens x hidden too large for one call");
+        EDGC_LAUNCH(ctx, st, KID_EMBED_FORWARD, 2.0 * sizeof(T) * tokens * hidden, 0.0,
+                    k_embed_forward<T, decltype(id)><<<static_cast<uint32_t>(blocks), 256, 0, st>>>(a, parts));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        return EDGC_OK;
+    };
+    if (dtype == EDGC_F32) return id_bytes == 8 ? go(float{}, int64_t{}) : go(float{}, int32_t{});
+    return id_bytes == 8 ? go(__bf16{}, int64_t{}) : go(__bf16{}, int32_t{});
+}
+
+extern "C" int edgc_reserve_embed(edgc_ctx* ctx, uint32_t tokens, uint32_t vocab, uint32_t hidden)
+{
+    if (!ctx) return EDGC_EINVAL;
+    if (vocab == 0 || hidden == 0 || vocab > kEmbedMaxVocab || hidden > kEmbedMaxHidden || tokens > kEmbedMaxTokens)
+        return fail(ctx, EDGC_EINVAL, "vocab and hidden must be 1 to 2^20, tokens at most 2^26");
+    EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    const uint64_t need = tokens ? EmbedPlan(tokens, vocab, hidden).bytes : 0;
+    if (need && need <= ctx->embed.held) {
+        ctx->embed.bytes = need;
+        return EDGC_OK;
+    }
+    EDGC_HIP_TRY(ctx, hipDeviceSynchronize());          // nothing may still be using the old scratch
+    free_embed(ctx);
+    if (need == 0) return EDGC_OK;
+    if (hipMalloc(&ctx->embed.ws, need) != hipSuccess) {
+        (void)hipGetLastError();
+        ctx->embed = EmbedScratch{};
+        return fail(ctx, EDGC_ENOMEM, "embedding scratch allocation failed");
+    }
+    ctx->embed.bytes = ctx->embed.held = need;
+    return EDGC_OK;
+}
+
+extern "C" int edgc_embed_backward(edgc_ctx* ctx, edgc_dtype dtype, const void* ids, int id_bytes, int64_t first_id, uint64_t tokens, const void* dy,
+                                   uint64_t ld_dy, uint32_t vocab, uint32_t hidden, float scale, void* dtable, uint64_t ld_dtable, int accumulate,
+                                   void* hip_stream)
+{
+    if (!ctx) return EDGC_EINVAL;
+    if (int rc = check_embed(ctx, dtype, ids, id_bytes, first_id, tokens, vocab, hidden, scale)) return rc;
+    if (int rc = check_embed_rows(ctx, dtype, dtable, ld_dtable, hidden)) return rc;
+    if (tokens)
+        if (int rc = check_embed_rows(ctx, dtype, dy, ld_dy, hidden)) return rc;
+    if (tokens == 0 && accumulate) return EDGC_OK;
+    const EmbedPlan plan(tokens, vocab, hidden);
+    if (tokens && plan.bytes > ctx->embed.bytes) return fail(ctx, EDGC_EINVAL, "larger than what edgc_reserve_embed was called for");
+    EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
+    EmbedArgs a{};
+    a.ids = ids; a.first = first_id; a.tokens = tokens; a.dy = dy; a.out = dtable; a.ld_in = ld_dy; a.ld_out = ld_dtable;
+    a.vocab = vocab; a.hidden = hidden; a.scale = scale; a.accumulate = accumulate;
+    unsigned char* const ws = static_cast<unsigned char*>(ctx->embed.ws);
+    uint32_t *const order = reinterpret_cast<uint32_t*>(ws + plan.order), *const starts = reinterpret_cast<uint32_t*>(ws + plan.starts);
+    float* const part = reinterpret_cast<float*>(ws + plan.part);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    auto go = [&](auto type, auto id) -> int {
+        using T = decltype(type);
+        using I = decltype(id);
+        const uint32_t keys = std::min((vocab + kSortBlocks - 1) / kSortBlocks, kSortMaxKeys), sorts = (vocab + keys - 1) / keys;
+        if (tokens)
+            EDGC_LAUNCH(ctx, st, KID_EMBED_SORT, 2.0 * sizeof(I) * tokens * sorts, 0.0,
+                    k_embed_sort<I><<<sorts, 64 * kSortWaves, kSortWaves * keys * 4, st>>>(a, keys, order, starts));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        const uint32_t cols = 64 * Pack<T>::N, parts = (hidden + cols - 1) / cols, chunks = static_cast<uint32_t>((tokens + kEmbedChunk - 1) / kEmbedChunk);
+        const uint64_t zeros = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows, blocks = ((chunks + zeros) * parts + 3) / 4;
+        if (blocks > 0x7fffffffull) return fail(ctx, EDGC_EINVAL, "tokens x hidden too large for one call");
+        EDGC_LAUNCH(ctx, st, KID_EMBED_SUM, static_cast<double>(sizeof(T)) * hidden * (static_cast<double>(tokens) + vocab), 0.0,
+                    k_embed_sum<T, I><<<static_cast<uint32_t>(blocks), 256, 0, st>>>(a, order, tokens ? starts : nullptr, part, kEmbedChunk, chunks, parts));
+        EDGC_HIP_TRY(ctx, hipGetLastError());
+        if (chunks > 1) {
+            EDGC_LAUNCH(ctx, st, KID_EMBED_JOIN, 0.0, 0.0, k_embed_join<T, I><<<dim3(chunks - 1, parts), 64, 0, st>>>(a, order, starts, part, kEmbedChunk));
+            EDGC_HIP_TRY(ctx, hipGetLastError());
+        }
+        return EDGC_OK;
+    };
+    if (dtype == EDGC_F32) return id_bytes == 8 ? go(float{}, int64_t{}) : go(float{}, int32_t{});
+    return id_bytes == 8 ? go(__bf16{}, int64_t{}) : go(__bf16{}, int32_t{});
+}

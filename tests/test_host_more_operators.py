@@ -62,3 +62,85 @@ def test_tiles_of_a_symmetric_output_begin_inside_it_and_cover_its_lower_half_on
     for (n, bm, bn), at in seen.items():
         # every tile that has a square of 32 on or below the diagonal, and no other
         assert at == {(m, c) for m in range(0, n, bm) for c in range(0, n, bn) if c < m + bm}, (n, bm, bn)
+
+
+def _meta(*shape, dtype=torch.float32):
+    return torch.empty(shape, device="meta", dtype=dtype)
+
+
+def test_tensors_that_the_gpu_cannot_read_are_refused():
+    """Host memory, or another GPU's, is not handed to a kernel."""
+    c = _no_context()
+    table, ids, out = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64), torch.zeros(3, 8)
+    with pytest.raises(ValueError, match="device"):
+        c.embed_forward(table, ids, out, stream=STREAM)
+    with pytest.raises(ValueError, match="device"):
+        c.embed_backward(ids, out, table, stream=STREAM)
+    q, w = torch.zeros(3, 2, 8), torch.ones(8)
+    with pytest.raises(ValueError, match="device"):
+        c.qk_norm_forward(q, None, w, None, None, None, q, None, stream=STREAM)
+    with pytest.raises(ValueError, match="device"):
+        c.qk_norm_backward(q, None, q, None, w, None, None, None, q, None, w, None, stream=STREAM)
+
+
+def test_embed_without_a_context_and_with_what_it_does_not_take():
+    L = edgc.load_library()
+    assert L.edgc_embed_forward(None, 0, None, 0, 1, 1, None, 8, 0, 0, 1.0, None, 0, None) == b.EINVAL
+    assert L.edgc_reserve_embed(None, 1, 1, 1) == b.EINVAL
+    assert L.edgc_embed_backward(None, 0, None, 8, 0, 0, None, 0, 1, 1, 1.0, None, 0, 0, None) == b.EINVAL
+    c = _no_context()
+    c.device = -1                                           # (host tensors count as the context's)
+    table, ids, out = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64), torch.zeros(3, 8)
+    with pytest.raises(edgc.EdgcError):                     # what fits is handed on
+        c.embed_forward(table, ids, out, stream=STREAM)
+    with pytest.raises(edgc.EdgcError):
+        c.embed_backward(ids.int(), out, table, stream=STREAM)
+    for bad in (ids.double(), ids.short(), ids.bool()):
+        with pytest.raises(TypeError, match="ids"):
+            c.embed_forward(table, bad, out, stream=STREAM)
+    with pytest.raises(ValueError, match="ids"):
+        c.embed_forward(table, torch.zeros(3, 2, dtype=torch.int64)[:, 0], out, stream=STREAM)
+    with pytest.raises(ValueError, match="ids"):
+        c.embed_forward(table, ids.view(3, 1), out, stream=STREAM)
+    with pytest.raises(ValueError, match="out"):
+        c.embed_forward(table, ids, torch.zeros(4, 8), stream=STREAM)
+    with pytest.raises(TypeError, match="out"):
+        c.embed_forward(table, ids, out.bfloat16(), stream=STREAM)
+    with pytest.raises(ValueError, match="dy"):
+        c.embed_backward(ids, torch.zeros(8, 3).t(), table, stream=STREAM)
+    with pytest.raises(ValueError, match="first_id"):
+        c.embed_forward(table, ids, out, first_id=2 ** 63, stream=STREAM)
+    with pytest.raises(TypeError):
+        c.embed_forward(table.double(), ids, out.double(), stream=STREAM)
+    for sizes in ((2 ** 32 + 1, 4, 4), (4, 2 ** 32 + 1, 4), (4, 4, 2 ** 32 + 1), (-1, 4, 4)):
+        with pytest.raises(ValueError, match="2\\^32"):
+            c.reserve_embed(*sizes)
+    with pytest.raises(ValueError, match="2\\^32"):
+        c.embed_forward(_meta(2 ** 32 + 1, 8), ids, out, stream=STREAM)
+
+
+def test_qk_norm_without_a_context_and_with_what_it_does_not_take():
+    L = edgc.load_library()
+    assert L.edgc_reserve_qk_norm(None, 1, 1, 1, 1) == b.EINVAL
+    assert L.edgc_qk_norm_forward(None, 0, 0, 1, 0, 1, *[None] * 5, 8, None, 0, 0, 0.0, None, None, None) == b.EINVAL
+    assert L.edgc_qk_norm_backward(None, 0, 0, 1, 0, 1, *[None] * 7, 8, None, 0, 0, 0.0, *[None] * 5) == b.EINVAL
+    c = _no_context()
+    c.device = -1
+    q, k, w, pos, f = torch.zeros(3, 4, 8), torch.zeros(3, 2, 8), torch.ones(8), torch.arange(3), torch.ones(4, dtype=torch.float64)
+    with pytest.raises(edgc.EdgcError):                     # what fits is handed on
+        c.qk_norm_forward(q, k, w, w, pos, f, q, k, stream=STREAM)
+    with pytest.raises(edgc.EdgcError):
+        c.qk_norm_forward(q, None, w, None, None, None, q, None, stream=STREAM)
+    fwd = lambda *a: c.qk_norm_forward(*a, stream=STREAM)
+    for bad, kind in (((q, k, w, w, pos, f.float(), q, k), TypeError), ((q, k, w, w, pos.double(), f, q, k), TypeError), ((q, k, w, w, pos[:2], f, q, k), ValueError),
+                      ((q, k, w, w, None, f, q, k), ValueError), ((q, k, w, None, pos, f, q, k), ValueError), ((q, k, w, w, pos, f, q, None), ValueError),
+                      ((q, None, w, None, pos, f, q, k), ValueError), ((q, k, w[:7], w, pos, f, q, k), ValueError), ((q, k, w, w.bfloat16(), pos, f, q, k), TypeError),
+                      ((q, k.bfloat16(), w, w, pos, f, q, k), TypeError), ((q, torch.zeros(2, 2, 8), w, w, pos, f, q, k), ValueError),
+                      ((q, k, w, w, pos, f, torch.zeros(3, 8, 4).transpose(1, 2), k), ValueError), ((q[0], k, w, w, pos, f, q, k), ValueError)):
+        with pytest.raises(kind):
+            fwd(*bad)
+    with pytest.raises(ValueError):
+        c.qk_norm_backward(q, k, q, k, w, w, pos, f, q, k, w, torch.ones(16)[::2], stream=STREAM)
+    for sizes in ((2 ** 32 + 1, 4, 4, 4), (4, 2 ** 32 + 1, 4, 4), (4, 4, -1, 4), (4, 4, 4, 2 ** 32 + 1)):
+        with pytest.raises(ValueError, match="2\\^32"):
+            c.reserve_qk_norm(*sizes)
