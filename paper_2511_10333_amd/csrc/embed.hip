@@ -71,7 +71,8 @@ __global__ __launch_bounds__(256) void k_embed_forward(const EmbedArgs a, uint32
 // ---------------------------------------------------------------------------------------------
 // The tokens in the order of their rows
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 2048;      // keys: 128 KB of LDS
+constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 2048,      // keys: 128 KB of LDS
+                   kSortAhead = 16;             // tokens of a lane on their way at a time
 
 // A block has `keys` neighbouring rows of the table and looks at all tokens twice: once to count those of its rows (and those of rows before them, which is
 // where its own begin), once to put them in their places.  A wave has a run of the tokens; the places of a row's tokens in it follow those in the waves
@@ -87,10 +88,19 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
     __syncthreads();
     uint32_t below = 0;
     uint32_t* const mine = count + wave * keys;
-    for (uint64_t t = t0 + lane; t < t1; t += 64) {
-        const uint32_t r = embed_row<I>(a, t);
-        below += r < row0 ? 1u : 0u;
-        if (r != ~0u && r - row0 < keys) atomicAdd(mine + (r - row0), 1u);
+    uint32_t rows[kSortAhead];
+    // rows of kSortAhead x 64 tokens, from t on
+    auto look = [&](uint64_t t) {
+#pragma unroll
+        for (uint32_t i = 0; i < kSortAhead; ++i) rows[i] = t + i * 64 + lane < t1 ? embed_row<I>(a, t + i * 64 + lane) : ~0u;
+    };
+    for (uint64_t t = t0; t < t1; t += kSortAhead * 64) {
+        look(t);
+#pragma unroll
+        for (uint32_t i = 0; i < kSortAhead; ++i) {
+            below += rows[i] < row0 ? 1u : 0u;
+            if (rows[i] != ~0u && rows[i] - row0 < keys) atomicAdd(mine + (rows[i] - row0), 1u);
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
@@ -130,20 +140,28 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
         __syncthreads();
     }
     if (tid == 0 && row0 + keys >= a.vocab && row0 < a.vocab) starts[a.vocab] = base;
-    for (uint64_t t = t0; t < t1; t += 64) {
-        const uint32_t r = t + lane < t1 ? embed_row<I>(a, t + lane) : ~0u, k = r - row0;
-        uint64_t left = __ballot(r != ~0u && k < keys);
-        while (left) {                                  // a row of those that these 64 tokens have at a time
-            const uint32_t key = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
-            const uint64_t same = __ballot(k == key) & left;
-            const uint32_t at = mine[key];
-            if (k == key && (same >> lane & 1)) order[at + __popcll(same & ((1ull << lane) - 1))] = static_cast<uint32_t>(t + lane);
-            __builtin_amdgcn_wave_barrier();
-            if (lane == 0) mine[key] = at + static_cast<uint32_t>(__popcll(same));
+    const uint32_t bits = 32 - __builtin_clz(keys);
+    const uint64_t before = (1ull << lane) - 1;
+    for (uint64_t t = t0; t < t1; t += kSortAhead * 64) {
+        if (t1 - t0 > kSortAhead * 64) look(t);         // (else they are there still)
+#pragma unroll
+        for (uint32_t i = 0; i < kSortAhead; ++i) {
+            const uint32_t k = rows[i] - row0;
+            const bool ours = rows[i] != ~0u && k < keys;
+            uint64_t same = __ballot(ours);
+            if (same == 0) continue;
+            for (uint32_t bit = 0; bit < bits; ++bit) { // the lanes that have a token of the same row
+                const uint64_t set = __ballot(k >> bit & 1);
+                same &= k >> bit & 1 ? set : ~set;
+            }
+            if (ours) {
+                const uint32_t at = mine[k];
+                order[at + __popcll(same & before)] = static_cast<uint32_t>(t + i * 64 + lane);
+                if ((same & before) == 0) mine[k] = at + static_cast<uint32_t>(__popcll(same));
+            }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            left &= ~same;
         }
     }
 }
@@ -151,7 +169,8 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
 // ---------------------------------------------------------------------------------------------
 // Their sums
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kSumAhead = 8, kZeroRows = 8;        // tokens on their way at a time; rows that a wave looks for tokens of
+constexpr uint32_t kEmbedChunk = 32, kSumAhead = 8;     // tokens of a wave; on their way at a time
+constexpr uint32_t kZeroRows = 8;                       // rows that a wave looks for tokens of
 enum { kPartHead = 0, kPartTail = 1 };                  // of a row begun in an earlier chunk; of one that goes on in the next
 
 template <typename T>
@@ -171,101 +190,102 @@ __device__ __forceinline__ void embed_write(const EmbedArgs& a, uint32_t row, ui
     o.set(f);
     o.store(to, len);
 }
+// A wave's share of a part: rows of `hidden` padded to the columns of whole waves, so that it is stored and loaded whole
+__host__ __device__ inline uint64_t embed_part_ld(uint32_t hidden) { return (static_cast<uint64_t>(hidden) + 511) / 512 * 512; }
 template <int N>
-__device__ __forceinline__ float* embed_part(float* part, uint32_t hidden, uint32_t chunk, int which, uint32_t c)
+__device__ __forceinline__ float4* embed_part(float* part, uint32_t hidden, uint32_t chunk, int which, uint32_t c)
 {
-    const uint64_t ld = (static_cast<uint64_t>(hidden) + 7) / 8 * 8;
-    return part + (static_cast<uint64_t>(chunk) * 2 + which) * ld + c;
+    return reinterpret_cast<float4*>(part + (static_cast<uint64_t>(chunk) * 2 + which) * embed_part_ld(hidden) + c);
 }
 
-// A wave adds up `chunk` neighbours of the order, 64 items of 16 bytes of each; the blocks behind the chunks' write zeros to rows without tokens.
+struct EmbedWork {
+    const uint32_t *order, *starts;     // starts null: no tokens
+    float* part;
+    uint32_t chunks, zeros, parts;      // of the order; groups of rows that may be without tokens; of a row
+};
+
+// A wave adds up a chunk of the order, 64 items of 16 bytes of each, or writes zeros to those of a group of rows that have no token.  Chunks and groups take
+// turns, so that reading and writing go on at the same time.
 template <typename T, typename I>
-__global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const uint32_t* order, const uint32_t* starts, float* part, uint32_t chunk, uint32_t chunks,
-                                                   uint32_t parts)
+__global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const EmbedWork w)
 {
     constexpr int N = Pack<T>::N;
-    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
-    const uint64_t which = unit / parts;
-    const uint32_t c = static_cast<uint32_t>(unit - which * parts) * (64 * N) + threadIdx.x % 64 * N;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t unit = static_cast<uint64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t which = static_cast<uint32_t>(unit / w.parts), total = w.chunks + w.zeros;
+    if (which >= total) return;
+    const uint32_t c = static_cast<uint32_t>(unit - static_cast<uint64_t>(which) * w.parts) * (64 * N) + lane * N;
     const uint32_t len = c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u;
-    if (which >= chunks) {
-        if (a.accumulate) return;
-        const uint64_t r0 = (which - chunks) * kZeroRows;
+    const uint32_t every = w.chunks ? total / w.chunks : 0u, turn = every ? which / every : 0u;
+    if (!every || which % every || turn >= w.chunks) {
+        const uint32_t r0 = (which - (every ? min(w.chunks, turn + 1) : 0u)) * kZeroRows, r = r0 + lane;
+        uint64_t empty = __ballot(lane < kZeroRows && r < a.vocab && (!w.starts || w.starts[r] == w.starts[r + 1]));
         const float none[N] = {};
-        for (uint64_t r = r0; r < min(r0 + kZeroRows, static_cast<uint64_t>(a.vocab)); ++r)
-            if (!starts || starts[r] == starts[r + 1]) embed_write<T>(a, static_cast<uint32_t>(r), c, len, none);
+        for (; empty; empty &= empty - 1) embed_write<T>(a, r0 + __builtin_ctzll(empty), c, len, none);
         return;
     }
-    const uint32_t all = starts[a.vocab], p0 = static_cast<uint32_t>(which) * chunk;
+    // lane l: token l - 1 of the chunk, so that the neighbours on both sides are there
+    const uint32_t all = w.starts[a.vocab], p0 = turn * kEmbedChunk;
     if (p0 >= all) return;
-    const uint32_t p1 = min(all, p0 + chunk);
-    uint32_t row = embed_row<I>(a, order[p0]);
+    const uint32_t n = min(all - p0, kEmbedChunk);
+    static_assert(kEmbedChunk + 2 <= 64, "");
+    const bool there = lane <= n + 1 && p0 + lane > 0 && p0 + lane - 1 < all;
+    const uint32_t token = there ? w.order[p0 + lane - 1] : 0u, row = there ? embed_row<I>(a, token) : ~0u;
+    auto row_of = [&](uint32_t k) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(row, k)); };       // (lanes)
     float sum[N] = {};
-    auto done = [&]() {                                 // with the tokens of `row` in this chunk
-        const uint32_t s0 = starts[row], s1 = starts[row + 1];
-        if (s0 >= p0 && s1 <= p1) {
-            embed_write<T>(a, row, c, len, sum);
-        } else {
-            float* const to = embed_part<N>(part, a.hidden, static_cast<uint32_t>(which), s0 < p0 ? kPartHead : kPartTail, c);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (static_cast<uint32_t>(i) < len) to[i] = sum[i];
-        }
-    };
-    for (uint32_t p = p0; p < p1; p += kSumAhead) {
+    bool open = row_of(0) == row_of(1);                 // begun in an earlier chunk
+    for (uint32_t k0 = 1; k0 <= n; k0 += kSumAhead) {
         Pack<T> v[kSumAhead];
-        uint32_t rows[kSumAhead];
+#pragma unroll
+        for (uint32_t k = 0; k < kSumAhead; ++k)
+            if (k0 + k <= n) v[k].load(static_cast<const T*>(a.dy) + static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(token, k0 + k))) * a.ld_in + c, len);
 #pragma unroll
         for (uint32_t k = 0; k < kSumAhead; ++k) {
-            if (p + k < p1) {
-                const uint32_t t = order[p + k];
-                rows[k] = embed_row<I>(a, t);
-                v[k].load(static_cast<const T*>(a.dy) + t * a.ld_in + c, len);
+            if (k0 + k > n) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] += v[k].get(i);
+            const uint32_t mine = row_of(k0 + k);
+            const bool more = row_of(k0 + k + 1) == mine;
+            if (more && k0 + k < n) continue;
+            if (!open && !more) {
+                embed_write<T>(a, mine, c, len, sum);
+            } else {
+                float4* const to = embed_part<N>(w.part, a.hidden, turn, open ? kPartHead : kPartTail, c);
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) to[i] = float4{sum[4 * i], sum[4 * i + 1], sum[4 * i + 2], sum[4 * i + 3]};
             }
-        }
+            open = false;
 #pragma unroll
-        for (uint32_t k = 0; k < kSumAhead; ++k) {
-            if (p + k < p1) {
-                if (rows[k] != row) {
-                    done();
-                    row = rows[k];
-#pragma unroll
-                    for (int i = 0; i < N; ++i) sum[i] = 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] += v[k].get(i);
-            }
+            for (int i = 0; i < N; ++i) sum[i] = 0.f;
         }
     }
-    done();
 }
 
-// Adds up the parts of a row that begins in a chunk and goes on in the next: a block for every chunk and 64 items of 16 bytes
+// Adds up the parts of a row that begins in a chunk and goes on in the next: a wave for every chunk and 64 items of 16 bytes
 template <typename T, typename I>
-__global__ __launch_bounds__(64) void k_embed_join(const EmbedArgs a, const uint32_t* order, const uint32_t* starts, float* part, uint32_t chunk)
+__global__ __launch_bounds__(64) void k_embed_join(const EmbedArgs a, const EmbedWork w)
 {
     constexpr int N = Pack<T>::N;
-    const uint32_t k = blockIdx.x, all = starts[a.vocab];
-    if (static_cast<uint64_t>(k + 1) * chunk >= all) return;        // the last one, or none
-    const uint32_t p1 = (k + 1) * chunk, row = embed_row<I>(a, order[p1 - 1]), s0 = starts[row], s1 = starts[row + 1];
-    if (s0 < k * chunk || s1 <= p1) return;
+    const uint32_t k = blockIdx.x, all = w.starts[a.vocab], p1 = (k + 1) * kEmbedChunk;
+    if (p1 >= all) return;                              // the last one, or none
+    const uint32_t row = embed_row<I>(a, w.order[p1 - 1]), s0 = w.starts[row], s1 = w.starts[row + 1];
+    if (s0 < k * kEmbedChunk || s1 <= p1) return;
     const uint32_t c = blockIdx.y * (64 * N) + threadIdx.x * N, len = c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u;
     float sum[N] = {};
     auto add = [&](uint32_t at, int which) {
-        const float* const from = embed_part<N>(part, a.hidden, at, which, c);
+        const float4* const from = embed_part<N>(w.part, a.hidden, at, which, c);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (static_cast<uint32_t>(i) < len) sum[i] += from[i];
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 v = from[i];
+            sum[4 * i] += v.x; sum[4 * i + 1] += v.y; sum[4 * i + 2] += v.z; sum[4 * i + 3] += v.w;
+        }
     };
     add(k, kPartTail);
-    const uint32_t last = (s1 - 1) / chunk;
+    const uint32_t last = (s1 - 1) / kEmbedChunk;
 #pragma unroll 8
     for (uint32_t j = k + 1; j <= last; ++j) add(j, kPartHead);
     embed_write<T>(a, row, c, len, sum);
 }
-
-// Tokens of a chunk: a few waves for every SIMD of a large batch
-constexpr uint32_t kEmbedChunk = 32;
 
 uint64_t pad256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 struct EmbedPlan {
@@ -275,7 +295,7 @@ struct EmbedPlan {
         order = 0;
         starts = pad256(tokens * 4);
         part = starts + pad256((vocab + 1) * 4);
-        bytes = part + (tokens + kEmbedChunk - 1) / kEmbedChunk * 2 * ((hidden + 7) / 8 * 8) * 4;
+        bytes = part + (tokens + kEmbedChunk - 1) / kEmbedChunk * 2 * embed_part_ld(static_cast<uint32_t>(hidden)) * 4;
     }
 };
 
@@ -394,14 +414,16 @@ extern "C" int edgc_embed_backward(edgc_ctx* ctx, edgc_dtype dtype, const void* 
             EDGC_LAUNCH(ctx, st, KID_EMBED_SORT, 2.0 * sizeof(I) * tokens * sorts, 0.0,
                     k_embed_sort<I><<<sorts, 64 * kSortWaves, kSortWaves * keys * 4, st>>>(a, keys, order, starts));
         EDGC_HIP_TRY(ctx, hipGetLastError());
-        const uint32_t cols = 64 * Pack<T>::N, parts = (hidden + cols - 1) / cols, chunks = static_cast<uint32_t>((tokens + kEmbedChunk - 1) / kEmbedChunk);
-        const uint64_t zeros = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows, blocks = ((chunks + zeros) * parts + 3) / 4;
+        const uint32_t cols = 64 * Pack<T>::N;
+        EmbedWork w{order, tokens ? starts : nullptr, part, static_cast<uint32_t>((tokens + kEmbedChunk - 1) / kEmbedChunk),
+                    accumulate ? 0u : (vocab + kZeroRows - 1) / kZeroRows, (hidden + cols - 1) / cols};
+        const uint64_t blocks = ((static_cast<uint64_t>(w.chunks) + w.zeros) * w.parts + 3) / 4;
         if (blocks > 0x7fffffffull) return fail(ctx, EDGC_EINVAL, "tokens x hidden too large for one call");
         EDGC_LAUNCH(ctx, st, KID_EMBED_SUM, static_cast<double>(sizeof(T)) * hidden * (static_cast<double>(tokens) + vocab), 0.0,
-                    k_embed_sum<T, I><<<static_cast<uint32_t>(blocks), 256, 0, st>>>(a, order, tokens ? starts : nullptr, part, kEmbedChunk, chunks, parts));
+                    k_embed_sum<T, I><<<static_cast<uint32_t>(blocks), 256, 0, st>>>(a, w));
         EDGC_HIP_TRY(ctx, hipGetLastError());
-        if (chunks > 1) {
-            EDGC_LAUNCH(ctx, st, KID_EMBED_JOIN, 0.0, 0.0, k_embed_join<T, I><<<dim3(chunks - 1, parts), 64, 0, st>>>(a, order, starts, part, kEmbedChunk));
+        if (w.chunks > 1) {
+            EDGC_LAUNCH(ctx, st, KID_EMBED_JOIN, 0.0, 0.0, k_embed_join<T, I><<<dim3(w.chunks - 1, w.parts), 64, 0, st>>>(a, w));
             EDGC_HIP_TRY(ctx, hipGetLastError());
         }
         return EDGC_OK;
