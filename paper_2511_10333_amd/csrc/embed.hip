@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void k_embed_forward(const EmbedArgs a, uint32
 // ---------------------------------------------------------------------------------------------
 // The tokens in the order of their rows
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 2048,      // keys: 128 KB of LDS
+constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 512,       // keys: 96 KB of LDS
                    kSortAhead = 16;             // tokens of a lane on their way at a time
 
 // A block has `keys` neighbouring rows of the table and looks at all tokens twice: once to count those of its rows (and those of rows before them, which is
@@ -80,11 +80,11 @@ constexpr uint32_t kSortBlocks = 256, kSortWaves = 16, kSortMaxKeys = 2048,     
 template <typename I>
 __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs a, uint32_t keys, uint32_t* order, uint32_t* starts)
 {
-    extern __shared__ uint32_t count[];                 // [kSortWaves][keys], then the first place of each
+    extern __shared__ uint32_t count[];                 // [kSortWaves][keys], then the first place of each; and as many sets of lanes
     __shared__ uint32_t s_below[kSortWaves], s_scan[kSortWaves];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, row0 = blockIdx.x * keys;
     const uint64_t per = ((a.tokens + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, t0 = wave * per, t1 = min(a.tokens, t0 + per);
-    for (uint32_t i = tid; i < kSortWaves * keys; i += 64 * kSortWaves) count[i] = 0;
+    for (uint32_t i = tid; i < 3 * kSortWaves * keys; i += 64 * kSortWaves) count[i] = 0;
     __syncthreads();
     uint32_t below = 0;
     uint32_t* const mine = count + wave * keys;
@@ -140,7 +140,14 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
         __syncthreads();
     }
     if (tid == 0 && row0 + keys >= a.vocab && row0 < a.vocab) starts[a.vocab] = base;
-    const uint32_t bits = 32 - __builtin_clz(keys);
+    // Which lanes of a wave have a token of the same row they find in LDS, where each leaves its bit.  (Comparing the rows' bits one after the other, ballots of
+    // the wave, took the block with the most frequent words 18 us instead of 11.)
+    auto wave_sync = [] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    uint32_t* const sets = count + kSortWaves * keys + wave * keys * 2;
     const uint64_t before = (1ull << lane) - 1;
     for (uint64_t t = t0; t < t1; t += kSortAhead * 64) {
         if (t1 - t0 > kSortAhead * 64) look(t);         // (else they are there still)
@@ -148,20 +155,24 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
         for (uint32_t i = 0; i < kSortAhead; ++i) {
             const uint32_t k = rows[i] - row0;
             const bool ours = rows[i] != ~0u && k < keys;
-            uint64_t same = __ballot(ours);
-            if (same == 0) continue;
-            for (uint32_t bit = 0; bit < bits; ++bit) { // the lanes that have a token of the same row
-                const uint64_t set = __ballot(k >> bit & 1);
-                same &= k >> bit & 1 ? set : ~set;
-            }
+            if (__ballot(ours) == 0) continue;
+            if (ours) atomicOr(sets + 2 * k + lane / 32, 1u << (lane & 31));
+            wave_sync();
+            uint64_t same = 0;
+            uint32_t at = 0;
             if (ours) {
-                const uint32_t at = mine[k];
-                order[at + __popcll(same & before)] = static_cast<uint32_t>(t + i * 64 + lane);
-                if ((same & before) == 0) mine[k] = at + static_cast<uint32_t>(__popcll(same));
+                same = sets[2 * k] | static_cast<uint64_t>(sets[2 * k + 1]) << 32;
+                at = mine[k];
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            wave_sync();
+            if (ours) {
+                order[at + __popcll(same & before)] = static_cast<uint32_t>(t + i * 64 + lane);
+                if ((same & before) == 0) {
+                    mine[k] = at + static_cast<uint32_t>(__popcll(same));
+                    sets[2 * k] = sets[2 * k + 1] = 0;
+                }
+            }
+            wave_sync();
         }
     }
 }
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
 // ---------------------------------------------------------------------------------------------
 // Their sums
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kEmbedChunk = 32, kSumAhead = 8;     // tokens of a wave; on their way at a time
+constexpr uint32_t kEmbedChunk = 32, kSumAhead = 8;     // tokens of a wave at most; on their way at a time
 constexpr uint32_t kZeroRows = 8;                       // rows that a wave looks for tokens of
 enum { kPartHead = 0, kPartTail = 1 };                  // of a row begun in an earlier chunk; of one that goes on in the next
 
@@ -201,7 +212,7 @@ __device__ __forceinline__ float4* embed_part(float* part, uint32_t hidden, uint
 struct EmbedWork {
     const uint32_t *order, *starts;     // starts null: no tokens
     float* part;
-    uint32_t chunks, zeros, parts;      // of the order; groups of rows that may be without tokens; of a row
+    uint32_t chunk, chunks, zeros, parts;       // tokens of a wave; those of the order, groups of rows that may be without tokens, both; waves of a row
 };
 
 // A wave adds up a chunk of the order, 64 items of 16 bytes of each, or writes zeros to those of a group of rows that have no token.  Chunks and groups take
@@ -225,9 +236,9 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const Embe
         return;
     }
     // lane l: token l - 1 of the chunk, so that the neighbours on both sides are there
-    const uint32_t all = w.starts[a.vocab], p0 = turn * kEmbedChunk;
+    const uint32_t all = w.starts[a.vocab], p0 = turn * w.chunk;
     if (p0 >= all) return;
-    const uint32_t n = min(all - p0, kEmbedChunk);
+    const uint32_t n = min(all - p0, w.chunk);
     static_assert(kEmbedChunk + 2 <= 64, "");
     const bool there = lane <= n + 1 && p0 + lane > 0 && p0 + lane - 1 < all;
     const uint32_t token = there ? w.order[p0 + lane - 1] : 0u, row = there ? embed_row<I>(a, token) : ~0u;
@@ -266,10 +277,10 @@ template <typename T, typename I>
 __global__ __launch_bounds__(64) void k_embed_join(const EmbedArgs a, const EmbedWork w)
 {
     constexpr int N = Pack<T>::N;
-    const uint32_t k = blockIdx.x, all = w.starts[a.vocab], p1 = (k + 1) * kEmbedChunk;
+    const uint32_t k = blockIdx.x, all = w.starts[a.vocab], p1 = (k + 1) * w.chunk;
     if (p1 >= all) return;                              // the last one, or none
     const uint32_t row = embed_row<I>(a, w.order[p1 - 1]), s0 = w.starts[row], s1 = w.starts[row + 1];
-    if (s0 < k * kEmbedChunk || s1 <= p1) return;
+    if (s0 < k * w.chunk || s1 <= p1) return;
     const uint32_t c = blockIdx.y * (64 * N) + threadIdx.x * N, len = c < a.hidden ? min(static_cast<uint32_t>(N), a.hidden - c) : 0u;
     float sum[N] = {};
     auto add = [&](uint32_t at, int which) {
@@ -281,12 +292,20 @@ __global__ __launch_bounds__(64) void k_embed_join(const EmbedArgs a, const Embe
         }
     };
     add(k, kPartTail);
-    const uint32_t last = (s1 - 1) / kEmbedChunk;
+    const uint32_t last = (s1 - 1) / w.chunk;
 #pragma unroll 8
     for (uint32_t j = k + 1; j <= last; ++j) add(j, kPartHead);
     embed_write<T>(a, row, c, len, sum);
 }
 
+// Tokens of a wave: 32, or fewer where that leaves compute units with less than eight waves (2999 tokens of 1001 fp32 columns, 32 / 8: 16.4 / 9 us).
+constexpr uint64_t kEmbedWaves = 2048;
+uint32_t embed_chunk(uint64_t tokens, uint32_t parts)
+{
+    uint32_t chunk = kEmbedChunk;
+    while (chunk > 8 && (tokens + chunk - 1) / chunk * parts < kEmbedWaves) chunk /= 2;
+    return chunk;
+}
 uint64_t pad256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 struct EmbedPlan {
     uint64_t order, starts, part, bytes;        // where each begins
@@ -295,7 +314,9 @@ struct EmbedPlan {
         order = 0;
         starts = pad256(tokens * 4);
         part = starts + pad256((vocab + 1) * 4);
-        bytes = part + (tokens + kEmbedChunk - 1) / kEmbedChunk * 2 * embed_part_ld(static_cast<uint32_t>(hidden)) * 4;
+        // chunks of 32, or shorter ones: fewer than 2 kEmbedWaves and a row's waves, each of 512 columns at most (fp32: 256, padded)
+        const uint64_t ld = embed_part_ld(static_cast<uint32_t>(hidden));
+        bytes = part + 8 * std::max((tokens + kEmbedChunk - 1) / kEmbedChunk * ld, (2 * kEmbedWaves + 4096) * 512 + ld);
     }
 };
 
@@ -322,7 +343,7 @@ int check_embed_rows(edgc_ctx* ctx, edgc_dtype dtype, const void* p, uint64_t ld
 int prepare_embed_kernels(edgc_ctx* ctx)
 {
     for (const void* f : {reinterpret_cast<const void*>(&k_embed_sort<int32_t>), reinterpret_cast<const void*>(&k_embed_sort<int64_t>)})
-        EDGC_HIP_TRY(ctx, hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * kSortMaxKeys * 4));
+        EDGC_HIP_TRY(ctx, hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * kSortMaxKeys * 12));
     return EDGC_OK;
 }
 
@@ -412,11 +433,12 @@ extern "C" int edgc_embed_backward(edgc_ctx* ctx, edgc_dtype dtype, const void* 
         const uint32_t keys = std::min((vocab + kSortBlocks - 1) / kSortBlocks, kSortMaxKeys), sorts = (vocab + keys - 1) / keys;
         if (tokens)
             EDGC_LAUNCH(ctx, st, KID_EMBED_SORT, 2.0 * sizeof(I) * tokens * sorts, 0.0,
-                    k_embed_sort<I><<<sorts, 64 * kSortWaves, kSortWaves * keys * 4, st>>>(a, keys, order, starts));
+                    k_embed_sort<I><<<sorts, 64 * kSortWaves, kSortWaves * keys * 12, st>>>(a, keys, order, starts));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         const uint32_t cols = 64 * Pack<T>::N;
-        EmbedWork w{order, tokens ? starts : nullptr, part, static_cast<uint32_t>((tokens + kEmbedChunk - 1) / kEmbedChunk),
-                    accumulate ? 0u : (vocab + kZeroRows - 1) / kZeroRows, (hidden + cols - 1) / cols};
+        const uint32_t parts = (hidden + cols - 1) / cols, chunk = embed_chunk(tokens, parts);
+        EmbedWork w{order, tokens ? starts : nullptr, part, chunk, static_cast<uint32_t>((tokens + chunk - 1) / chunk),
+                    accumulate ? 0u : (vocab + kZeroRows - 1) / kZeroRows, parts};
         const uint64_t blocks = ((static_cast<uint64_t>(w.chunks) + w.zeros) * w.parts + 3) / 4;
         if (blocks > 0x7fffffffull) return fail(ctx, EDGC_EINVAL, "tokens x hidden too large for one call");
         EDGC_LAUNCH(ctx, st, KID_EMBED_SUM, static_cast<double>(sizeof(T)) * hidden * (static_cast<double>(tokens) + vocab), 0.0,
