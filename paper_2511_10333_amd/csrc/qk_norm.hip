@@ -131,52 +131,74 @@ __device__ __forceinline__ float qk_head_sum(float v, uint32_t lanes)
 
 // A block has `per` tokens.  blockIdx.y: a share of the heads (few tokens, forward)
 template <typename T, int N, int U, bool BACK>
-__global__ __launch_bounds__(256) void k_qk_norm(const QkArgs a)
+__global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
 {
     extern __shared__ float2 angles[];          // [kQkTokens][pairs]; BACK: then the sums
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, in = lane & (a.lanes - 1), group = (threadIdx.x / a.lanes), groups = 256 / a.lanes;
+    const uint32_t lane = threadIdx.x & 63, in = lane & (a.lanes - 1), group = (threadIdx.x / a.lanes), groups = 256 / a.lanes;
     const uint64_t t0 = static_cast<uint64_t>(blockIdx.x) * a.per, t1 = min(a.tokens, t0 + a.per);
-    (void)wave;
     const uint32_t units = (a.dim + 2 * N - 1) / (2 * N);
     auto len = [&](uint32_t u, uint32_t at) { return u < units && at < a.dim ? min(static_cast<uint32_t>(N), a.dim - at) : 0u; };
-    float sums[2][U][2][BACK ? N : 1] = {};
-    for (uint64_t b0 = t0; b0 < t1; b0 += kQkTokens) {
-        const uint32_t n = static_cast<uint32_t>(min(static_cast<uint64_t>(kQkTokens), t1 - b0));
+    auto turn_by = [&](uint64_t b0, uint32_t n) {       // the angles of n tokens
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < n * a.pairs; i += 256) angles[i] = qk_angle(a, b0 + i / a.pairs, i % a.pairs);
         __syncthreads();
-        auto kind = [&](auto which) {
-            constexpr int K = decltype(which)::value;
-            const QkHeads& h = a.h[K];
-            const uint32_t per = (h.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * per, h1 = min(h.heads, h0 + per);
-            if (h0 >= h1) return;
-            QkPack<T, N> w[U][2];
+    };
+    // queries, then keys: of one of them the sums fit a wave's registers with three others on its SIMD (both: 161, a third of the blocks in a second round)
+    for (int K = 0; K < 2; ++K) {
+        const QkHeads& h = a.h[K];
+        const uint32_t share = (h.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share, h1 = min(h.heads, h0 + share), H = h1 > h0 ? h1 - h0 : 0u;
+        float sums[U][2][BACK ? N : 1] = {};
+        QkPack<T, N> w[U][2];
+        if (H) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 const QkUnit<N> u(a, in + k * a.lanes);
                 w[k][0].load(static_cast<const T*>(h.w) + u.first, len(in + k * a.lanes, u.first));
                 w[k][1].load(static_cast<const T*>(h.w) + u.second, len(in + k * a.lanes, u.second));
             }
-            const uint32_t items = n * (h1 - h0);
-            for (uint32_t it = group; it < (items + groups - 1) / groups * groups; it += groups) {     // (all lanes of a wave take part in the sums)
-                const bool there = it < items;
-                const uint64_t token = b0 + (there ? it / (h1 - h0) : 0), head = h0 + (there ? it % (h1 - h0) : 0);
+        }
+        for (uint64_t b0 = t0; b0 < t1; b0 += kQkTokens) {
+            const uint32_t n = static_cast<uint32_t>(min(static_cast<uint64_t>(kQkTokens), t1 - b0));
+            if (K == 0 || t1 - t0 > kQkTokens || BACK) turn_by(b0, n);
+            if (H == 0) continue;
+            // heads of the tokens one after the other, a group of lanes each; forward, the next one's elements are on their way during a head
+            const uint32_t items = n * H, rounds = (items + groups - 1) / groups;      // (all lanes of a wave take part in the sums)
+            const uint32_t tokens_on = groups / H, heads_on = groups - tokens_on * H;
+            uint32_t it = group, tok = group / H, hd = group - tok * H;
+            QkPack<T, N> v[U][2], d[U][2], next[U][2];
+            auto ask = [&](QkPack<T, N> (&xs)[U][2], QkPack<T, N> (&ds)[U][2]) {
+                const uint64_t token = b0 + tok, head = h0 + hd;
                 const T* const x = static_cast<const T*>(h.x) + token * h.x_token + head * h.x_head;
                 const T* const dy = BACK ? static_cast<const T*>(h.dy) + token * h.dy_token + head * h.dy_head : nullptr;
-                T* const out = static_cast<T*>(h.out) + token * h.out_token + head * h.out_head;
-                const float2* const turn = angles + (token - b0) * a.pairs;
-                QkPack<T, N> v[U][2], d[U][2];
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
                     const uint32_t unit = in + k * a.lanes;
                     const QkUnit<N> u(a, unit);
-                    v[k][0].load(x + u.first, len(unit, u.first));
-                    v[k][1].load(x + u.second, len(unit, u.second));
+                    xs[k][0].load(x + u.first, len(unit, u.first));
+                    xs[k][1].load(x + u.second, len(unit, u.second));
                     if constexpr (BACK) {
-                        d[k][0].load(dy + u.first, len(unit, u.first));
-                        d[k][1].load(dy + u.second, len(unit, u.second));
+                        ds[k][0].load(dy + u.first, len(unit, u.first));
+                        ds[k][1].load(dy + u.second, len(unit, u.second));
                     }
                 }
+            };
+            if (!BACK && it < items) ask(next, d);
+            for (uint32_t round = 0; round < rounds; ++round) {
+                const bool there = it < items;
+                const uint64_t token = b0 + tok, head = h0 + hd;
+                T* const out = static_cast<T*>(h.out) + token * h.out_token + head * h.out_head;
+                const float2* const turn = angles + (there ? tok : 0u) * a.pairs;
+                if constexpr (BACK) {
+                    if (there) ask(v, d);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < U; ++k) v[k][0] = next[k][0], v[k][1] = next[k][1];
+                }
+                it += groups;
+                tok += tokens_on;
+                hd += heads_on;
+                if (hd >= H) hd -= H, ++tok;
+                if (!BACK && it < items) ask(next, d);
                 float q = 0.f, s = 0.f;
                 float g[U][2][N];               // BACK: d, rotated back
 #pragma unroll
@@ -214,7 +236,7 @@ __global__ __launch_bounds__(256) void k_qk_norm(const QkArgs a)
                             const float xh = v[k][e].get(i) * r;
                             if constexpr (BACK) {
                                 y[e][i] = r * (g[k][e][i] * w[k][e].get(i) - xh * m);
-                                sums[K][k][e][i] = __builtin_fmaf(g[k][e][i], xh, sums[K][k][e][i]);
+                                sums[k][e][i] = __builtin_fmaf(g[k][e][i], xh, sums[k][e][i]);
                             } else {
                                 y[e][i] = xh * w[k][e].get(i);
                             }
@@ -224,15 +246,10 @@ __global__ __launch_bounds__(256) void k_qk_norm(const QkArgs a)
                     QkPack<T, N>::store(out + u.second, len(unit, u.second), y[1]);
                 }
             }
-        };
-        kind(std::integral_constant<int, 0>{});
-        kind(std::integral_constant<int, 1>{});
-    }
-    if constexpr (BACK) {
-        // the block's sums, in the order of the groups
-        float* const all = reinterpret_cast<float*>(angles);        // [groups][dim]
-        auto add = [&](auto which) {
-            constexpr int K = decltype(which)::value;
+        }
+        if constexpr (BACK) {
+            // the block's sums, in the order of the groups
+            float* const all = reinterpret_cast<float*>(angles);        // [groups][dim]
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < U; ++k) {
@@ -243,7 +260,7 @@ __global__ __launch_bounds__(256) void k_qk_norm(const QkArgs a)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
                         const uint32_t at = e ? u.second : u.first;
-                        if (static_cast<uint32_t>(i) < len(unit, at)) all[group * a.dim + at + i] = sums[K][k][e][i];
+                        if (static_cast<uint32_t>(i) < len(unit, at)) all[group * a.dim + at + i] = sums[k][e][i];
                     }
             }
             __syncthreads();
@@ -252,9 +269,7 @@ __global__ __launch_bounds__(256) void k_qk_norm(const QkArgs a)
                 for (uint32_t g = 0; g < groups; ++g) t += all[g * a.dim + c];
                 a.part[(static_cast<uint64_t>(blockIdx.x) * 2 + K) * a.dim + c] = t;
             }
-        };
-        add(std::integral_constant<int, 0>{});
-        add(std::integral_constant<int, 1>{});
+        }
     }
 }
 
