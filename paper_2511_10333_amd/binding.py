@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -152,7 +153,7 @@ def load_library() -> C.CDLL:
     L.edgc_reserve_orthogonalize.argtypes = [vp, i32, C.POINTER(u32), C.POINTER(u32), u32, u32]
     L.edgc_orthogonalize_batch.restype = i32
     L.edgc_orthogonalize_batch.argtypes = [vp, C.POINTER(_Tensor), u32, i32, u32, f64, f64, f64, f64, vp, vp]
-    i64, heads = C.c_int64, C.POINTER(_Heads)
+    i64, heads = C.c_int64, vp              # heads: the bytes of an edgc_heads
     L.edgc_embed_forward.restype = i32
     L.edgc_embed_forward.argtypes = [vp, i32, vp, u64, u32, u32, vp, i32, i64, u64, f32, vp, u64, vp]
     L.edgc_reserve_embed.restype = i32
@@ -190,6 +191,9 @@ class _FF(C.Structure):
 
 class _Heads(C.Structure):
     _fields_ = [("p", C.c_void_p), ("token", C.c_uint64), ("head", C.c_uint64)]
+
+
+_pack_heads = struct.Struct("@PQQ").pack        # a tenth of the time that a ctypes structure takes to build
 
 
 @dataclass
@@ -423,8 +427,10 @@ def _check_u32(*sizes) -> None:
             raise ValueError("tokens and widths must be 0 or more and below 2^32")
 
 
-def _head_views(name, t, dtype, shape) -> _Heads:
-    """Queries or keys (tokens x heads x dim) of that dtype and shape, the dimensions of a head adjacent."""
+def _heads(name, t, dtype, shape) -> bytes:
+    """The edgc_heads of queries or keys (tokens x heads x dim) of that dtype and shape, the dimensions of a head adjacent."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
     if t.shape != shape:
@@ -432,7 +438,7 @@ def _head_views(name, t, dtype, shape) -> _Heads:
     token, head, step = t.stride()
     if step != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have the dimensions of a head next to each other")
-    return _Heads(t.data_ptr(), token, head)
+    return _pack_heads(t.data_ptr(), token, head)
 
 
 def _integers(name, t, shape) -> int:
@@ -910,8 +916,9 @@ class Context:
 
     def _on_device(self, *tensors) -> None:
         """Every given tensor lies on the context's GPU: another address would be one for its kernels to fault on."""
+        device = self.device
         for t in tensors:
-            if t is not None and t.get_device() != self.device:
+            if t is not None and t.get_device() != device:
                 raise ValueError(f"tensors must be on the context's device, cuda:{self.device}")
 
     def embed_forward(self, table, ids, out, scale: float = 1.0, first_id: int = 0, stream=None) -> None:
@@ -957,46 +964,39 @@ class Context:
             self._check(rc, "edgc_embed_backward")
 
     def _qk_args(self, q, k, w_q, w_k, positions, inv_freq):
-        """What the two passes have in common: type, sizes, positions and frequencies, all as they have to be."""
-        if len(q.shape) != 3 or (k is not None and len(k.shape) != 3):
+        """What the two passes have in common, all as it has to be: shapes of queries and keys, type and sizes, positions and frequencies."""
+        sq = q.shape
+        if len(sq) != 3 or (k is not None and len(k.shape) != 3):
             raise ValueError("queries and keys must be tokens x heads x dim")
-        t, hq, dim = q.shape
+        t, hq, dim = sq
         hk = 0 if k is None else k.shape[1]
-        _check_u32(hq, hk, dim)
+        if (hq | hk | dim) >> 32:
+            _check_u32(hq, hk, dim)
         code, dtype = _dtype_code(q), q.dtype
-        _check_dense(("w_q", "w_k"), (w_q, w_k), dtype, (dim,))
-        if w_q is None or (k is not None and w_k is None):
+        if w_q is None or (k is None) != (w_k is None):
             raise ValueError("queries need w_q, and keys w_k")
-        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-        bytes_ = 8
-        if rot:
-            if positions is None:
-                raise ValueError("inv_freq needs positions")
-            bytes_ = _integers("positions", positions, (t,))
-            _check_dense(("inv_freq",), (inv_freq,), _torch.float64, (rot // 2,))
-        self._on_device(q, k, w_q, w_k, positions, inv_freq)
-        return code, dtype, t, hq, hk, dim, rot, bytes_
-
-    @staticmethod
-    def _heads(name, t, like, dtype, shape):
-        """Descriptor of queries or keys of that shape, or None where the layer has none (``like`` is None)."""
-        if like is None:
-            if t is not None:
-                raise ValueError(f"{name} without keys")
-            return None
-        if t is None:
-            raise ValueError(f"{name} is missing")
-        return C.byref(_head_views(name, t, dtype, shape))
+        _check_dense(("w_q", "w_k"), (w_q, w_k), dtype, (dim,))
+        if inv_freq is None or not inv_freq.numel():
+            return sq, (t, hk, dim), (self._h, code, t, hq, hk, dim), (None, 8, None, 0)
+        if positions is None:
+            raise ValueError("inv_freq needs positions")
+        bytes_, n = _integers("positions", positions, (t,)), inv_freq.numel()
+        _check_dense(("inv_freq",), (inv_freq,), _torch.float64, (n,))
+        return sq, (t, hk, dim), (self._h, code, t, hq, hk, dim), (positions.data_ptr(), bytes_, inv_freq.data_ptr(), 2 * n)
 
     def qk_norm_forward(self, q, k, w_q, w_k, positions, inv_freq, q_out, k_out, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
         """edgc_qk_norm_forward: every head of ``q`` and ``k`` (tokens x heads x dim, any strides of tokens and heads; ``k`` may be None) normed, times
         its weight, and the first 2 * len(inv_freq) dimensions rotated by positions * inv_freq (int32 or int64, and float64; None: none are)."""
-        code, dtype, t, hq, hk, dim, rot, bytes_ = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
-        sq, sk, h = (t, hq, dim), (t, hk, dim), self._heads
-        self._on_device(q_out, k_out)
-        rc = self._L.edgc_qk_norm_forward(self._h, code, t, hq, hk, dim, h("q", q, q, dtype, sq), h("k", k, k, dtype, sk), _ptr(w_q), _ptr(w_k),
-                                          _ptr(positions), bytes_, _ptr(inv_freq), rot, 1 if interleaved else 0, eps, h("q_out", q_out, q, dtype, sq),
-                                          h("k_out", k_out, k, dtype, sk), _stream_handle(stream))
+        sq, sk, sizes, angle = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
+        dtype = q.dtype
+        hq, hq_out, hk, hk_out = _heads("q", q, dtype, sq), _heads("q_out", q_out, dtype, sq), None, None
+        if k is not None:
+            hk, hk_out = _heads("k", k, dtype, sk), _heads("k_out", k_out, dtype, sk)
+        elif k_out is not None:
+            raise ValueError("k_out without keys")
+        self._on_device(q, k, w_q, w_k, positions, inv_freq, q_out, k_out)
+        rc = self._L.edgc_qk_norm_forward(*sizes, hq, hk, w_q.data_ptr(), _ptr(w_k), *angle, 1 if interleaved else 0, eps, hq_out, hk_out,
+                                          _stream_handle(stream))
         if rc:
             self._check(rc, "edgc_qk_norm_forward")
 
@@ -1009,13 +1009,18 @@ class Context:
     def qk_norm_backward(self, dq_out, dk_out, q, k, w_q, w_k, positions, inv_freq, dq, dk, dw_q, dw_k, eps: float = 1e-6, interleaved: bool = False,
                          stream=None) -> None:
         """edgc_qk_norm_backward: the gradients of what :meth:`qk_norm_forward` read, from those of what it wrote."""
-        code, dtype, t, hq, hk, dim, rot, bytes_ = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
-        sq, sk, h = (t, hq, dim), (t, hk, dim), self._heads
-        _check_dense(("dw_q", "dw_k"), (dw_q, dw_k), dtype, (dim,))
-        self._on_device(dq_out, dk_out, dq, dk, dw_q, dw_k)
-        rc = self._L.edgc_qk_norm_backward(self._h, code, t, hq, hk, dim, h("dq_out", dq_out, q, dtype, sq), h("dk_out", dk_out, k, dtype, sk),
-                                           h("q", q, q, dtype, sq), h("k", k, k, dtype, sk), _ptr(w_q), _ptr(w_k), _ptr(positions), bytes_,
-                                           _ptr(inv_freq), rot, 1 if interleaved else 0, eps, h("dq", dq, q, dtype, sq), h("dk", dk, k, dtype, sk),
-                                           _ptr(dw_q), _ptr(dw_k), _stream_handle(stream))
+        sq, sk, sizes, angle = self._qk_args(q, k, w_q, w_k, positions, inv_freq)
+        dtype = q.dtype
+        hq, hdy_q, hdx_q, hk, hdy_k, hdx_k = _heads("q", q, dtype, sq), _heads("dq_out", dq_out, dtype, sq), _heads("dq", dq, dtype, sq), None, None, None
+        if k is not None:
+            hk, hdy_k, hdx_k = _heads("k", k, dtype, sk), _heads("dk_out", dk_out, dtype, sk), _heads("dk", dk, dtype, sk)
+        elif dk_out is not None or dk is not None:
+            raise ValueError("dk_out or dk without keys")
+        if dw_q is None or (k is None) != (dw_k is None):
+            raise ValueError("queries need dw_q, and keys dw_k")
+        _check_dense(("dw_q", "dw_k"), (dw_q, dw_k), dtype, (sq[2],))
+        self._on_device(q, k, w_q, w_k, positions, inv_freq, dq_out, dk_out, dq, dk, dw_q, dw_k)
+        rc = self._L.edgc_qk_norm_backward(*sizes, hdy_q, hdy_k, hq, hk, w_q.data_ptr(), _ptr(w_k), *angle, 1 if interleaved else 0, eps, hdx_q, hdx_k,
+                                           dw_q.data_ptr(), _ptr(dw_k), _stream_handle(stream))
         if rc:
             self._check(rc, "edgc_qk_norm_backward")
