@@ -242,10 +242,8 @@ bool coefs_bounded(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps)
 uint32_t ortho_places(const edgc_ctx* ctx, int bm) { return static_cast<uint32_t>(ctx->num_cu) * (bm == 256 ? 1 : 2); }
 // sums that workers can leave behind: at most two tiles per place
 uint64_t ortho_sums_elems(const edgc_ctx* ctx) { return 2ull * 256 * 256 * ctx->num_cu; }
-// the rate at which tiles of 128 x 128 get done, of that of the large ones
-template <int PA> constexpr double kOrthoLittle = PA == 1 ? 0.65 : 0.8;
-// the least tiles of k that are worth a worker
-constexpr uint32_t kOrthoMinTiles = 8;
+// the least tiles of k that are worth a worker, whose sums go through memory
+constexpr uint32_t ortho_least(int bm) { return bm == 64 ? 32 : 8; }
 
 template <int BM, int BN, int PA, int PB, bool TB, typename T>
 hipError_t prepare_ortho_tiles()
@@ -299,7 +297,7 @@ struct OrthoPass {
             }
         };
         count_rest();
-        args.workers = std::min(places, args.steps / kOrthoMinTiles);
+        args.workers = std::min(places, args.steps / ortho_least(BM));
         // (a last round that is nearly full is not worth the sums' way through memory)
         if (args.workers <= args.rest || args.rest * 10ull > places * 9ull) {
             args.whole = tiles;
@@ -327,19 +325,33 @@ struct OrthoPass {
     {
         constexpr int BN = PA == 1 ? 256 : 128;         // one plane: a wave has room for 128 x 128
         std::stable_sort(args.p, args.p + args.count, [](const OrthoProblem& x, const OrthoProblem& y) { return x.ktiles > y.ktiles; });
-        // the time that either tile shape would take, in a tile of k of the large one on a compute unit; `alone`: of the little one without a second
-        auto time_of = [&](auto bm, auto bn, double step, double alone) {
-            double steps = 0.0, least = 0.0;
+        // The time that a tile shape would take, in us: `step`: for a tile of k of each of a compute unit's blocks at a time, `alone`: where a block has its
+        // compute unit for itself, `share`: for sums to go through memory and be joined.  Measured on products of 512 to 4096.
+        auto time_of = [&](auto bm, auto bn, double step, double alone, double share) {
+            double steps = 0.0, tiles = 0.0, longest = 0.0;
             for (uint32_t i = 0; i < args.count; ++i) {
-                steps += static_cast<double>(args.p[i].ktiles) * tiles_of<bm, bn, TB>(args.p[i]);
-                least = std::max(least, 1.0 * std::min(args.p[i].ktiles, kOrthoMinTiles));
+                const double n = tiles_of<bm, bn, TB>(args.p[i]);
+                tiles += n;
+                steps += n * args.p[i].ktiles;
+                longest = std::max(longest, 1.0 * args.p[i].ktiles);
             }
-            return std::max(step * steps / ortho_places(ctx, bm), alone * least);
+            const double places = ortho_places(ctx, bm), least = ortho_least(bm);
+            if (tiles >= places || longest <= least) return std::max(step * steps / places, alone * longest);
+            return share + std::max(step * steps / places, alone * std::min(longest, least));
         };
         using std::integral_constant;
-        const double large = time_of(integral_constant<int, 256>{}, integral_constant<int, BN>{}, 1.0, 1.0),
-                     little = time_of(integral_constant<int, 128>{}, integral_constant<int, 128>{}, 2.0 * 64 / BN / kOrthoLittle<PA>, 0.75);
-        if (large <= little) return launch<256, BN, PA, PB, TB, T>(args, kid);
+        using Large = integral_constant<int, 256>;
+        using Middle = integral_constant<int, 128>;
+        using Small = integral_constant<int, 64>;
+        constexpr double work = PA == 1 ? 1.0 : PB == 1 ? 2.0 / 3.0 : 1.0;     // a tile of k: 64 of one product, or 32 of three or two
+        const double large = time_of(Large{}, integral_constant<int, BN>{}, work * (PA == 1 ? 2.0 : 1.5), work * (PA == 1 ? 2.0 : 1.5), 8.0),
+                     middle = time_of(Middle{}, Middle{}, work * 1.9, work * 1.0, 8.0);
+        // (one plane of a transposed operand is too narrow for the small tiles' reads)
+        if constexpr (!(TB && PB == 1)) {
+            const double small = time_of(Small{}, Small{}, work * 1.0, work * 0.4, 8.0);
+            if (small < large && small < middle) return launch<64, 64, PA, PB, TB, T>(args, kid);
+        }
+        if (large <= middle) return launch<256, BN, PA, PB, TB, T>(args, kid);
         return launch<128, 128, PA, PB, TB, T>(args, kid);
     }
     // a product of two matrices of the smaller side, or the first of a segment
@@ -511,7 +523,9 @@ int check_shape(edgc_ctx* ctx, uint64_t m, uint64_t n)
 
 int prepare_ortho_kernels(edgc_ctx* ctx)
 {
-    for (hipError_t e : {prepare_ortho_tiles<256, 256, 1, 1, false, void>(), prepare_ortho_tiles<256, 128, 2, 2, false, void>(),
+    for (hipError_t e : {prepare_ortho_tiles<64, 64, 1, 1, false, void>(), prepare_ortho_tiles<64, 64, 2, 2, false, void>(),
+                         prepare_ortho_tiles<64, 64, 2, 2, true, void>(), prepare_ortho_tiles<64, 64, 2, 2, true, float>(),
+                         prepare_ortho_tiles<64, 64, 2, 2, true, __bf16>(), prepare_ortho_tiles<256, 256, 1, 1, false, void>(), prepare_ortho_tiles<256, 128, 2, 2, false, void>(),
                          prepare_ortho_tiles<256, 128, 2, 1, true, void>(), prepare_ortho_tiles<256, 128, 2, 2, true, void>(),
                          prepare_ortho_tiles<256, 128, 2, 2, true, float>(), prepare_ortho_tiles<256, 128, 2, 1, true, __bf16>(),
                          prepare_ortho_tiles<256, 128, 2, 2, true, __bf16>()})

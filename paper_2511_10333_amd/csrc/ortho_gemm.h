@@ -189,15 +189,19 @@ __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
     return factor;
 }
 
-// k of a tile, bytes of either operand's tile in LDS, all of LDS: two tiles of each, of A three where a block has the compute unit for itself
+// k of a tile, bytes of either operand's tile in LDS, tiles of A and B that are there, all of LDS.  Blocks of 256 rows have a compute unit for themselves, of the
+// others two share it.  A tile of 64 x 64 is multiplied in a fraction of the time that the next takes to come: four are on their way.
 template <int PA, int PB> constexpr int kOrthoK = PA == 1 && PB == 1 ? 64 : 32;
 template <int BN, int PB, bool TB> constexpr uint32_t kOrthoBytesB = TB ? 32u * BN * PB * 2u : BN * 128u;
-template <int BM, int BN, int PB, bool TB> constexpr uint32_t kOrthoLds = (BM == 256 ? 3u : 2u) * BM * 128u + 2u * kOrthoBytesB<BN, PB, TB>;
+template <int BM> constexpr uint32_t kOrthoTilesA = BM == 256 ? 3u : BM == 128 ? 2u : 5u;
+template <int BM> constexpr uint32_t kOrthoTilesB = BM == 64 ? 5u : 2u;
+template <int BM, int BN, int PB, bool TB> constexpr uint32_t kOrthoLds = kOrthoTilesA<BM> * BM * 128u + kOrthoTilesB<BM> * kOrthoBytesB<BN, PB, TB>;
 
 // The sums of a tile over tiles kt0 to kt1 of k, by 2 x 2 waves: of a wave, I x J squares of 32 x 32.  The loop of ff_gemm.h: while a step of 16 k is
 // multiplied, the fragments of the next are read (in a tile's last step, the first of the next tile); the barrier before the last step ends the reads of the
 // tile, and from there on B of the tile after the next is asked for, into its place.  A, in three buffers (LARGE), is asked for in the first half of
-// the steps: the barrier of tile t finds tile t + 1 there, after which A of tile t + 2 alone was asked for.
+// the steps: the barrier of tile t finds tile t + 1 there, after which A of tile t + 2 alone was asked for.  (Smaller blocks ask for both operands there, as many
+// tiles ahead as they have buffers.)
 template <int BM, int BN, int PA, int PB, bool TB>
 __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char* lds, uint32_t lane, uint32_t wave, uint32_t m0, uint32_t n0, uint32_t kt0, uint32_t kt1,
                                            f32x16 (&acc)[BM / 64][BN / 64])
@@ -207,7 +211,9 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
     constexpr int WIDTH = BN * PB;                                                 // TB: elements of a tile's row of k
     constexpr int LA = BM / 32, LB = TB ? WIDTH / 64 : BN / 32;                    // a wave's loads of a tile
     constexpr int FA = I * PA, FB = J * PB, F = FA + FB, MM = I * J * (PA + PB - 1);    // fragments and products of a step
-    constexpr uint32_t kBufsA = LARGE ? 3 : 2, kBytesA = BM * 128, kBytesB = kOrthoBytesB<BN, PB, TB>, kAtB = kBufsA * kBytesA;    // lds: [kBufsA][kBytesA], [2][kBytesB]
+    // lds: [kBufsA][kBytesA], [kBufsB][kBytesB]
+    constexpr uint32_t kBufsA = kOrthoTilesA<BM>, kBufsB = kOrthoTilesB<BM>, kBytesA = BM * 128, kBytesB = kOrthoBytesB<BN, PB, TB>, kAtB = kBufsA * kBytesA;
+    constexpr uint32_t AHEAD = kBufsB;                  // tiles
     static_assert(!TB || PA == 2, "the transposed operand is the gradient, multiplied by two planes");
     static_assert(PA == PB || (PB == 1 && TB), "");
     const uint32_t wm = wave / 2, wn = wave % 2;
@@ -256,7 +262,7 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
             fa[to][f - FB] = __builtin_bit_cast(f16x8, frag_a.read(lds + buf_a * kBytesA, (f - FB) % PA * 2 + kk, (f - FB) / PA));
         }
     };
-    for (uint32_t t = 0; t < 2 && t < n; ++t) {
+    for (uint32_t t = 0; t < AHEAD && t < n; ++t) {
 #pragma unroll
         for (int i = 0; i < LA; ++i) bring_a(t, i);
         pa += a_step;
@@ -264,25 +270,26 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
         for (int i = 0; i < LB; ++i) bring_b(t, i);
         pb += b_step;
     }
-    if (n > 1) tile_barrier<LA + LB>();
+    if (n >= AHEAD) tile_barrier<(AHEAD - 1) * (LA + LB)>();
     else tile_barrier<0>();
 #pragma unroll
     for (int f = 0; f < F; ++f) read(0, 0, 0, f);
-    uint32_t buf_a = 0, ask_a = kBufsA - 1;     // buffers of this tile's A and of the one asked for next
+    uint32_t buf_a = 0, buf_b = 0, ask_a = kBufsA - 1;      // buffers of this tile's operands; LARGE: of the A asked for next
     for (uint32_t t = 0; t < n; ++t) {
-        const uint32_t buf_b = t & 1, next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1;
-        const bool more_a = LARGE && t + 2 < n, more_b = t + 2 < n;
+        const uint32_t next_buf_a = buf_a + 1 == kBufsA ? 0 : buf_a + 1, next_buf_b = buf_b + 1 == kBufsB ? 0 : buf_b + 1;
+        const bool more_a = LARGE && t + AHEAD < n, more_b = t + AHEAD < n;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            if (kk == KK - 1) {
-                if (more_a) tile_barrier<LA>();
+            if (kk == KK - 1) {                             // tile t + 1 has to be there; what may be on its way still
+                if (LARGE && more_a) tile_barrier<LA>();
+                else if (!LARGE && AHEAD > 2 && t + AHEAD <= n) tile_barrier<(AHEAD - 2) * (LA + LB)>();
                 else tile_barrier<0>();
             }
             const int from = kk & 1;
 #pragma unroll
             for (int c = 0; c < F; ++c) {
                 if (kk < KK - 1) read(buf_a, buf_b, kk + 1, c);
-                else read(next_buf_a, buf_b ^ 1, 0, c);
+                else read(next_buf_a, next_buf_b, 0, c);
                 if (LARGE && kk < KK / 2 && more_a) {
                     constexpr int SLOTS = KK / 2 * F;
 #pragma unroll
@@ -293,7 +300,7 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
                     for (int i = c * LB / F; i < (c + 1) * LB / F; ++i) bring_b(buf_b, i);
                     if constexpr (!LARGE) {
 #pragma unroll
-                        for (int i = c * LA / F; i < (c + 1) * LA / F; ++i) bring_a(buf_b, i);
+                        for (int i = c * LA / F; i < (c + 1) * LA / F; ++i) bring_a(buf_a, i);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -314,6 +321,7 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
             if (!LARGE) pa += a_step;
         }
         buf_a = next_buf_a;
+        buf_b = next_buf_b;
         ask_a = ask_a + 1 == kBufsA ? 0 : ask_a + 1;
     }
     tile_barrier<0>();
