@@ -19,6 +19,7 @@
 namespace edgc {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 struct OrthoProblem {
@@ -114,6 +115,24 @@ __device__ __forceinline__ void ortho_spread(float factor, const f32x16& acc, fl
         *reinterpret_cast<float4*>(mine + (lane & 31) * kOrthoRow + 8 * q + 4 * (lane >> 5)) =
             float4{factor * acc[4 * q], factor * acc[4 * q + 1], factor * acc[4 * q + 2], factor * acc[4 * q + 3]};
 }
+// alpha times the sums of a square, and what is added to them, still in the order of the registers: a loop of squares whose stores are on their way must
+// not load anything, or each waits for the last one's stores
+__device__ __forceinline__ void ortho_add(const OrthoProblem& p, float factor, f32x16& acc, uint32_t lane, uint32_t m0, uint32_t n0)
+{
+    const uint32_t m = m0 + lane % 32;
+    const uint16_t* const row = p.e + min(m, p.rows - 1) * p.ldo;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t n = n0 + 8 * q + 4 * (lane / 32);
+        const uint16_t* const from = row + ortho_at(min(n, p.cols - 4));
+        const f16x4 h = *reinterpret_cast<const f16x4*>(from), l = *reinterpret_cast<const f16x4*>(from + 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v = fmaf(p.beta, static_cast<float>(h[i]) + static_cast<float>(l[i]), factor * acc[4 * q + i]);
+            acc[4 * q + i] = m == n + i ? v + p.gamma : v;
+        }
+    }
+}
 template <bool SYM, typename T>
 __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine, uint32_t lane, uint32_t m0, uint32_t n0)
 {
@@ -134,21 +153,13 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
             const float4 x = *reinterpret_cast<const float4*>(mine + r * kOrthoRow + c), y = *reinterpret_cast<const float4*>(mine + r * kOrthoRow + c + 4);
             float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
             if constexpr (PLANES) {
-                const uint64_t at = m * p.ldo + ortho_at(n);
-                if (SYM && p.e) {
-                    const f16x8 h = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(p.e + at)),
-                                l = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(p.e + at + 32));
+                if (m0 + 32 > p.M || n0 + 32 > p.N) {
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        v[i] = fmaf(p.beta, static_cast<float>(h[i]) + static_cast<float>(l[i]), v[i]);
-                        if (m == n + i) v[i] += p.gamma;
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = m < p.M && n + i < p.N ? v[i] : 0.f;
+                    if (SYM && mirror) {
+                        *reinterpret_cast<float4*>(mine + r * kOrthoRow + c) = float4{v[0], v[1], v[2], v[3]};
+                        *reinterpret_cast<float4*>(mine + r * kOrthoRow + c + 4) = float4{v[4], v[5], v[6], v[7]};
                     }
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) v[i] = m < p.M && n + i < p.N ? v[i] : 0.f;
-                if (SYM && mirror) {
-                    *reinterpret_cast<float4*>(mine + r * kOrthoRow + c) = float4{v[0], v[1], v[2], v[3]};
-                    *reinterpret_cast<float4*>(mine + r * kOrthoRow + c + 4) = float4{v[4], v[5], v[6], v[7]};
                 }
                 ortho_put(p.out + m * p.ldo, n, v);
             } else {
@@ -379,18 +390,32 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
         ortho_sums<BM, BN, PA, PB, TB>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
 
         if (kt1 - kt0 == p.ktiles) {
-            const float factor = ortho_factor(p);
+            // (The lane is hidden from what comes before, and all loads are waited for here: addresses kept over the products would be spilled, and waiting for
+            // one of them inside the loop waits for the last square's stores too.  A square took 2 us.)
+            uint32_t l = lane;
+            asm volatile("" : "+v"(l));
+            float factor = ortho_factor(p);
             float* const mine = reinterpret_cast<float*>(lds) + wave * (32 * kOrthoRow);
+            auto m_of = [&](int s) { return m0 + (wm * I + s / J) * 32; };
+            auto n_of = [&](int s) { return n0 + (wn * J + s % J) * 32; };
+            if (SYM && p.e) {
+                ff_each<I * J>([&](auto q) {
+                    constexpr int k = decltype(q)::value;
+                    ortho_add(p, factor, acc[k / J][k % J], l, m_of(k), n_of(k));
+                    if constexpr (k % 2 == 1) __builtin_amdgcn_sched_barrier(0);        // (two squares' loads at a time have registers)
+                });
+                factor = 1.0f;
+            }
+            __builtin_amdgcn_s_waitcnt(0);
             // a loop, whose code stays in the instruction cache
 #pragma unroll 1
             for (int s = 0; s < I * J; ++s) {
-                const uint32_t m = m0 + (wm * I + s / J) * 32, n = n0 + (wn * J + s % J) * 32;
-                if (SYM && n > m) continue;
+                if (SYM && n_of(s) > m_of(s)) continue;
                 ff_each<I * J>([&](auto q) {
                     constexpr int k = decltype(q)::value;
-                    if (s == k) ortho_spread(factor, acc[k / J][k % J], mine, lane);
+                    if (s == k) ortho_spread(factor, acc[k / J][k % J], mine, l);
                 });
-                ortho_square<SYM, T>(p, mine, lane, m, n);
+                ortho_square<SYM, T>(p, mine, l, m_of(s), n_of(s));
             }
         } else {
 #pragma unroll
@@ -436,7 +461,12 @@ __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
         }
     }
     float* const mine = stage + wave * (32 * kOrthoRow);
-    ortho_spread(ortho_factor(p), acc, mine, lane);
+    float factor = ortho_factor(p);
+    if (SYM && p.e) {
+        ortho_add(p, factor, acc, lane, m, n);
+        factor = 1.0f;
+    }
+    ortho_spread(factor, acc, mine, lane);
     ortho_square<SYM, T>(p, mine, lane, m, n);
 }
 
