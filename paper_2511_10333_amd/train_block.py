@@ -1,12 +1,14 @@
 """A data-parallel training step around the compressor, on one GPU: a stack of residual gated feed-forward blocks.
 
     python -m paper_2511_10333_amd.train_block --layers 4 --hidden 512 --ff 2048 --tokens 1024 --steps 40
+    python -m paper_2511_10333_amd.train_block --vocab 5000 --update orthogonal --lr 0.05
 
-Per step: the norm before the first block; per block the gated feed-forward block and the norms after it and before the next,
+Per step: the embedding of the tokens (with --vocab; otherwise the inputs are given); the norm before the first block; per block the gated feed-forward block and the norms after it and before the next,
 with gate and residual scale; the backward passes, which leave the weight gradients in the compressor's tensors; the entropy of
 those gradients and, per window, the rank; compress and decompress with error feedback (a job of several ranks all-reduces P and
-Q between the two phases of the compress); the global norm and clipping; a momentum update.  The model learns the outputs of
-another one of the same shape.  Prints one JSON line per window.  Needs a GPU and the built library.
+Q between the two phases of the compress); the global norm and clipping; a momentum update, or with --update orthogonal one whose
+matrices' momentum is orthogonalised (of the blocks' matrices, not of the embedding's).  The model learns the outputs of another one of the
+same shape.  Prints one JSON line per window.  Needs a GPU and the built library.
 """
 from __future__ import annotations
 
@@ -34,7 +36,7 @@ class Model:
     """Weights of ``layers`` blocks, their gradients, and the two passes through them."""
 
     def __init__(self, ctx: Context, layers: int, hidden: int, ff: int, tokens: int, sequence: int, dtype=torch.float32,
-                 act: str = "silu", seed: int = 0):
+                 act: str = "silu", seed: int = 0, vocab: int = 0):
         g = torch.Generator(device="cuda").manual_seed(seed)
         randn = lambda *s, std=1.0, mean=0.0: (mean + std * torch.randn(*s, generator=g, device="cuda")).to(dtype)
         self.ctx, self.hidden, self.ff, self.tokens, self.sequence = ctx, hidden, ff, tokens, sequence
@@ -47,6 +49,8 @@ class Model:
         self.w_last = randn(hidden, std=0.02, mean=1.0)         # of the norm after the last block
         self.grads = [{k: torch.zeros_like(w) for k, w in b.items()} for b in self.blocks]
         self.g_last = torch.zeros_like(self.w_last)
+        self.table = randn(vocab, hidden) if vocab else None    # of the tokens' embedding
+        self.g_table = torch.zeros_like(self.table) if vocab else None
         self.weights = [FeedForward(b["w_gate"], b["w_up"], b["w_down"], act) for b in self.blocks]
         act_of = lambda *s: torch.empty(s, device="cuda", dtype=dtype)
         stat = lambda: torch.empty(tokens, device="cuda")
@@ -57,10 +61,23 @@ class Model:
         self.d = {k: act_of(tokens, hidden) for k in ("x", "n", "y")}
         ctx.reserve_ff(dtype, tokens, hidden, ff, backward=True)
         ctx.reserve_block_norm(tokens, hidden)
+        if vocab:
+            self.embedded = act_of(tokens, hidden)
+            ctx.reserve_embed(tokens, vocab, hidden)
 
     def parameters(self):
         """Pairs of weight and gradient."""
-        return [(b[k], g[k]) for b, g in zip(self.blocks, self.grads) for k in b] + [(self.w_last, self.g_last)]
+        pairs = [(b[k], g[k]) for b, g in zip(self.blocks, self.grads) for k in b] + [(self.w_last, self.g_last)]
+        return pairs + [(self.table, self.g_table)] if self.table is not None else pairs
+
+    def forward_tokens(self, ids):
+        """forward() of the tokens' embeddings."""
+        self.ctx.embed_forward(self.table, ids, self.embedded)
+        return self.forward(self.embedded)
+
+    def backward_tokens(self, ids, dn):
+        """backward(), and on to the gradient of the embedding."""
+        self.ctx.embed_backward(ids, self.backward(dn), self.g_table)
 
     def _after(self, i):
         """The norm that follows block i: its weight, its output, the sum and the statistic."""
@@ -100,7 +117,7 @@ class Model:
 class Step:
     """What follows the backward pass: entropy, rank, compress and decompress with error feedback, clipping, update."""
 
-    def __init__(self, model: Model, max_norm: float, lr: float, momentum: float, seed: int = 0):
+    def __init__(self, model: Model, max_norm: float, lr: float, momentum: float, seed: int = 0, orthogonal: bool = False):
         self.m, self.ctx, self.max_norm, self.lr, self.momentum = model, model.ctx, max_norm, lr, momentum
         self.pairs = model.parameters()
         self.velocity = [torch.zeros_like(w) for w, _ in self.pairs]
@@ -119,8 +136,21 @@ class Step:
         self.batch = PreparedBatch(self.tensors)
         self.clip = PreparedBatch([Tensor(o, o) for o in self.sent])
         self.norm_coef = torch.zeros(2, device="cuda")
+        # what is added to the weights: the momentum itself, or of the blocks' matrices the nearest matrix with singular values about one, with rows of tall
+        # matrices as long as those of wide ones
+        self.steps, self.turned = list(self.velocity), None
+        if orthogonal:
+            at = [i for i, (w, _) in enumerate(self.pairs) if w.dim() == 2 and min(w.shape) > 1 and w is not model.table and not self._is_gate(w)]
+            for i in at:
+                self.steps[i] = torch.empty_like(self.velocity[i])
+            self.turned = PreparedBatch([Tensor(self.velocity[i], self.steps[i]) for i in at])
+            self.scales = [max(1.0, self.pairs[i][0].shape[0] / self.pairs[i][0].shape[1]) ** 0.5 for i in at]
+            self.ctx.reserve_orthogonalize(self.pairs[0][0].dtype, [tuple(self.pairs[i][0].shape) for i in at])
         flats = [g.view(-1) for _, g in self.pairs if g.dim() == 2]
         self.flats = flats[:32]                                # one estimate takes up to 32 buffers
+
+    def _is_gate(self, w) -> bool:
+        return any(w is b["gate"] for b in self.m.blocks)
 
     def entropy(self, step: int) -> float:
         return self.ctx.entropy_estimate(self.flats, STRIDE, CHUNK, 7, step, BINS).h_diff_nats
@@ -139,26 +169,38 @@ class Step:
         c.clip_batch(self.clip, self.max_norm, self.norm_coef)
         torch._foreach_mul_(self.velocity, self.momentum)
         torch._foreach_add_(self.velocity, self.sent)
-        torch._foreach_add_([w for w, _ in self.pairs], self.velocity, alpha=-self.lr)
+        if self.turned is not None:
+            c.orthogonalize_batch(self.turned, scales=self.scales)
+        torch._foreach_add_([w for w, _ in self.pairs], self.steps, alpha=-self.lr)
 
 
 def train(layers=4, hidden=512, ff=2048, tokens=1024, sequence=256, steps=40, window=5, dtype=torch.float32, lr=0.5, momentum=0.9,
-          max_norm=1.0, seed=0, report=None):
-    """Trains and returns the losses; ``report``: called with a dict per window."""
+          max_norm=1.0, seed=0, report=None, vocab=0, update="momentum"):
+    """Trains and returns the losses; ``report``: called with a dict per window.  ``vocab``: the inputs are tokens of that many words; ``update``: "momentum"
+    or "orthogonal"."""
+    if update not in ("momentum", "orthogonal"):
+        raise ValueError("update must be momentum or orthogonal")
     ctx = Context(0, max_bins=BINS, max_rank=max(RANKS), max_rows=64, max_cols=64)
-    teacher = Model(ctx, layers, hidden, ff, tokens, sequence, dtype, seed=seed + 1)
-    model = Model(ctx, layers, hidden, ff, tokens, sequence, dtype, seed=seed + 2)
-    step = Step(model, max_norm, lr, momentum)
+    teacher = Model(ctx, layers, hidden, ff, tokens, sequence, dtype, seed=seed + 1, vocab=vocab)
+    model = Model(ctx, layers, hidden, ff, tokens, sequence, dtype, seed=seed + 2, vocab=vocab)
+    step = Step(model, max_norm, lr, momentum, orthogonal=update == "orthogonal")
     state = RankState()
     prm = RankParams(*reference_shape([w.shape for w, _ in step.pairs]), min(RANKS), max(RANKS), allowed=RANKS, total_iters=steps)
     g = torch.Generator(device="cuda").manual_seed(seed)
     losses, entropies, rank = [], [], 0
     for i in range(steps):
-        x = torch.randn(tokens, hidden, generator=g, device="cuda").to(dtype)
-        target = teacher.forward(x).clone()
-        diff = (model.forward(x).float() - target.float())
+        if vocab:
+            x = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
+            target, out = teacher.forward_tokens(x).clone(), model.forward_tokens(x)
+        else:
+            x = torch.randn(tokens, hidden, generator=g, device="cuda").to(dtype)
+            target, out = teacher.forward(x).clone(), model.forward(x)
+        diff = (out.float() - target.float())
         losses.append(float(0.5 * diff.square().sum(1).mean()))
-        model.backward((diff / tokens).to(dtype))
+        if vocab:
+            model.backward_tokens(x, (diff / tokens).to(dtype))
+        else:
+            model.backward((diff / tokens).to(dtype))
         entropies.append(step.entropy(i))
         step.update(rank)
         if len(entropies) == window:
@@ -175,13 +217,14 @@ def train(layers=4, hidden=512, ff=2048, tokens=1024, sequence=256, steps=40, wi
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
-    for name, value in (("layers", 4), ("hidden", 512), ("ff", 2048), ("tokens", 1024), ("sequence", 256), ("steps", 40), ("window", 5)):
+    for name, value in (("layers", 4), ("hidden", 512), ("ff", 2048), ("tokens", 1024), ("sequence", 256), ("steps", 40), ("window", 5), ("vocab", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--dtype", choices=["f32", "bf16"], default="f32")
     ap.add_argument("--lr", type=float, default=0.5)
+    ap.add_argument("--update", choices=["momentum", "orthogonal"], default="momentum")
     a = ap.parse_args(argv)
     losses = train(a.layers, a.hidden, a.ff, a.tokens, a.sequence, a.steps, a.window, torch.float32 if a.dtype == "f32" else torch.bfloat16,
-                   lr=a.lr, report=lambda d: print(json.dumps(d), flush=True))
+                   lr=a.lr, report=lambda d: print(json.dumps(d), flush=True), vocab=a.vocab, update=a.update)
     print(json.dumps({"first_loss": losses[0], "last_loss": losses[-1]}))
 
 
