@@ -609,7 +609,8 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
  * With a, b, c = 3.4445, -4.7750, 2.0315 and five steps all singular values
  * that are not tiny come out between 0.7 and 1.2.  A vector is a matrix of one
  * row.  After a decompress and clipping, grad and grad_out are both the
- * decompressed gradient (in place); otherwise no output overlaps an input.
+ * decompressed gradient (in place); otherwise no output overlaps an input, and
+ * no two entries have one output.
  * All products are on the smaller side of a matrix, of fp16 planes that hold 22
  * bits of every operand (bf16 gradients: all of theirs), summed in fp32; the
  * norm's squares and sums are in 64 bits.  A step's error counts twelve times
@@ -642,8 +643,8 @@ int edgc_orthogonalize_batch(edgc_ctx* ctx, const edgc_tensor* tensors, uint32_t
  *     dtable[v] = round_dtype(scale * sum of dy[t] over ids[t] - first_id = v)
  * table, dtable: vocab x hidden; out, dy: tokens x hidden; row-major of one dtype,
  * with leading dimensions.  ids: device, int32 or int64 (id_bytes 4 or 8).
- * Sums are in fp32 in the order of the tokens (in runs of 32 of a row's and
- * those in order): the same tokens give the same bits.  A row without a token
+ * Sums are in fp32, in the order of a row's tokens (by runs of up to 32 of them,
+ * then the runs): the same call gives the same bits.  A row without a token
  * becomes zeros; accumulate != 0 adds to what is there, and leaves such a row.
  * No output may overlap an input.  tokens = 0 does nothing (backward without
  * accumulate: all rows become zeros).

@@ -189,11 +189,8 @@ class _FF(C.Structure):
                 ("dtype", C.c_int32), ("act", C.c_int32)]
 
 
-class _Heads(C.Structure):
-    _fields_ = [("p", C.c_void_p), ("token", C.c_uint64), ("head", C.c_uint64)]
-
-
-_pack_heads = struct.Struct("@PQQ").pack        # a tenth of the time that a ctypes structure takes to build
+# An edgc_heads: address, elements from a token and from a head to the next.  (A ctypes structure takes ten times as long to build.)
+_pack_heads = struct.Struct("@PQQ").pack
 
 
 @dataclass
@@ -502,6 +499,11 @@ def _check_dense(names, tensors, dtype, shape) -> None:
             _bad_dense(names, tensors, dtype, shape)
 
 
+def _devices(tensors) -> set:
+    """Where the gradients of a list, and what is made of them, lie."""
+    return {g.get_device() for t in tensors for g in (t.grad, t.grad_out) if g is not None}
+
+
 class PreparedBatch:
     """The descriptor array of a list of :class:`Tensor`, built once.  The batched calls take it in
     place of the list; only the two per-call flags are written again (``residual_is_zero`` from the
@@ -511,6 +513,7 @@ class PreparedBatch:
     def __init__(self, tensors: Sequence[Tensor]):
         self.tensors = list(tensors)
         self.arr, self.code = Context._marshal(self.tensors)
+        self.devices = _devices(self.tensors)
 
     def __len__(self):
         return len(self.tensors)
@@ -906,6 +909,8 @@ class Context:
         itself; ``scales``: one per tensor."""
         arr, code = self._gradients(tensors)
         n = len(tensors)
+        if not (tensors.devices if isinstance(tensors, PreparedBatch) else _devices(tensors)) <= {self.device}:
+            raise ValueError(f"tensors must be on the context's device, cuda:{self.device}")
         if scales is not None and len(scales) != n:
             raise ValueError("scales must be one per tensor")
         _check_u32(steps)

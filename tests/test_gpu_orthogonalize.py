@@ -212,7 +212,7 @@ def test_refusals():
     refused("reserve_orthogonalize", ctx.orthogonalize_batch, t)                # nothing reserved
     ctx.reserve_orthogonalize(F32, [(40, 50)])
     ctx.orthogonalize_batch(t)
-    ctx.orthogonalize_batch(t * 3)                                              # one after the other in the same scratch
+    ctx.orthogonalize_batch([edgc.Tensor(g, torch.empty_like(g)) for _ in range(3)])    # one after the other in the same scratch
     ctx.orthogonalize_batch([])
     refused("reserve_orthogonalize", ctx.orthogonalize_batch, [edgc.Tensor(torch.zeros(40, 500, device="cuda"), torch.zeros(40, 500, device="cuda"))])
     for steps in (0, 65):

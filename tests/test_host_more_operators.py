@@ -26,8 +26,13 @@ def test_orthogonalize_without_a_context_or_with_sizes_beyond_its_fields():
     assert L.edgc_orthogonalize_batch(None, None, 0, 0, 5, 1.0, 0.0, 0.0, 0.0, None, None) == b.EINVAL
     c = _no_context()
     t = [edgc.Tensor(torch.zeros(4, 4), torch.zeros(4, 4))]
-    with pytest.raises(edgc.EdgcError):                     # what fits is handed on
-        c.orthogonalize_batch(t, stream=STREAM)
+    for batch in (t, edgc.PreparedBatch(t)):                # host memory is not handed to a kernel
+        with pytest.raises(ValueError, match="device"):
+            c.orthogonalize_batch(batch, stream=STREAM)
+    c.device = -1                                           # (host tensors count as the context's)
+    for batch in (t, edgc.PreparedBatch(t)):
+        with pytest.raises(edgc.EdgcError):                 # what fits is handed on
+            c.orthogonalize_batch(batch, stream=STREAM)
     for steps in (-1, 2 ** 32 + 5):
         with pytest.raises(ValueError, match="2\\^32"):
             c.orthogonalize_batch(t, steps=steps, stream=STREAM)
@@ -89,7 +94,7 @@ def test_embed_without_a_context_and_with_what_it_does_not_take():
     assert L.edgc_reserve_embed(None, 1, 1, 1) == b.EINVAL
     assert L.edgc_embed_backward(None, 0, None, 8, 0, 0, None, 0, 1, 1, 1.0, None, 0, 0, None) == b.EINVAL
     c = _no_context()
-    c.device = -1                                           # (host tensors count as the context's)
+    c.device = -1
     table, ids, out = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64), torch.zeros(3, 8)
     with pytest.raises(edgc.EdgcError):                     # what fits is handed on
         c.embed_forward(table, ids, out, stream=STREAM)
@@ -144,3 +149,16 @@ def test_qk_norm_without_a_context_and_with_what_it_does_not_take():
     for sizes in ((2 ** 32 + 1, 4, 4, 4), (4, 2 ** 32 + 1, 4, 4), (4, 4, -1, 4), (4, 4, 4, 2 ** 32 + 1)):
         with pytest.raises(ValueError, match="2\\^32"):
             c.reserve_qk_norm(*sizes)
+
+
+def test_the_heads_descriptor_agrees_with_the_header(tmp_path):
+    src = tmp_path / "heads.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "edgc.h"\n'
+                   'int main(void) { printf("%zu %zu %zu %zu\\n", sizeof(edgc_heads), offsetof(edgc_heads, p), offsetof(edgc_heads, token), offsetof(edgc_heads, head));'
+                   ' return 0; }\n')
+    exe = tmp_path / "heads"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I" + os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    sizes = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    packed = b._pack_heads(0x1122334455667788, 3, 5)
+    assert sizes == [len(packed), 0, 8, 16]
+    assert [int.from_bytes(packed[at:at + 8], "little") for at in sizes[1:]] == [0x1122334455667788, 3, 5]
