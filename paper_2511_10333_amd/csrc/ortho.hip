@@ -242,14 +242,15 @@ bool coefs_bounded(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps)
 uint32_t ortho_places(const edgc_ctx* ctx, int bm) { return static_cast<uint32_t>(ctx->num_cu) * (bm == 256 ? 1 : 2); }
 // sums that workers can leave behind: at most two tiles per place
 uint64_t ortho_sums_elems(const edgc_ctx* ctx) { return 2ull * 256 * 256 * ctx->num_cu; }
-// the least tiles of k that are worth a worker, whose sums go through memory
-constexpr uint32_t ortho_least(int bm) { return bm == 64 ? 32 : 8; }
+// the least tiles of k that are worth a worker, whose sums go through memory: those of a small tile are soon done (of a hidden-512 block, products whose 16
+// tiles of k are shared among workers cost 230 us, 225 if not; a hidden-2048 block's, in tiles of 128 x 128, 3616 and 3841)
+constexpr uint32_t ortho_least(int bm) { return bm == 64 ? 64 : 8; }
 
-template <int BM, int BN, int PA, int PB, bool TB, typename T>
+template <int BM, int PA, int PB, bool TB, typename T>
 hipError_t prepare_ortho_tiles()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ortho_gemm<BM, BN, PA, PB, TB, T>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               kOrthoLds<BM, BN, PB, TB>);
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ortho_gemm<BM, PA, PB, TB, T>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               kOrthoLds<BM, PB, TB>);
 }
 
 struct OrthoPass {
@@ -269,7 +270,7 @@ struct OrthoPass {
     Mat mats[kOrthoGroup] = {};
     uint32_t n = 0;                             // of them
 
-    template <int BM, int BN, int PA, int PB, bool TB, typename T>
+    template <int BM, int PA, int PB, bool TB, typename T>
     int launch(OrthoArgs& args, int kid)
     {
         uint32_t tiles = 0;
@@ -277,9 +278,9 @@ struct OrthoPass {
         for (uint32_t i = 0; i < args.count; ++i) {
             OrthoProblem& p = args.p[i];
             p.tiles_m = (p.M + BM - 1) / BM;
-            p.tiles_n = (p.N + BN - 1) / BN;
+            p.tiles_n = (p.N + BM - 1) / BM;
             p.first = tiles;
-            tiles += tiles_of<BM, BN, TB>(p);
+            tiles += tiles_of<BM, TB>(p);
             const double k = static_cast<double>(p.ktiles) * kOrthoK<PA, PB>;
             flops += (TB ? 2.0 : 1.0) * p.M * p.N * k * (PA + PB - 1);
             bytes += 2.0 * k * (static_cast<double>(p.M) * PA + static_cast<double>(p.N) * PB);
@@ -305,32 +306,33 @@ struct OrthoPass {
             count_rest();
         }
         args.part = ctx->ortho.sums;
-        EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ortho_gemm<BM, BN, PA, PB, TB, T><<<args.whole + args.workers, 256, kOrthoLds<BM, BN, PB, TB>, st>>>(args));
+        EDGC_LAUNCH(ctx, st, kid, bytes, flops, k_ortho_gemm<BM, PA, PB, TB, T><<<args.whole + args.workers, 256, kOrthoLds<BM, PB, TB>, st>>>(args));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         if (args.rest) {
-            EDGC_LAUNCH(ctx, st, KID_ORTHO_JOIN, 4.0 * BM * BN * (args.workers + args.rest), 0.0,
-                        k_ortho_join<BM, BN, TB, T><<<args.rest * (BM / 64) * (BN / 64), 256, 0, st>>>(args));
+            EDGC_LAUNCH(ctx, st, KID_ORTHO_JOIN, 4.0 * BM * BM * (args.workers + args.rest), 0.0,
+                        k_ortho_join<BM, TB, T><<<args.rest * (BM / 64) * (BM / 64), 256, 0, st>>>(args));
             EDGC_HIP_TRY(ctx, hipGetLastError());
         }
         return EDGC_OK;
     }
-    template <int BM, int BN, bool TB>
+    template <int BM, bool TB>
     static uint32_t tiles_of(const OrthoProblem& p)
     {
-        const uint32_t tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
-        return TB ? tm * tn : ortho_tiles<BM / BN>(tm, tn);
+        const uint32_t tm = (p.M + BM - 1) / BM, tn = (p.N + BM - 1) / BM;
+        return TB ? tm * tn : ortho_tiles(tm);
     }
     template <int PA, int PB, bool TB, typename T>
     int product(OrthoArgs& args, int kid)
     {
-        constexpr int BN = PA == 1 ? 256 : 128;         // one plane: a wave has room for 128 x 128
         std::stable_sort(args.p, args.p + args.count, [](const OrthoProblem& x, const OrthoProblem& y) { return x.ktiles > y.ktiles; });
         // The time that a tile shape would take, in us: `step`: for a tile of k of each of a compute unit's blocks at a time, `alone`: where a block has its
-        // compute unit for itself, `share`: for sums to go through memory and be joined.  Measured on products of 512 to 4096.
-        auto time_of = [&](auto bm, auto bn, double step, double alone, double share) {
+        // compute unit for itself; sums that go through memory and are joined cost a launch.  Measured on products of 512 to 4096.  A block of hidden 512 takes
+        // 231 us with tiles of 64 x 64, 329 with 128 x 128; odd matrices up to 2731 282 and 531; a block of hidden 2048 4540 and 3616.
+        auto time_of = [&](auto bm, double step, double alone) {
+            constexpr double share = 8.0;
             double steps = 0.0, tiles = 0.0, longest = 0.0;
             for (uint32_t i = 0; i < args.count; ++i) {
-                const double n = tiles_of<bm, bn, TB>(args.p[i]);
+                const double n = tiles_of<bm, TB>(args.p[i]);
                 tiles += n;
                 steps += n * args.p[i].ktiles;
                 longest = std::max(longest, 1.0 * args.p[i].ktiles);
@@ -339,20 +341,21 @@ struct OrthoPass {
             if (tiles >= places || longest <= least) return std::max(step * steps / places, alone * longest);
             return share + std::max(step * steps / places, alone * std::min(longest, least));
         };
-        using std::integral_constant;
-        using Large = integral_constant<int, 256>;
-        using Middle = integral_constant<int, 128>;
-        using Small = integral_constant<int, 64>;
-        constexpr double work = PA == 1 ? 1.0 : PB == 1 ? 2.0 / 3.0 : 1.0;     // a tile of k: 64 of one product, or 32 of three or two
-        const double large = time_of(Large{}, integral_constant<int, BN>{}, work * (PA == 1 ? 2.0 : 1.5), work * (PA == 1 ? 2.0 : 1.5), 8.0),
-                     middle = time_of(Middle{}, Middle{}, work * 1.9, work * 1.0, 8.0);
+        using Large = std::integral_constant<int, 256>;
+        using Middle = std::integral_constant<int, 128>;
+        using Small = std::integral_constant<int, 64>;
+        constexpr double work = PA == 1 || PB == 2 ? 1.0 : 2.0 / 3.0;     // a tile of k: 64 of one product, or 32 of three or two
+        const double middle = time_of(Middle{}, work * 1.58, work * 0.9);
         // (one plane of a transposed operand is too narrow for the small tiles' reads)
         if constexpr (!(TB && PB == 1)) {
-            const double small = time_of(Small{}, Small{}, work * 1.0, work * 0.4, 8.0);
-            if (small < large && small < middle) return launch<64, 64, PA, PB, TB, T>(args, kid);
+            if (time_of(Small{}, work * 0.53, work * 0.33) < middle) return launch<64, PA, PB, TB, T>(args, kid);
         }
-        if (large <= middle) return launch<256, BN, PA, PB, TB, T>(args, kid);
-        return launch<128, 128, PA, PB, TB, T>(args, kid);
+        // The first products of bf16 matrices, of one plane: for a block of hidden 4096 they take 880 us, with tiles of 128 x 128 949.  (Of two planes, with
+        // two sums, a wave has room for 128 x 64, and tiles of 256 x 128 took 1643 us for the products of a hidden-2048 block's smaller sides, not 1505.)
+        if constexpr (PA == 1) {
+            if (time_of(Large{}, work * 2.2, work * 2.2) <= middle) return launch<256, PA, PB, TB, T>(args, kid);
+        }
+        return launch<128, PA, PB, TB, T>(args, kid);
     }
     // a product of two matrices of the smaller side, or the first of a segment
     static OrthoProblem symmetric(const Mat& m, const uint16_t* a, const uint16_t* b, uint16_t* out, double alpha)
@@ -523,12 +526,13 @@ int check_shape(edgc_ctx* ctx, uint64_t m, uint64_t n)
 
 int prepare_ortho_kernels(edgc_ctx* ctx)
 {
-    for (hipError_t e : {prepare_ortho_tiles<64, 64, 1, 1, false, void>(), prepare_ortho_tiles<64, 64, 2, 2, false, void>(),
-                         prepare_ortho_tiles<64, 64, 2, 2, true, void>(), prepare_ortho_tiles<64, 64, 2, 2, true, float>(),
-                         prepare_ortho_tiles<64, 64, 2, 2, true, __bf16>(), prepare_ortho_tiles<256, 256, 1, 1, false, void>(), prepare_ortho_tiles<256, 128, 2, 2, false, void>(),
-                         prepare_ortho_tiles<256, 128, 2, 1, true, void>(), prepare_ortho_tiles<256, 128, 2, 2, true, void>(),
-                         prepare_ortho_tiles<256, 128, 2, 2, true, float>(), prepare_ortho_tiles<256, 128, 2, 1, true, __bf16>(),
-                         prepare_ortho_tiles<256, 128, 2, 2, true, __bf16>()})
+    for (hipError_t e : {prepare_ortho_tiles<64, 1, 1, false, void>(), prepare_ortho_tiles<64, 2, 2, false, void>(),
+                         prepare_ortho_tiles<64, 2, 2, true, void>(), prepare_ortho_tiles<64, 2, 2, true, float>(),
+                         prepare_ortho_tiles<64, 2, 2, true, __bf16>(), prepare_ortho_tiles<128, 1, 1, false, void>(),
+                         prepare_ortho_tiles<256, 1, 1, false, void>(), prepare_ortho_tiles<128, 2, 2, false, void>(),
+                         prepare_ortho_tiles<128, 2, 1, true, void>(), prepare_ortho_tiles<128, 2, 2, true, void>(),
+                         prepare_ortho_tiles<128, 2, 2, true, float>(), prepare_ortho_tiles<128, 2, 1, true, __bf16>(),
+                         prepare_ortho_tiles<128, 2, 2, true, __bf16>()})
         EDGC_HIP_TRY(ctx, e);
     return EDGC_OK;
 }

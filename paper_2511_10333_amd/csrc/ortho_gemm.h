@@ -5,12 +5,12 @@
 // the fourth is left out: below 2^-24 of the product, of either sign.  bf16 inputs are one plane, exactly.  (bf16 planes would take three and six.)
 //
 // The planes lie next to each other: 32 neighbours of a row's hi, then their lo, 128 bytes.  A tile of 32 k of both is 64 columns of memory, and a
-// step's fragments are read from LDS once for its three products.  (As three sums over k, with each plane brought and read twice, tiles of 128 x 128
-// took 4.64 ms instead of 3.80 for a hidden-2048 block.)
+// step's fragments are read from LDS once for its three products.  (As three sums over k, with each plane brought and read twice, a hidden-2048 block took
+// 4.64 ms instead of 3.80 at the time.)
 //
 // The two small products have a sum of their own.  An MFMA adds its 16 k to the sum in several roundings, and the errors of these, not of the planes, are
 // what an update is off by: with all three products in one sum it was 3.4e-6 off for a block of hidden 512 and 3.7e-6 for odd matrices up to 2731, where
-// fp32 products are 2.5e-6 and 2.2e-6; with two sums 2.1e-6 and 1.9e-6.  So a wave has 128 x 64 of a tile of 256 x 128.
+// fp32 products are 2.5e-6 and 2.2e-6; with two sums 1.6e-6 and 1.8e-6.
 #pragma once
 
 #include "ff_gemm.h"
@@ -46,7 +46,7 @@ struct OrthoArgs {
     OrthoProblem p[kOrthoProblems];
     uint32_t count, whole, rest, workers;
     uint32_t steps;                     // of the other tiles, all together
-    float* part;                        // [workers + rest][BM * BN]
+    float* part;                        // [workers + rest][BM * BM]
 };
 static_assert(sizeof(OrthoArgs) <= 4032, "kernel arguments are limited to 4 KiB");
 
@@ -187,10 +187,10 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
     ff_wave_sync();
 }
 
-template <bool SYM, int BM, int BN>
+template <bool SYM>
 __device__ __forceinline__ void ortho_place(const OrthoProblem& p, uint32_t tile, uint32_t& tm, uint32_t& tn)
 {
-    if constexpr (SYM) ortho_tile_of<BM / BN>(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
+    if constexpr (SYM) ortho_tile_of(tile - p.first, p.tiles_m, tm, tn);
     else ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
 }
 __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
@@ -203,27 +203,27 @@ __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
 // k of a tile, bytes of either operand's tile in LDS, tiles of A and B that are there, all of LDS.  Blocks of 256 rows have a compute unit for themselves, of the
 // others two share it.  A tile of 64 x 64 is multiplied in a fraction of the time that the next takes to come: four are on their way.
 template <int PA, int PB> constexpr int kOrthoK = PA == 1 && PB == 1 ? 64 : 32;
-template <int BN, int PB, bool TB> constexpr uint32_t kOrthoBytesB = TB ? 32u * BN * PB * 2u : BN * 128u;
+template <int BM, int PB, bool TB> constexpr uint32_t kOrthoBytesB = TB ? 32u * BM * PB * 2u : BM * 128u;
 template <int BM> constexpr uint32_t kOrthoTilesA = BM == 256 ? 3u : BM == 128 ? 2u : 5u;
 template <int BM> constexpr uint32_t kOrthoTilesB = BM == 64 ? 5u : 2u;
-template <int BM, int BN, int PB, bool TB> constexpr uint32_t kOrthoLds = kOrthoTilesA<BM> * BM * 128u + kOrthoTilesB<BM> * kOrthoBytesB<BN, PB, TB>;
+template <int BM, int PB, bool TB> constexpr uint32_t kOrthoLds = kOrthoTilesA<BM> * BM * 128u + kOrthoTilesB<BM> * kOrthoBytesB<BM, PB, TB>;
 
 // The sums of a tile over tiles kt0 to kt1 of k, by 2 x 2 waves: of a wave, I x J squares of 32 x 32.  The loop of ff_gemm.h: while a step of 16 k is
 // multiplied, the fragments of the next are read (in a tile's last step, the first of the next tile); the barrier before the last step ends the reads of the
 // tile, and from there on B of the tile after the next is asked for, into its place.  A, in three buffers (LARGE), is asked for in the first half of
 // the steps: the barrier of tile t finds tile t + 1 there, after which A of tile t + 2 alone was asked for.  (Smaller blocks ask for both operands there, as many
 // tiles ahead as they have buffers.)
-template <int BM, int BN, int PA, int PB, bool TB>
+template <int BM, int PA, int PB, bool TB>
 __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char* lds, uint32_t lane, uint32_t wave, uint32_t m0, uint32_t n0, uint32_t kt0, uint32_t kt1,
-                                           f32x16 (&acc)[BM / 64][BN / 64])
+                                           f32x16 (&acc)[BM / 64][BM / 64])
 {
     constexpr bool LARGE = BM == 256, SMALL = PA + PB > 2;                          // SMALL: there are small products
-    constexpr int I = BM / 64, J = BN / 64, BK = kOrthoK<PA, PB>, KK = BK / 16;     // squares of a wave; k of a tile; steps of 16 k
-    constexpr int WIDTH = BN * PB;                                                 // TB: elements of a tile's row of k
-    constexpr int LA = BM / 32, LB = TB ? WIDTH / 64 : BN / 32;                    // a wave's loads of a tile
+    constexpr int I = BM / 64, J = BM / 64, BK = kOrthoK<PA, PB>, KK = BK / 16;     // squares of a wave; k of a tile; steps of 16 k
+    constexpr int WIDTH = BM * PB;                                                 // TB: elements of a tile's row of k
+    constexpr int LA = BM / 32, LB = TB ? WIDTH / 64 : BM / 32;                    // a wave's loads of a tile
     constexpr int FA = I * PA, FB = J * PB, F = FA + FB, MM = I * J * (PA + PB - 1);    // fragments and products of a step
     // lds: [kBufsA][kBytesA], [kBufsB][kBytesB]
-    constexpr uint32_t kBufsA = kOrthoTilesA<BM>, kBufsB = kOrthoTilesB<BM>, kBytesA = BM * 128, kBytesB = kOrthoBytesB<BN, PB, TB>, kAtB = kBufsA * kBytesA;
+    constexpr uint32_t kBufsA = kOrthoTilesA<BM>, kBufsB = kOrthoTilesB<BM>, kBytesA = BM * 128, kBytesB = kOrthoBytesB<BM, PB, TB>, kAtB = kBufsA * kBytesA;
     constexpr uint32_t AHEAD = kBufsB;                  // tiles
     static_assert(!TB || PA == 2, "the transposed operand is the gradient, multiplied by two planes");
     static_assert(PA == PB || (PB == 1 && TB), "");
@@ -345,21 +345,21 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
 }
 
 // Where a worker leaves the sums of a tile: in the order of its registers
-template <int BM, int BN>
+template <int BM>
 __device__ __forceinline__ float4* ortho_slot(float* part, uint32_t slot, uint32_t i, uint32_t j, uint32_t q, uint32_t tid)
 {
-    return ff_slot<BM, BN, BN / 64>(part, slot, i, j, q, tid);
+    return ff_slot<BM, BM, BM / 64>(part, slot, i, j, q, tid);
 }
 
-// A block of 2 x 2 waves makes a BM x BN tile of the output; PA, PB: planes of the operands.  !TB: the output is symmetric, M = N.  T: void, planes, or
+// A block of 2 x 2 waves makes a BM x BM tile of the output; PA, PB: planes of the operands.  !TB: the output is symmetric, M = N.  T: void, planes, or
 // the caller's type.
-template <int BM, int BN, int PA, int PB, bool TB, typename T>
+template <int BM, int PA, int PB, bool TB, typename T>
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const OrthoArgs args)
 {
     constexpr bool SYM = !TB;
-    constexpr int I = BM / 64, J = BN / 64;
+    constexpr int I = BM / 64, J = BM / 64;
     extern __shared__ __align__(16) unsigned char lds[];        // ortho_sums' tiles
-    static_assert(4 * 32 * kOrthoRow * 4 <= kOrthoLds<BM, BN, PB, TB>, "the waves' parts of LDS in ortho_square fit where the tiles were");
+    static_assert(4 * 32 * kOrthoRow * 4 <= kOrthoLds<BM, PB, TB>, "the waves' parts of LDS in ortho_square fit where the tiles were");
 
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / 2, wn = wave % 2;
     const bool shares = blockIdx.x >= args.whole;
@@ -383,11 +383,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
         }
         step += kt1 - kt0;
         uint32_t tm, tn;
-        ortho_place<SYM, BM, BN>(p, tile, tm, tn);
-        const uint32_t m0 = tm * BM, n0 = tn * BN;
+        ortho_place<SYM>(p, tile, tm, tn);
+        const uint32_t m0 = tm * BM, n0 = tn * BM;
 
         f32x16 acc[I][J];
-        ortho_sums<BM, BN, PA, PB, TB>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
+        ortho_sums<BM, PA, PB, TB>(p, lds, lane, wave, m0, n0, kt0, kt1, acc);
 
         if (kt1 - kt0 == p.ktiles) {
             // (The lane is hidden from what comes before, and all loads are waited for here: addresses kept over the products would be spilled, and waiting for
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
                 for (int j = 0; j < J; ++j)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *ortho_slot<BM, BN>(args.part, worker + tile - args.whole, i, j, q, tid) =
+                        *ortho_slot<BM>(args.part, worker + tile - args.whole, i, j, q, tid) =
                             float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         }
         if (step < steps_end) __syncthreads();      // the next tile's rows go where this one's sums were
@@ -432,11 +432,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
 }
 
 // Adds up the sums that several workers have of a tile, in the order of the workers: one square of every wave's part per block
-template <int BM, int BN, bool TB, typename T>
+template <int BM, bool TB, typename T>
 __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
 {
     constexpr bool SYM = !TB;
-    constexpr uint32_t I = BM / 64, J = BN / 64;
+    constexpr uint32_t I = BM / 64, J = BM / 64;
     __shared__ __align__(16) float stage[4 * 32 * kOrthoRow];
     const uint32_t at = blockIdx.x / (I * J), i = blockIdx.x / J % I, j = blockIdx.x % J, tile = args.whole + at;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
@@ -448,15 +448,15 @@ __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
     while (last + 1 < args.workers && ortho_share(args, last + 1) < s1) ++last;
     if (first == last) return;                      // one, which has finished it
     uint32_t tm, tn;
-    ortho_place<SYM, BM, BN>(p, tile, tm, tn);
-    const uint32_t m = tm * BM + (wave / 2 * I + i) * 32, n = tn * BN + (wave % 2 * J + j) * 32;
+    ortho_place<SYM>(p, tile, tm, tn);
+    const uint32_t m = tm * BM + (wave / 2 * I + i) * 32, n = tn * BM + (wave % 2 * J + j) * 32;
     if (SYM && n > m) return;
     f32x16 acc = {};
 #pragma unroll 4
     for (uint32_t w = first; w <= last; ++w) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float4 v = *ortho_slot<BM, BN>(args.part, w + at, i, j, q, tid);
+            const float4 v = *ortho_slot<BM>(args.part, w + at, i, j, q, tid);
             acc[4 * q] += v.x; acc[4 * q + 1] += v.y; acc[4 * q + 2] += v.z; acc[4 * q + 3] += v.w;
         }
     }
