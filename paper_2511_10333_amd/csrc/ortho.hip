@@ -272,11 +272,13 @@ struct OrthoPass {
     {
         uint32_t tiles = 0;
         double flops = 0.0, bytes = 0.0;
+        std::fill(args.first, args.first + kOrthoProblems, UINT32_MAX);
+        std::fill(args.begin, args.begin + kOrthoProblems, UINT32_MAX);
         for (uint32_t i = 0; i < args.count; ++i) {
             OrthoProblem& p = args.p[i];
             p.tiles_m = (p.M + BM - 1) / BM;
             p.tiles_n = (p.N + BM - 1) / BM;
-            p.first = tiles;
+            args.first[i] = tiles;
             tiles += tiles_of<BM, TB>(p);
             const double k = static_cast<double>(p.ktiles) * kOrthoK<PA, PB>;
             flops += (TB ? 2.0 : 1.0) * p.M * p.N * k * (PA + PB - 1);
@@ -289,9 +291,9 @@ struct OrthoPass {
             args.steps = 0;
             for (uint32_t i = 0; i < args.count; ++i) {
                 OrthoProblem& p = args.p[i];
-                const uint32_t end = i + 1 < args.count ? args.p[i + 1].first : tiles;
-                p.begin = args.steps;
-                if (end > args.whole) args.steps += (end - std::max(p.first, args.whole)) * p.ktiles;
+                const uint32_t end = i + 1 < args.count ? args.first[i + 1] : tiles;
+                args.begin[i] = args.steps;
+                if (end > args.whole) args.steps += (end - std::max(args.first[i], args.whole)) * p.ktiles;
             }
         };
         count_rest();

@@ -28,8 +28,7 @@ struct OrthoProblem {
     uint32_t M, N;                      // of the output
     uint32_t ktiles;                    // tiles of k
     uint32_t spread;                    // one plane of an operand that has two is taken
-    uint32_t tiles_m, tiles_n, first;   // tiles of the output; the first's number
-    uint32_t begin;                     // the first of its steps of k among those that are shared
+    uint32_t tiles_m, tiles_n;          // tiles of the output
     uint32_t rows, cols;                // of `out`, with what is padding: zeros
     uint16_t* out;                      // planes, or
     void* to;                           // the caller's matrix
@@ -43,19 +42,25 @@ constexpr uint32_t kOrthoProblems = 20;
 // Tiles are given out as in FfArgs: those of whole rounds of the compute units a block each, the others' steps of k in even shares to `workers` further
 // blocks, which leave the sums of tiles that they have a part of in `part`, for k_ortho_join.  Problems may differ in their steps: the longest come first.
 struct OrthoArgs {
-    OrthoProblem p[kOrthoProblems];
-    uint32_t count, whole, rest, workers;
+    uint32_t whole, rest, workers;
     uint32_t steps;                     // of the other tiles, all together
     float* part;                        // [workers + rest][BM * BM]
+    // A problem's first tile, and the first of its steps of k that are shared: next to each other, for ortho_problem_of.  Of problems that are not there, the
+    // largest number.
+    uint32_t first[kOrthoProblems], begin[kOrthoProblems];
+    uint32_t count;
+    OrthoProblem p[kOrthoProblems];
 };
 static_assert(sizeof(OrthoArgs) <= 4032, "kernel arguments are limited to 4 KiB");
 
 __host__ __device__ inline uint32_t ortho_share(const OrthoArgs& a, uint32_t worker) { return static_cast<uint32_t>(static_cast<uint64_t>(a.steps) * worker / a.workers); }
-__device__ __forceinline__ const OrthoProblem& ortho_problem_of(const OrthoArgs& a, uint32_t tile)
+// The problem that tile (or step) `at` is of.  (All numbers are loaded at once: one after the other, each with its problem, they were waited for in turn.)
+__device__ __forceinline__ uint32_t ortho_problem_of(const uint32_t (&first)[kOrthoProblems], uint32_t at)
 {
     uint32_t i = 0;
-    while (i + 1 < a.count && tile >= a.p[i + 1].first) ++i;
-    return a.p[i];
+#pragma unroll
+    for (uint32_t k = 1; k < kOrthoProblems; ++k) i += at >= first[k];
+    return __builtin_amdgcn_readfirstlane(i);
 }
 // hi and lo of eight neighbours
 __device__ __forceinline__ void ortho_planes(const float (&v)[8], u32x4& hi, u32x4& lo)
@@ -190,8 +195,8 @@ __device__ __forceinline__ void ortho_square(const OrthoProblem& p, float* mine,
 template <bool SYM>
 __device__ __forceinline__ void ortho_place(const OrthoProblem& p, uint32_t tile, uint32_t& tm, uint32_t& tn)
 {
-    if constexpr (SYM) ortho_tile_of(tile - p.first, p.tiles_m, tm, tn);
-    else ff_tile_of(tile - p.first, p.tiles_m, p.tiles_n, tm, tn);
+    if constexpr (SYM) ortho_tile_of(tile, p.tiles_m, tm, tn);
+    else ff_tile_of(tile, p.tiles_m, p.tiles_n, tm, tn);
 }
 __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
 {
@@ -367,23 +372,18 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
     uint32_t step = shares ? ortho_share(args, worker) : 0;
     const uint32_t steps_end = shares ? ortho_share(args, worker + 1) : 1;
     while (step < steps_end) {
-        uint32_t tile = blockIdx.x, pi = 0, kt0 = 0, kt1;
-        if (shares) {
-            while (pi + 1 < args.count && step >= args.p[pi + 1].begin) ++pi;
-        } else {
-            while (pi + 1 < args.count && tile >= args.p[pi + 1].first) ++pi;
-        }
+        const uint32_t pi = shares ? ortho_problem_of(args.begin, step) : ortho_problem_of(args.first, blockIdx.x);
         const OrthoProblem& p = args.p[pi];
-        kt1 = p.ktiles;
+        uint32_t tile = blockIdx.x, kt0 = 0, kt1 = p.ktiles;
         if (shares) {
-            const uint32_t in = (step - p.begin) / p.ktiles;
-            tile = max(p.first, args.whole) + in;
-            kt0 = step - p.begin - in * p.ktiles;
+            const uint32_t from = step - args.begin[pi], in = from / p.ktiles;
+            tile = max(args.first[pi], args.whole) + in;
+            kt0 = from - in * p.ktiles;
             kt1 = min(p.ktiles, kt0 + (steps_end - step));
         }
         step += kt1 - kt0;
         uint32_t tm, tn;
-        ortho_place<SYM>(p, tile, tm, tn);
+        ortho_place<SYM>(p, tile - args.first[pi], tm, tn);
         const uint32_t m0 = tm * BM, n0 = tn * BM;
 
         f32x16 acc[I][J];
@@ -440,15 +440,16 @@ __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
     __shared__ __align__(16) float stage[4 * 32 * kOrthoRow];
     const uint32_t at = blockIdx.x / (I * J), i = blockIdx.x / J % I, j = blockIdx.x % J, tile = args.whole + at;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-    const OrthoProblem& p = ortho_problem_of(args, tile);
-    const uint32_t s0 = p.begin + (tile - max(p.first, args.whole)) * p.ktiles, s1 = s0 + p.ktiles;
+    const uint32_t pi = ortho_problem_of(args.first, tile);
+    const OrthoProblem& p = args.p[pi];
+    const uint32_t s0 = args.begin[pi] + (tile - max(args.first[pi], args.whole)) * p.ktiles, s1 = s0 + p.ktiles;
     // the workers that have a step of this tile
     uint32_t first = static_cast<uint32_t>(static_cast<uint64_t>(s0) * args.workers / args.steps), last = static_cast<uint32_t>(static_cast<uint64_t>(s1 - 1) * args.workers / args.steps);
     while (ortho_share(args, first + 1) <= s0) ++first;
     while (last + 1 < args.workers && ortho_share(args, last + 1) < s1) ++last;
     if (first == last) return;                      // one, which has finished it
     uint32_t tm, tn;
-    ortho_place<SYM>(p, tile, tm, tn);
+    ortho_place<SYM>(p, tile - args.first[pi], tm, tn);
     const uint32_t m = tm * BM + (wave / 2 * I + i) * 32, n = tn * BM + (wave % 2 * J + j) * 32;
     if (SYM && n > m) return;
     f32x16 acc = {};
