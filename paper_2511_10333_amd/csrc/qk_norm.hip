@@ -129,7 +129,7 @@ __device__ __forceinline__ float qk_head_sum(float v, uint32_t lanes)
     return v;
 }
 
-// A block has `per` tokens.  blockIdx.y: a share of the heads (few tokens, forward)
+// A block has `per` tokens.  Few tokens: blockIdx.z: queries, keys; forward, blockIdx.y: a share of the heads
 template <typename T, int N, int U, bool BACK>
 __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
 {
@@ -144,7 +144,8 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
         __syncthreads();
     };
     // queries, then keys: of one of them the sums fit a wave's registers with three others on its SIMD (both: 161, a third of the blocks in a second round)
-    for (int K = 0; K < 2; ++K) {
+    const int K0 = gridDim.z > 1 ? blockIdx.z : 0, K1 = gridDim.z > 1 ? K0 + 1 : 2;
+    for (int K = K0; K < K1; ++K) {
         const QkHeads& h = a.h[K];
         const uint32_t share = (h.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share, h1 = min(h.heads, h0 + share), H = h1 > h0 ? h1 - h0 : 0u;
         float sums[U][2][BACK ? N : 1] = {};
@@ -159,12 +160,10 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
         }
         for (uint64_t b0 = t0; b0 < t1; b0 += kQkTokens) {
             const uint32_t n = static_cast<uint32_t>(min(static_cast<uint64_t>(kQkTokens), t1 - b0));
-            if (K == 0 || t1 - t0 > kQkTokens || BACK) turn_by(b0, n);
-            if (H == 0) continue;
             // heads of the tokens one after the other, a group of lanes each; forward, the next one's elements are on their way during a head
             const uint32_t items = n * H, rounds = (items + groups - 1) / groups;      // (all lanes of a wave take part in the sums)
-            const uint32_t tokens_on = groups / H, heads_on = groups - tokens_on * H;
-            uint32_t it = group, tok = group / H, hd = group - tok * H;
+            const uint32_t some = max(H, 1u), tokens_on = groups / some, heads_on = groups - tokens_on * some;
+            uint32_t it = group, tok = group / some, hd = group - tok * some;
             QkPack<T, N> v[U][2], d[U][2], next[U][2];
             auto ask = [&](QkPack<T, N> (&xs)[U][2], QkPack<T, N> (&ds)[U][2]) {
                 const uint64_t token = b0 + tok, head = h0 + hd;
@@ -183,6 +182,7 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
                 }
             };
             if (!BACK && it < items) ask(next, d);
+            if (K == K0 || t1 - t0 > kQkTokens || BACK) turn_by(b0, n);
             for (uint32_t round = 0; round < rounds; ++round) {
                 const bool there = it < items;
                 const uint64_t token = b0 + tok, head = h0 + hd;
@@ -334,10 +334,9 @@ int check_qk(edgc_ctx* ctx, const QkShape& s, const void* w_q, const void* w_k, 
 
 // f(type, elements of a pack, units of a lane): packs of 16 bytes where halves, or pairs, and what is not rotated are whole units of two of them
 template <typename F>
-int by_head(const QkShape& s, int interleaved, QkArgs& a, F&& f)
+int by_head(const QkShape& s, QkArgs& a, F&& f)
 {
     using std::integral_constant;
-    (void)interleaved;
     auto lanes = [&](uint32_t units) {
         a.lanes = 1;
         while (a.lanes < units && a.lanes < 64) a.lanes *= 2;
@@ -404,16 +403,18 @@ extern "C" int edgc_qk_norm_forward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t to
     a.positions = positions; a.inv_freq = inv_freq; a.tokens = tokens; a.dim = dim; a.pairs = rot / 2;
     a.interleaved = interleaved; a.pos_bytes = pos_bytes; a.eps = eps; a.inv_dim = 1.0f / static_cast<float>(dim);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return by_head(s, interleaved, a, [&](auto type, auto n, auto u) -> int {
+    return by_head(s, a, [&](auto type, auto n, auto u) -> int {
         using T = decltype(type);
         const uint64_t most = static_cast<uint64_t>(ctx->num_cu) * 8;
         a.per = static_cast<uint32_t>(std::max<uint64_t>(1, (tokens + most - 1) / most));
         const uint32_t blocks = static_cast<uint32_t>((tokens + a.per - 1) / a.per), groups = 256 / a.lanes;
-        // few tokens: a block for as many heads as it takes at a time
-        const uint32_t shares = blocks < static_cast<uint32_t>(ctx->num_cu) ? std::max(1u, std::min((std::max(heads_q, heads_k) + groups - 1) / groups, 64u)) : 1u;
+        // few tokens: a block for as many heads as it takes at a time, of queries or keys (eight tokens of 32 and 8 heads: 2.8 us, with
+        // both in turn 5.0)
+        const bool few = blocks < static_cast<uint32_t>(ctx->num_cu);
+        const uint32_t shares = few ? std::max(1u, std::min((std::max(heads_q, heads_k) + groups - 1) / groups, 64u)) : 1u;
         const double bytes = 2.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim;
         EDGC_LAUNCH(ctx, st, KID_QK_FORWARD, bytes, 0.0,
-                    k_qk_norm<T, n, u, false><<<dim3(blocks, shares), 256, kQkTokens * std::max(1u, a.pairs) * sizeof(float2), st>>>(a));
+                    k_qk_norm<T, n, u, false><<<dim3(blocks, shares, few && heads_k ? 2 : 1), 256, kQkTokens * std::max(1u, a.pairs) * sizeof(float2), st>>>(a));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         return EDGC_OK;
     });
@@ -475,15 +476,18 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
     a.positions = positions; a.inv_freq = inv_freq; a.tokens = tokens; a.dim = dim; a.pairs = rot / 2; a.part = ctx->qk.part;
     a.interleaved = interleaved; a.pos_bytes = pos_bytes; a.eps = eps; a.inv_dim = 1.0f / static_cast<float>(dim);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return by_head(s, interleaved, a, [&](auto type, auto n, auto u) -> int {
+    return by_head(s, a, [&](auto type, auto n, auto u) -> int {
         using T = decltype(type);
         uint32_t blocks = 0;
         if (tokens) {
-            const uint64_t most = std::min<uint64_t>(tokens, qk_most_blocks(ctx));
+            // few tokens: queries and keys in blocks of their own (1001 tokens of 7 and 3 heads of 72: 5.4 us, with both in turn 9.2)
+            const bool few = tokens <= qk_most_blocks(ctx) && heads_k;
+            const uint64_t most = std::min<uint64_t>(tokens, qk_most_blocks(ctx) / (few ? 2 : 1));
             a.per = static_cast<uint32_t>((tokens + most - 1) / most);
             blocks = static_cast<uint32_t>((tokens + a.per - 1) / a.per);
             const uint32_t groups = 256 / a.lanes, lds = std::max(kQkTokens * a.pairs * static_cast<uint32_t>(sizeof(float2)), groups * dim * 4u);
-            EDGC_LAUNCH(ctx, st, KID_QK_BACKWARD, 3.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim, 0.0, k_qk_norm<T, n, u, true><<<blocks, 256, lds, st>>>(a));
+            EDGC_LAUNCH(ctx, st, KID_QK_BACKWARD, 3.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim, 0.0,
+                        k_qk_norm<T, n, u, true><<<dim3(blocks, 1, few ? 2 : 1), 256, lds, st>>>(a));
             EDGC_HIP_TRY(ctx, hipGetLastError());
         }
         EDGC_LAUNCH(ctx, st, KID_QK_SUM, 8.0 * blocks * dim, 0.0,
