@@ -133,7 +133,7 @@ __device__ __forceinline__ float qk_head_sum(float v, uint32_t lanes)
 template <typename T, int N, int U, bool BACK>
 __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
 {
-    extern __shared__ float2 angles[];          // [kQkTokens][pairs]; BACK: then the sums
+    extern __shared__ float2 angles[];          // [kQkTokens][pairs]; BACK: and [groups][dim] sums
     const uint32_t lane = threadIdx.x & 63, in = lane & (a.lanes - 1), group = (threadIdx.x / a.lanes), groups = 256 / a.lanes;
     const uint64_t t0 = static_cast<uint64_t>(blockIdx.x) * a.per, t1 = min(a.tokens, t0 + a.per);
     const uint32_t units = (a.dim + 2 * N - 1) / (2 * N);
@@ -181,15 +181,16 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
                     }
                 }
             };
-            if (!BACK && it < items) ask(next, d);
-            if (K == K0 || t1 - t0 > kQkTokens || BACK) turn_by(b0, n);
+            // (on their way during the angles)
+            if (it < items) ask(BACK ? v : next, d);
+            if (K == K0 || t1 - t0 > kQkTokens) turn_by(b0, n);
             for (uint32_t round = 0; round < rounds; ++round) {
                 const bool there = it < items;
                 const uint64_t token = b0 + tok, head = h0 + hd;
                 T* const out = static_cast<T*>(h.out) + token * h.out_token + head * h.out_head;
                 const float2* const turn = angles + (there ? tok : 0u) * a.pairs;
                 if constexpr (BACK) {
-                    if (there) ask(v, d);
+                    if (there && round) ask(v, d);
                 } else {
 #pragma unroll
                     for (int k = 0; k < U; ++k) v[k][0] = next[k][0], v[k][1] = next[k][1];
@@ -249,8 +250,8 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
         }
         if constexpr (BACK) {
             // the block's sums, in the order of the groups
-            float* const all = reinterpret_cast<float*>(angles);        // [groups][dim]
-            __syncthreads();
+            float* const all = reinterpret_cast<float*>(angles + kQkTokens * a.pairs);
+            __syncthreads();        // queries' have been read
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 const uint32_t unit = in + k * a.lanes;
@@ -485,7 +486,7 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
             const uint64_t most = std::min<uint64_t>(tokens, qk_most_blocks(ctx) / (few ? 2 : 1));
             a.per = static_cast<uint32_t>((tokens + most - 1) / most);
             blocks = static_cast<uint32_t>((tokens + a.per - 1) / a.per);
-            const uint32_t groups = 256 / a.lanes, lds = std::max(kQkTokens * a.pairs * static_cast<uint32_t>(sizeof(float2)), groups * dim * 4u);
+            const uint32_t groups = 256 / a.lanes, lds = kQkTokens * a.pairs * static_cast<uint32_t>(sizeof(float2)) + groups * dim * 4u;
             EDGC_LAUNCH(ctx, st, KID_QK_BACKWARD, 3.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim, 0.0,
                         k_qk_norm<T, n, u, true><<<dim3(blocks, 1, few ? 2 : 1), 256, lds, st>>>(a));
             EDGC_HIP_TRY(ctx, hipGetLastError());

@@ -172,6 +172,27 @@ def test_backward(ctx, case, interleaved, dtype):
         check_backward(dk, dw_k, dk_out, k, w_k, cos, sin, rot // 2, interleaved)
 
 
+@pytest.mark.parametrize("hk", [0, 2])
+@pytest.mark.parametrize("t", [255, 256, 257, 511, 512, 513, 1023, 1024, 1025, 2049, 9000])
+def test_tokens_where_the_blocks_are_dealt_out_otherwise(ctx, t, hk):
+    """Few tokens have blocks of queries and of keys, more have blocks of both, of one token or several."""
+    case = (t, 3, hk, 16, 8, "dense")
+    q, k, w_q, w_k, pos, f = inputs(case, F32)
+    dq_out, dk_out = randn((t, 3, 16), 6, F32), randn((t, hk, 16), 7, F32) if hk else None
+    cuda = lambda x: None if x is None else x.cuda()
+    like = lambda x: None if x is None else torch.full_like(x, 7.0, device="cuda")
+    out_q, out_k, dq, dk, dw_q, dw_k = like(q), like(k), like(q), like(k), like(w_q), like(w_k)
+    ctx.reserve_qk_norm(t, 3, hk, 16)
+    ctx.qk_norm_forward(cuda(q), cuda(k), cuda(w_q), cuda(w_k), cuda(pos), cuda(f), out_q, out_k, eps=EPS)
+    ctx.qk_norm_backward(cuda(dq_out), cuda(dk_out), cuda(q), cuda(k), cuda(w_q), cuda(w_k), cuda(pos), cuda(f), dq, dk, dw_q, dw_k, eps=EPS)
+    cos, sin = angles(pos, f, 16, False)
+    check_forward(out_q, q, w_q, cos, sin, 4, False)
+    check_backward(dq, dw_q, dq_out, q, w_q, cos, sin, 4, False)
+    if hk:
+        check_forward(out_k, k, w_k, cos, sin, 4, False)
+        check_backward(dk, dw_k, dk_out, k, w_k, cos, sin, 4, False)
+
+
 @pytest.mark.parametrize("far", [1 << 20, 1 << 31, 1 << 40])
 def test_far_positions(ctx, far):
     """Angles of a position are as exact as their product in 64 bits, far beyond what 32 bits or one double's digits of a circle hold."""
