@@ -36,20 +36,20 @@ struct QkArgs {
     float eps, inv_dim;
 };
 
-// N elements of a head: 16 bytes, or one
-template <typename T, int N> struct QkPack {
+// N elements of a head: 16 bytes, or one.  STREAM: past the caches
+template <typename T, int N, bool STREAM> struct QkPack {
     static_assert(N == Pack<T>::N, "");
     Pack<T> v;
-    __device__ __forceinline__ void load(const T* p, uint32_t len) { v.load(p, len); }
+    __device__ __forceinline__ void load(const T* p, uint32_t len) { v.template load<STREAM>(p, len); }
     __device__ __forceinline__ float get(int i) const { return v.get(i); }
     static __device__ __forceinline__ void store(T* p, uint32_t len, const float (&f)[N])
     {
         Pack<T> o;
         o.set(f);
-        o.store(p, len);
+        o.template store<STREAM>(p, len);
     }
 };
-template <typename T> struct QkPack<T, 1> {
+template <typename T> struct QkPack<T, 1, false> {
     float v;
     __device__ __forceinline__ void load(const T* p, uint32_t len) { v = len ? static_cast<float>(*p) : 0.f; }
     __device__ __forceinline__ float get(int) const { return v; }
@@ -130,9 +130,10 @@ __device__ __forceinline__ float qk_head_sum(float v, uint32_t lanes)
 }
 
 // A block has `per` tokens.  Few tokens: blockIdx.z: queries, keys; forward, blockIdx.y: a share of the heads
-template <typename T, int N, int U, bool BACK>
+template <typename T, int N, int U, bool BACK, bool STREAM>
 __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
 {
+    using Item = QkPack<T, N, STREAM>;
     extern __shared__ float2 angles[];          // [kQkTokens][pairs]; BACK: and [groups][dim] sums
     const uint32_t lane = threadIdx.x & 63, in = lane & (a.lanes - 1), group = (threadIdx.x / a.lanes), groups = 256 / a.lanes;
     const uint64_t t0 = static_cast<uint64_t>(blockIdx.x) * a.per, t1 = min(a.tokens, t0 + a.per);
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
         const QkHeads& h = a.h[K];
         const uint32_t share = (h.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share, h1 = min(h.heads, h0 + share), H = h1 > h0 ? h1 - h0 : 0u;
         float sums[U][2][BACK ? N : 1] = {};
-        QkPack<T, N> w[U][2];
+        Item w[U][2];
         if (H) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
             const uint32_t items = n * H, rounds = (items + groups - 1) / groups;      // (all lanes of a wave take part in the sums)
             const uint32_t some = max(H, 1u), tokens_on = groups / some, heads_on = groups - tokens_on * some;
             uint32_t it = group, tok = group / some, hd = group - tok * some;
-            QkPack<T, N> v[U][2], d[U][2], next[U][2];
-            auto ask = [&](QkPack<T, N> (&xs)[U][2], QkPack<T, N> (&ds)[U][2]) {
+            Item v[U][2], d[U][2], next[U][2];
+            auto ask = [&](Item (&xs)[U][2], Item (&ds)[U][2]) {
                 const uint64_t token = b0 + tok, head = h0 + hd;
                 const T* const x = static_cast<const T*>(h.x) + token * h.x_token + head * h.x_head;
                 const T* const dy = BACK ? static_cast<const T*>(h.dy) + token * h.dy_token + head * h.dy_head : nullptr;
@@ -243,8 +244,8 @@ __global__ __launch_bounds__(256, 4) void k_qk_norm(const QkArgs a)
                             }
                         }
                     if constexpr (!BACK) qk_turn<N, false>(a, u, turn, y[0], y[1]);
-                    QkPack<T, N>::store(out + u.first, len(unit, u.first), y[0]);
-                    QkPack<T, N>::store(out + u.second, len(unit, u.second), y[1]);
+                    Item::store(out + u.first, len(unit, u.first), y[0]);
+                    Item::store(out + u.second, len(unit, u.second), y[1]);
                 }
             }
         }
@@ -359,6 +360,17 @@ int by_head(const QkShape& s, QkArgs& a, F&& f)
     return s.dtype == EDGC_F32 ? go(float{}) : go(__bf16{});
 }
 
+// f(whether heads go past the caches): what moves more than 2^27 bytes is not there any more when it is next looked for.  (16384 tokens of 40 and 8 heads of 128,
+// bf16, 403 MB: 84.5 us through the caches, 81.5 past them; backward, 8192 tokens of 32 and 8, 251 MB: 58.5 and 55; 1001 of 7 and 3 of 72, fp32, 9 MB: 6.3 and
+// 7.4.)
+template <int N, typename F>
+int by_size(double bytes, F&& f)
+{
+    if constexpr (N > 1)
+        if (bytes > 134217728.0) return f(std::true_type{});
+    return f(std::false_type{});
+}
+
 QkHeads qk_heads(const edgc_heads* x, const edgc_heads* dy, const edgc_heads* out, const void* w, uint32_t heads)
 {
     QkHeads h{};
@@ -414,10 +426,13 @@ extern "C" int edgc_qk_norm_forward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t to
         const bool few = blocks < static_cast<uint32_t>(ctx->num_cu);
         const uint32_t shares = few ? std::max(1u, std::min((std::max(heads_q, heads_k) + groups - 1) / groups, 64u)) : 1u;
         const double bytes = 2.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim;
-        EDGC_LAUNCH(ctx, st, KID_QK_FORWARD, bytes, 0.0,
-                    k_qk_norm<T, n, u, false><<<dim3(blocks, shares, few && heads_k ? 2 : 1), 256, kQkTokens * std::max(1u, a.pairs) * sizeof(float2), st>>>(a));
-        EDGC_HIP_TRY(ctx, hipGetLastError());
-        return EDGC_OK;
+        return by_size<n>(bytes, [&](auto stream) -> int {
+            EDGC_LAUNCH(ctx, st, KID_QK_FORWARD, bytes, 0.0,
+                        k_qk_norm<T, n, u, false, stream>
+                        <<<dim3(blocks, shares, few && heads_k ? 2 : 1), 256, kQkTokens * std::max(1u, a.pairs) * sizeof(float2), st>>>(a));
+            EDGC_HIP_TRY(ctx, hipGetLastError());
+            return EDGC_OK;
+        });
     });
 }
 
@@ -487,9 +502,13 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
             a.per = static_cast<uint32_t>((tokens + most - 1) / most);
             blocks = static_cast<uint32_t>((tokens + a.per - 1) / a.per);
             const uint32_t groups = 256 / a.lanes, lds = kQkTokens * a.pairs * static_cast<uint32_t>(sizeof(float2)) + groups * dim * 4u;
-            EDGC_LAUNCH(ctx, st, KID_QK_BACKWARD, 3.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim, 0.0,
-                        k_qk_norm<T, n, u, true><<<dim3(blocks, 1, few ? 2 : 1), 256, lds, st>>>(a));
-            EDGC_HIP_TRY(ctx, hipGetLastError());
+            const double bytes = 3.0 * sizeof(T) * tokens * (heads_q + heads_k) * dim;
+            const int rc = by_size<n>(bytes, [&](auto stream) -> int {
+                EDGC_LAUNCH(ctx, st, KID_QK_BACKWARD, bytes, 0.0, k_qk_norm<T, n, u, true, stream><<<dim3(blocks, 1, few ? 2 : 1), 256, lds, st>>>(a));
+                EDGC_HIP_TRY(ctx, hipGetLastError());
+                return EDGC_OK;
+            });
+            if (rc) return rc;
         }
         EDGC_LAUNCH(ctx, st, KID_QK_SUM, 8.0 * blocks * dim, 0.0,
                     k_qk_sum<T><<<dim3((dim + 31) / 32, heads_k ? 2 : 1), 32 * kQkWays, 0, st>>>(a.part, blocks, dim, dw_q, dw_k));

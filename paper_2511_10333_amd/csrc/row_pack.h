@@ -9,6 +9,20 @@ typedef float f32x4_at __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_at __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4r __attribute__((ext_vector_type(4)));
 
+// STREAM: what is not read again soon, and need not stay in the caches
+template <bool STREAM, typename V>
+__device__ __forceinline__ V pack_read(const void* p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const V*>(p));
+    else return *static_cast<const V*>(p);
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void pack_write(void* p, V v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<V*>(p) = v;
+}
+
 // 16 bytes of a row in registers, as they stand in memory
 template <typename T> struct Pack;
 template <> struct Pack<float> {
@@ -20,10 +34,11 @@ template <> struct Pack<float> {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = __float_as_uint(f[i]);
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void load(const float* p, uint32_t len)
     {
         if (len == N) {
-            const f32x4_at x = *reinterpret_cast<const f32x4_at*>(p);
+            const f32x4_at x = pack_read<STREAM, f32x4_at>(p);
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = __float_as_uint(x[i]);
             return;
@@ -32,13 +47,14 @@ template <> struct Pack<float> {
         for (int i = 0; i < N; ++i)
             if (static_cast<uint32_t>(i) < len) v[i] = __float_as_uint(p[i]);
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void store(float* p, uint32_t len) const
     {
         if (len == N) {
             f32x4_at x;
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v[i]);
-            *reinterpret_cast<f32x4_at*>(p) = x;
+            pack_write<STREAM>(p, x);
             return;
         }
         for (int i = 0; i < N; ++i)
@@ -56,10 +72,11 @@ template <> struct Pack<__bf16> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), b2));
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void load(const __bf16* p, uint32_t len)
     {
         if (len == N) {
-            const u32x4_at x = *reinterpret_cast<const u32x4_at*>(p);
+            const u32x4_at x = pack_read<STREAM, u32x4_at>(p);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = x[i];
             return;
@@ -69,13 +86,14 @@ template <> struct Pack<__bf16> {
         for (int i = 0; i < N; ++i)
             if (static_cast<uint32_t>(i) < len) v[i / 2] |= static_cast<uint32_t>(q[i]) << (16 * (i & 1));
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void store(__bf16* p, uint32_t len) const
     {
         if (len == N) {
             u32x4_at x;
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = v[i];
-            *reinterpret_cast<u32x4_at*>(p) = x;
+            pack_write<STREAM>(p, x);
             return;
         }
         uint16_t* q = reinterpret_cast<uint16_t*>(p);

@@ -193,6 +193,42 @@ def test_tokens_where_the_blocks_are_dealt_out_otherwise(ctx, t, hk):
         check_backward(dk, dw_k, dk_out, k, w_k, cos, sin, 4, False)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rot", [0, 512])
+def test_what_is_larger_than_the_caches(ctx, rot, dtype):
+    """More than 2^27 bytes go past the caches: the same bits as a part of the tokens at a time, and the weights' gradients by the formulas."""
+    t, hq, hk, dim = (9500 if dtype is BF16 else 4750), 6, 2, 512
+    g = torch.Generator(device="cuda").manual_seed(3)
+    make = lambda h: torch.randn((t, h, dim), generator=g, device="cuda").to(dtype)
+    q, k, dq_out, dk_out = make(hq), make(hk), make(hq), make(hk)
+    w_q, w_k = [(1 + 0.2 * torch.randn(dim, generator=g, device="cuda")).to(dtype) for _ in range(2)]
+    pos = torch.randint(0, 5000, (t,), generator=g, device="cuda") if rot else None
+    f = frequencies(rot).cuda() if rot else None
+    ctx.reserve_qk_norm(t, hq, hk, dim)
+
+    def run(at):
+        some = lambda x: x[at].contiguous()
+        out = [torch.full_like(some(x), 7.0) for x in (q, k, q, k)]
+        dw = [torch.empty(dim, dtype=dtype, device="cuda") for _ in range(2)]
+        p = pos[at].contiguous() if rot else None
+        ctx.qk_norm_forward(some(q), some(k), w_q, w_k, p, f, out[0], out[1], eps=EPS)
+        ctx.qk_norm_backward(some(dq_out), some(dk_out), some(q), some(k), w_q, w_k, p, f, out[2], out[3], *dw, eps=EPS)
+        return out, dw
+
+    whole, dw = run(slice(0, t))
+    parts = [run(slice(i, min(i + 2000, t)))[0] for i in range(0, t, 2000)]
+    for i, x in enumerate(whole):
+        assert torch.equal(x, torch.cat([p[i] for p in parts]))
+    if rot:
+        return
+    for got, x, dy in ((dw[0], q, dq_out), (dw[1], k, dk_out)):
+        x, dy = x.double(), dy.double()
+        terms = dy * x * (x.square().mean(-1, keepdim=True) + EPS).rsqrt()
+        want = terms.sum((0, 1))
+        bound = terms.abs().sum((0, 1)) * (fp32(dim) + t * x.shape[1] * 2.0 ** -24) + want.abs() * torch.finfo(dtype).eps / 2
+        assert bool(((got.double() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("far", [1 << 20, 1 << 31, 1 << 40])
 def test_far_positions(ctx, far):
     """Angles of a position are as exact as their product in 64 bits, far beyond what 32 bits or one double's digits of a circle hold."""
