@@ -13,9 +13,9 @@ F32, BF16 = torch.float32, torch.bfloat16
 SEGMENT = {F32: 3, BF16: 5}         # steps on A between two A = X X^T
 
 
-def want(g, steps, scale=1.0, eps=1e-7, coefs=COEFS):
+def want(g, steps, scale=1.0, eps=1e-7, coefs=COEFS, device="cpu"):
     a, b, c = coefs
-    x = g.double().cpu()
+    x = g.double().to(device)
     x = x.view(1, -1) if x.dim() == 1 else x
     x = x / (x.norm() + eps)
     for _ in range(steps):
@@ -86,6 +86,19 @@ def test_one_matrix(shape, dtype):
     out = torch.full_like(g, 9.0)
     run([g], [out], dtype=dtype)
     check(out, want(g, 5), 5, dtype)
+
+
+@pytest.mark.parametrize("dtype, steps", [(F32, 5), (F32, 2), (BF16, 5), (BF16, 7), (BF16, 11)])
+@pytest.mark.parametrize("shapes", [[(1000, 4000)], [(2100, 2333), (4100, 1999)], [(3001, 3001)]], ids=str)
+def test_matrices_that_have_larger_tiles(shapes, dtype, steps):
+    """Whole and shared tiles of 128 and 256 (smaller matrices have tiles of 64), into rows that are not aligned."""
+    grads = [randn(s, 20 + i, dtype) for i, s in enumerate(shapes)]
+    wide = [torch.full((m, n + 3), 6.0, dtype=dtype, device="cuda") for m, n in shapes]
+    outs = [w[:, 1:1 + n] for w, (_, n) in zip(wide, shapes)]
+    run(grads, outs, steps=steps, dtype=dtype)
+    for g, o, w in zip(grads, outs, wide):
+        check(o, want(g, steps, device="cuda").cpu(), steps, dtype)
+        assert bool((w[:, 0] == 6.0).all()) and bool((w[:, -2:] == 6.0).all())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
