@@ -612,17 +612,21 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
  * decompressed gradient (in place); otherwise no output overlaps an input, and
  * no two entries have one output.
  * All products are on the smaller side of a matrix, of fp16 planes that hold 22
- * bits of every operand (bf16 gradients: all of theirs), summed in fp32; the
- * norm's squares and sums are in 64 bits.  A step's error counts twelve times
- * more after every further step on A instead of on X, so X is formed again after
- * three steps with EDGC_F32, five with EDGC_BF16.  The same list, reservation
- * and GPU give the same bits.  A gradient of zeros stays zeros; one with Inf or
+ * bits of every operand, summed in fp32; the norm's squares and sums are in 64
+ * bits.  What is wrong with A counts a^2 times more after every further step on
+ * A instead of on X, so X is formed again after three steps, or fewer where a^2
+ * is larger than with these coefficients; with EDGC_F32 at most two steps follow
+ * the last one.  fp32 updates are off by no more than some four times what the
+ * steps on X in fp32 are, bf16 ones by little more than their rounding, also
+ * where singular values lie far apart.  The same list, reservation and GPU give
+ * the same bits.  A gradient of zeros stays zeros; one with Inf or
  * NaN comes out as NaN throughout, and no other one with it.
  *   edgc_reserve_orthogonalize: scratch for lists of tensors none of which needs
  *     more than these do (not a hot call; smaller side s, larger l, rounded up to
- *     multiples of 64: 20 s^2 + 4 s l bytes for a matrix, with EDGC_BF16
- *     20 s^2 + 2 s l, and 4 s l more where X is formed again; up to ten
- *     matrices are worked on together, as many as the scratch holds).  What it
+ *     multiples of 64: 20 s^2 + 8 s l bytes for a matrix; up to ten matrices
+ *     are worked on together, as many as the scratch holds), and for calls of
+ *     any number of steps; for up to three (EDGC_BF16: five) steps, for calls
+ *     of up to three (five).  What it
  *     replaces, keeps and frees is as for edgc_reserve_block_norm; count = 0
  *     frees alone.
  *   edgc_orthogonalize_batch: scales: host, one per tensor, or NULL for 1.

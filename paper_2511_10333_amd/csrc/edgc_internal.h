@@ -143,6 +143,7 @@ struct OrthoScratch {
     double*  part = nullptr;        // sums of squares per block
     float*   f = nullptr;           // a matrix's factor (behind the sums)
     uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
+    uint32_t steps = 0;             // reserved for
 };
 
 // Scratch of the embedding's gradient (edgc_reserve_embed) and of that of the norms of queries and keys (edgc_reserve_qk_norm).

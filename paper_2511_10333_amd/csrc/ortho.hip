@@ -8,7 +8,7 @@
 //
 // and of the symmetric products half the tiles are made: of s^3 operations 4 a step, instead of 3 l / s + 1 in every step as written above.  A_k+1 by
 // products instead of from X carries its rounding errors on, a^2 = 12 times larger relative to the small singular values with each step, so segments are
-// bounded (segment_steps).  Operands are fp16 planes (ortho_gemm.h); every sum is in fp32.
+// bounded (ortho_plan).  Operands are fp16 planes (ortho_gemm.h); every sum is in fp32.
 //
 // Bounded by the matrix instructions at the clock that the power allows: the four matrices of a block of hidden 4096, bf16, take 17.2 ms, their products
 // 1.09 to 1.12 PFLOP/s (the library's of one fp16 product of 8192 a side: 1.08 to 1.12), of hidden 2048, fp32, 3.46 ms.  Small ones by launches that wait for
@@ -143,10 +143,18 @@ __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
 // host
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kOrthoMaxSide = 1u << 14, kOrthoMaxLong = 1u << 20, kOrthoMaxSteps = 64;
-// Steps of a segment at most.  The rounding errors of A_0, 2^-24 of its largest value, are 12^(n - 1) times larger in A_n-1 relative to what comes of the
-// smallest singular values, 2 / sqrt s of that in the norm: with 3 steps they stay below the fp32 sums' own, with 5 below 1e-4, an eighth of what bf16
-// rounds.
-constexpr uint32_t segment_steps(edgc_dtype dt) { return dt == EDGC_F32 ? 3 : 5; }
+// Steps of a segment at most, of the last one, and what its errors may grow by.  A_0 is off by some 2^-22 of its largest value (its sums of l products more than
+// its planes), which each further step on the same A makes w^2 larger relative to what comes of the smallest singular values, w the largest value of W:
+// 12, of 3.4445, so 141 in a segment of three.  Later steps grow fp32 products' own errors as well, what the last ones carry comes out as it is.  A
+// gradient of one direction above noise, 256 x 2048, bf16: five steps on one A were 1.5e-2 off, three and two 7e-4 with the output's rounding, which alone
+// is 6e-4 there.  fp32, over four decades, 512 x 512 and 16 x 32768: two and three 1.9e-5 and 1.6e-5, three and two 3.6e-6 and 1.1e-5, products of X in fp32
+// 2.0e-6 and 5.2e-6; three alone 1.0e-6 and 8.5e-6, two and one 6e-7 and 1.2e-6, products 4e-7 and 8e-7.
+constexpr uint32_t kOrthoSegment = 3;
+constexpr uint32_t ortho_last(edgc_dtype dt) { return dt == EDGC_F32 ? 2 : 3; }
+constexpr double kOrthoCarried = 150.0;
+
+// A reservation for up to so many steps is for calls of up to so many, one for more is for any
+constexpr uint32_t ortho_few(edgc_dtype dt) { return dt == EDGC_F32 ? 3 : 5; }
 
 uint64_t pad64(uint64_t n) { return (n + 63) / 64 * 64; }
 
@@ -158,25 +166,19 @@ struct OrthoShape {
     // 16-bit elements: X, the X of a later segment, five matrices of the smaller side
     uint64_t x_elems(uint32_t planes) const { return S * L * planes; }
     uint64_t side_elems() const { return S * S * 2; }
-    uint64_t elems(edgc_dtype dt, uint32_t segments) const
-    {
-        return x_elems(first_planes(dt, segments)) + (segments > 1 ? x_elems(2) : 0) + 5 * side_elems();
-    }
-    // (with three segments the second X comes where the first one was)
-    static uint32_t first_planes(edgc_dtype dt, uint32_t segments) { return dt == EDGC_F32 || segments > 2 ? 2 : 1; }
+    uint64_t elems() const { return 2 * x_elems(2) + 5 * side_elems(); }
     uint64_t tiles() const { const uint64_t t = (s + 255) / 256; return t * (t + 1) / 2; }
 };
-uint32_t segments_of(edgc_dtype dt, uint32_t steps) { return (steps + segment_steps(dt) - 1) / segment_steps(dt); }
 
 // Matrices i, i + 1, .. that are worked on together: as many as give the smaller side's products a few rounds of tiles, and fit
 template <typename F>
-uint32_t ortho_group(const edgc_ctx* ctx, edgc_dtype dt, uint32_t segments, uint32_t i, uint32_t count, uint64_t held, F&& shape_of, uint64_t* used)
+uint32_t ortho_group(const edgc_ctx* ctx, uint32_t i, uint32_t count, uint64_t held, F&& shape_of, uint64_t* used)
 {
     uint64_t elems = 0, tiles = 0;
     uint32_t k = 0;
     for (; i + k < count && k < kOrthoGroup; ++k) {
         const OrthoShape sh = shape_of(i + k);
-        const uint64_t e = sh.elems(dt, segments);
+        const uint64_t e = sh.elems();
         if (k && (e > held - elems || tiles >= 4ull * ctx->num_cu)) break;
         elems += e;
         tiles += sh.tiles();
@@ -221,20 +223,38 @@ struct OrthoCoefs {
 };
 constexpr double kOrthoMost = 1e9;      // beyond this the steps diverge
 
-// whether `steps` of them keep every matrix representable
-bool coefs_bounded(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps)
+// Which steps are made on one A
+struct OrthoPlan {
+    uint32_t steps, segments;
+    // the step that segment `seg` ends before: the longer segments come first
+    uint32_t end(uint32_t seg) const { return (steps * (seg + 1) + segments - 1) / segments; }
+};
+
+// Cuts `steps` of them into segments; false where they do not keep every matrix representable
+bool ortho_plan(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps, OrthoPlan* plan)
 {
-    double top = 1.0, q = 1.0;
-    const uint32_t segments = segments_of(dt, steps);
-    for (uint32_t seg = 0, done = 0; seg < segments; ++seg) {
-        q = 1.0;
-        for (const uint32_t end = steps * (seg + 1) / segments; done < end; ++done) {
-            double w, v, s;
-            co.most(top, w, v, s);
-            q *= w;
-            if (!(w <= kOrthoMost && v <= kOrthoMost && s <= kOrthoMost && s * s <= kOrthoMost && q <= kOrthoMost)) return false;
-            top = s;
+    double top = 1.0, w[kOrthoMaxSteps];
+    for (uint32_t k = 0; k < steps; ++k) {
+        double v, s;
+        co.most(top, w[k], v, s);
+        if (!(w[k] <= kOrthoMost && v <= kOrthoMost && s <= kOrthoMost && s * s <= kOrthoMost)) return false;
+        top = s;
+    }
+    auto fits = [&]() {
+        for (uint32_t seg = 0, k = 0; seg < plan->segments; ++seg) {
+            double q = 1.0, carried = 1.0;
+            for (const uint32_t end = plan->end(seg); k < end; ++k) {
+                q *= w[k];
+                if (k + 1 < end) carried *= w[k] * w[k];
+            }
+            if (!(q <= kOrthoMost && carried <= kOrthoCarried)) return false;
         }
+        return true;
+    };
+    for (uint32_t most = kOrthoSegment; most > 0; --most) {
+        const uint32_t last = std::min({most, ortho_last(dt), steps});
+        *plan = OrthoPlan{steps, 1 + (steps - last + most - 1) / most};
+        if (fits()) break;              // (single steps do)
     }
     return true;
 }
@@ -260,7 +280,8 @@ struct OrthoPass {
     edgc_dtype dt;
     const edgc_tensor* tensors;
     const float* scales;
-    uint32_t count, segments, steps;
+    uint32_t count;
+    OrthoPlan plan;
     double eps;
     OrthoCoefs co;
     struct Mat {
@@ -268,6 +289,7 @@ struct OrthoPass {
         uint16_t *x[2], *a, *v, *w[3];
         float* f;
     };
+    uint32_t first_planes() const { return dt == EDGC_F32 ? 2 : 1; }
     Mat mats[kOrthoGroup] = {};
     uint32_t n = 0;                             // of them
 
@@ -379,9 +401,9 @@ struct OrthoPass {
         if (int rc = dt == EDGC_F32 ? pack<float>(i0) : pack<__bf16>(i0)) return rc;
         double top = 1.0;
         int x_scale = 0;                        // of X; the first one's is in f
-        for (uint32_t seg = 0, done = 0; seg < segments; ++seg) {
-            const uint32_t end = steps * (seg + 1) / segments, from = seg % 2;
-            const bool first = seg == 0, single = first && OrthoShape::first_planes(dt, segments) == 1;
+        for (uint32_t seg = 0, done = 0; seg < plan.segments; ++seg) {
+            const uint32_t end = plan.end(seg), from = seg % 2;
+            const bool first = seg == 0, single = first && first_planes() == 1;
             // A = X X^T
             int a_scale = OrthoScale::of(top * top), q_scale = 0;
             {
@@ -431,7 +453,7 @@ struct OrthoPass {
                 top = s_top;
             }
             // X <- Q X
-            const bool out = seg + 1 == segments;
+            const bool out = seg + 1 == plan.segments;
             const int next_x = OrthoScale::of(top);
             OrthoArgs g{};
             for (uint32_t i = 0; i < n; ++i) {
@@ -479,8 +501,7 @@ struct OrthoPass {
         auto take = [&](uint64_t elems) { uint16_t* const p = at; at += elems; return p; };
         for (uint32_t i = 0; i < n; ++i) {
             Mat m{OrthoShape(tensors[i0 + i].m, tensors[i0 + i].n), {}, nullptr, nullptr, {}, nullptr};
-            m.x[0] = take(m.sh.x_elems(OrthoShape::first_planes(dt, segments)));
-            m.x[1] = segments > 1 ? take(m.sh.x_elems(2)) : nullptr;
+            for (uint16_t*& x : m.x) x = take(m.sh.x_elems(2));
             m.a = take(m.sh.side_elems());
             m.v = take(m.sh.side_elems());
             for (uint16_t*& w : m.w) w = take(m.sh.side_elems());
@@ -493,7 +514,7 @@ struct OrthoPass {
     {
         OrthoList list{};
         list.eps = eps;
-        const uint32_t planes = OrthoShape::first_planes(dt, segments);
+        const uint32_t planes = first_planes();
         double elems = 0.0;
         for (uint32_t i = 0; i < n; ++i) {
             const edgc_tensor& d = tensors[i0 + i];
@@ -561,15 +582,15 @@ extern "C" int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const
     for (uint32_t i = 0; i < count; ++i)
         if (int rc = check_shape(ctx, rows[i], cols[i])) return rc;
     EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
-    const uint32_t segments = count ? segments_of(dtype, steps) : 0;
     uint64_t need = 0;
     for (uint32_t i = 0; i < count;) {
         uint64_t used = 0;
-        i += ortho_group(ctx, dtype, segments, i, count, ~0ull, [&](uint32_t k) { return OrthoShape(rows[k], cols[k]); }, &used);
+        i += ortho_group(ctx, i, count, ~0ull, [&](uint32_t k) { return OrthoShape(rows[k], cols[k]); }, &used);
         need = std::max(need, used);
     }
     if (need && need <= ctx->ortho.held) {
         ctx->ortho.elems = need;
+        ctx->ortho.steps = steps;
         return EDGC_OK;
     }
     EDGC_HIP_TRY(ctx, hipDeviceSynchronize());          // nothing may still be using the old scratch
@@ -586,6 +607,7 @@ extern "C" int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const
     }
     ctx->ortho.f = reinterpret_cast<float*>(ctx->ortho.part + parts);
     ctx->ortho.elems = ctx->ortho.held = need;
+    ctx->ortho.steps = steps;
     return EDGC_OK;
 }
 
@@ -597,19 +619,20 @@ extern "C" int edgc_orthogonalize_batch(edgc_ctx* ctx, const edgc_tensor* tensor
     if (steps == 0 || steps > kOrthoMaxSteps) return fail(ctx, EDGC_EINVAL, "steps must be 1 to 64");
     if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(ctx, EDGC_EINVAL, "eps must be finite and not negative");
     const OrthoCoefs co{a, b, c};
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c) || !coefs_bounded(co, dtype, steps))
+    OrthoPlan plan{};
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c) || !ortho_plan(co, dtype, steps, &plan))
         return fail(ctx, EDGC_EINVAL, "coefficients must be finite, and so that the steps keep singular values bounded");
-    const uint32_t segments = segments_of(dtype, steps);
+    const uint32_t few = ortho_few(dtype);
     for (uint32_t i = 0; i < count; ++i) {
         if (int rc = check_shape(ctx, tensors[i].m, tensors[i].n)) return rc;
         if (scales && !std::isfinite(scales[i])) return fail(ctx, EDGC_EINVAL, "scales must be finite");
-        if (OrthoShape(tensors[i].m, tensors[i].n).elems(dtype, segments) > ctx->ortho.elems)
+        if (OrthoShape(tensors[i].m, tensors[i].n).elems() > ctx->ortho.elems || (steps > few && ctx->ortho.steps <= few))
             return fail(ctx, EDGC_EINVAL, "larger than what edgc_reserve_orthogonalize was called for");
     }
     EDGC_HIP_TRY(ctx, hipSetDevice(ctx->device));
-    OrthoPass pass{ctx, static_cast<hipStream_t>(hip_stream), dtype, tensors, scales, count, segments, steps, eps, co};
+    OrthoPass pass{ctx, static_cast<hipStream_t>(hip_stream), dtype, tensors, scales, count, plan, eps, co};
     for (uint32_t i = 0; i < count;) {
-        const uint32_t n = ortho_group(ctx, dtype, segments, i, count, ctx->ortho.elems, [&](uint32_t k) { return OrthoShape(tensors[k].m, tensors[k].n); }, nullptr);
+        const uint32_t n = ortho_group(ctx, i, count, ctx->ortho.elems, [&](uint32_t k) { return OrthoShape(tensors[k].m, tensors[k].n); }, nullptr);
         if (int rc = pass.group(i, n)) return rc;
         i += n;
     }
