@@ -27,7 +27,6 @@ struct OrthoProblem {
     uint64_t lda, ldb;                  // 16-bit elements from row to row
     uint32_t M, N;                      // of the output
     uint32_t ktiles;                    // tiles of k
-    uint32_t spread;                    // one plane of an operand that has two is taken
     uint32_t tiles_m, tiles_n;          // tiles of the output
     uint32_t rows, cols;                // of `out`, with what is padding: zeros
     uint16_t* out;                      // planes, or
@@ -234,20 +233,14 @@ __device__ __forceinline__ void ortho_sums(const OrthoProblem& p, unsigned char*
     static_assert(PA == PB || (PB == 1 && TB), "");
     const uint32_t wm = wave / 2, wn = wave % 2;
 
-    // Bytes from the tile's first element to the units of 16 that this thread brings (ff_place).  One plane of two: every other four units of a row.
-    const uint32_t spread = PA == 1 ? p.spread : 0u;
+    // Bytes from the tile's first element to the units of 16 that this thread brings (ff_place).
     uint32_t oa[LA], ob[LB];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-        oa[i] = ff_place<false, BM>(wave, lane, i, [](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
-        if constexpr (PA == 1) oa[i] += spread * (oa[i] & 64u);
-    }
+    for (int i = 0; i < LA; ++i) oa[i] = ff_place<false, BM>(wave, lane, i, [](uint32_t r) { return r; }, p.M - 1 - m0, static_cast<uint32_t>(p.lda));
 #pragma unroll
-    for (int i = 0; i < LB; ++i) {
+    for (int i = 0; i < LB; ++i)
         ob[i] = ff_place<TB, WIDTH>(wave, lane, i, [](uint32_t r) { return r; }, TB ? static_cast<uint32_t>(p.ldb) - 1 - n0 * PB : p.N - 1 - n0, static_cast<uint32_t>(p.ldb));
-        if constexpr (PA == 1) ob[i] += spread * (ob[i] & 64u);
-    }
-    const uint64_t a_step = 64u << spread, b_step = TB ? BK * p.ldb : a_step;
+    const uint64_t a_step = 64, b_step = TB ? BK * p.ldb : a_step;
     const uint16_t *pa = p.a + m0 * p.lda + kt0 * a_step, *pb = p.b + (TB ? static_cast<uint64_t>(n0) * PB : n0 * p.ldb) + kt0 * b_step;
     const uint32_t base = lds_address(lds) + wave * 1024;
     auto bring_a = [&](uint32_t buf, int i) { load_to_lds(pa, oa[i], base + buf * kBytesA + i * 4096); };
