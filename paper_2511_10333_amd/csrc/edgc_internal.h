@@ -141,7 +141,7 @@ struct OrthoScratch {
     void*    ws = nullptr;          // the matrices' planes, 16 bits an element
     float*   sums = nullptr;        // partial sums of tiles whose k is shared
     double*  part = nullptr;        // sums of squares per block
-    float*   f = nullptr;           // a matrix's factor (behind the sums)
+    void*    f = nullptr;           // the matrices' factors (behind the sums)
     uint64_t elems = 0, held = 0;   // reserved; of ws: that or more
     uint32_t steps = 0;             // reserved for
 };

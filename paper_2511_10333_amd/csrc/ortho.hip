@@ -29,7 +29,7 @@ struct OrthoItem {
     const void* src;
     uint16_t* x;                        // planes
     double* part;                       // per block
-    float* f;
+    OrthoFactor* f;
     uint64_t ld, ldx;
     uint32_t m, n, tiles_c, tiles, first, blocks, tall, _pad;
 };
@@ -84,8 +84,8 @@ __global__ __launch_bounds__(256) void k_ortho_sumsq(const OrthoList list)
     acc = ortho_block_sum(acc);
     if (threadIdx.x == 0) t.part[at] = acc;
 }
-// X = f 2^k G: 2^k G, whose norm is in [2^14, 2^15), as planes (P of them), f = 1 / ((norm + eps) 2^k) beside them.  Of a gradient that has a value
-// that is not finite f is NaN, and so is the whole update.
+// X = f 2^k G: 2^k G, whose norm is in [2^14, 2^15), as planes (P of them), f = 1 / ((norm + eps) 2^k) beside them (OrthoFactor).  Of a gradient that has a
+// value that is not finite f is NaN, and so is the whole update.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
 {
@@ -100,7 +100,14 @@ __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
         (void)frexp(norm, &k);
         k = 15 - k;
     }
-    if (at == 0 && threadIdx.x == 0) *t.f = norm < 1e300 ? (norm > 0.0 ? static_cast<float>(ldexp(1.0 / (norm + list.eps), -k)) : 0.f) : __builtin_nanf("");
+    if (at == 0 && threadIdx.x == 0) {
+        OrthoFactor f{norm < 1e300 ? 0.f : __builtin_nanf(""), 0};
+        if (norm > 0.0 && norm < 1e300) {
+            (void)frexp(norm / (norm + list.eps), &f.exponent);
+            f.value = static_cast<float>(ldexp(1.0 / (norm + list.eps), -k - f.exponent));
+        }
+        *t.f = f;
+    }
     auto put = [&](uint32_t row, uint32_t col, const float (&v)[4]) {         // of X
         f16x4 h, l;
 #pragma unroll
@@ -191,6 +198,14 @@ uint32_t ortho_group(const edgc_ctx* ctx, uint32_t i, uint32_t count, uint64_t h
 // most its largest eigenvalue, a polynomial's largest value over the singular values that there can be.
 struct OrthoScale {
     static int of(double most) { int e; (void)std::frexp(std::max(most * 1.1, 1e-6), &e); return 15 - e; }
+    // bits by which values that small ones have `grown` to may pass `most`
+    static int reach(double grown, double most)
+    {
+        const double ratio = grown / std::max(most, 1e-6);
+        int e = 0;
+        if (ratio > 1.0) (void)std::frexp(std::min(ratio, 1e300), &e);
+        return e;
+    }
 };
 
 struct OrthoCoefs {
@@ -287,7 +302,7 @@ struct OrthoPass {
     struct Mat {
         OrthoShape sh;
         uint16_t *x[2], *a, *v, *w[3];
-        float* f;
+        OrthoFactor* f;
     };
     uint32_t first_planes() const { return dt == EDGC_F32 ? 2 : 1; }
     Mat mats[kOrthoGroup] = {};
@@ -392,6 +407,7 @@ struct OrthoPass {
         p.rows = p.cols = static_cast<uint32_t>(m.sh.S);
         p.ktiles = static_cast<uint32_t>(m.sh.S / 32);
         p.alpha = static_cast<float>(alpha);
+        p.into = kOrthoPlain;
         return p;
     }
 
@@ -400,7 +416,8 @@ struct OrthoPass {
         place(i0, many);
         if (int rc = dt == EDGC_F32 ? pack<float>(i0) : pack<__bf16>(i0)) return rc;
         double top = 1.0;
-        int x_scale = 0;                        // of X; the first one's is in f
+        double grown = 1.0;                     // what singular values may have been multiplied by
+        int x_scale = 0, reach = kOrthoFirst;   // of X; the first one's scale is in f
         for (uint32_t seg = 0, done = 0; seg < plan.segments; ++seg) {
             const uint32_t end = plan.end(seg), from = seg % 2;
             const bool first = seg == 0, single = first && first_planes() == 1;
@@ -412,7 +429,7 @@ struct OrthoPass {
                     OrthoProblem p = symmetric(m, m.x[from], m.x[from], m.a, std::ldexp(1.0, a_scale - (first ? 0 : 2 * x_scale)));
                     p.lda = p.ldb = m.sh.L * (single ? 1 : 2);
                     p.ktiles = static_cast<uint32_t>(m.sh.L / (single ? 64 : 32));
-                    if (first) p.f = m.f, p.power = 2;
+                    p.f = m.f; p.power = 2; p.from = reach;
                     g.p[g.count++] = p;
                 }
                 if (int rc = single ? product<1, 1, false, void>(g, KID_ORTHO_GRAM) : product<2, 2, false, void>(g, KID_ORTHO_GRAM)) return rc;
@@ -424,6 +441,7 @@ struct OrthoPass {
                 double w_top, v_top, s_top;
                 co.most(top, w_top, v_top, s_top);
                 q *= w_top;
+                grown *= w_top;
                 const int w_scale = OrthoScale::of(w_top), v_scale = OrthoScale::of(v_top), next_a = OrthoScale::of(s_top * s_top), next_q = OrthoScale::of(q);
                 const uint32_t at_w = begin ? 0 : (at_q + 1) % 3, at_new = (at_q + 2) % 3;
                 OrthoArgs g{};
@@ -454,7 +472,7 @@ struct OrthoPass {
             }
             // X <- Q X
             const bool out = seg + 1 == plan.segments;
-            const int next_x = OrthoScale::of(top);
+            const int next_x = OrthoScale::of(top), next_reach = out ? kOrthoPlain : OrthoScale::reach(grown, top);
             OrthoArgs g{};
             for (uint32_t i = 0; i < n; ++i) {
                 const Mat& m = mats[i];
@@ -466,7 +484,7 @@ struct OrthoPass {
                 p.ktiles = static_cast<uint32_t>(m.sh.S / 32);
                 const double scale = out ? (scales ? scales[i0 + i] : 1.0) : std::ldexp(1.0, next_x);
                 p.alpha = static_cast<float>(std::ldexp(scale, -q_scale - (first ? 0 : x_scale)));
-                if (first) p.f = m.f, p.power = 1;
+                p.f = m.f; p.power = 1; p.from = reach; p.into = next_reach;
                 if (out) {
                     p.to = d.grad_out; p.ldo = d.ld_out; p.transposed = m.sh.tall;
                 } else {
@@ -477,6 +495,7 @@ struct OrthoPass {
             }
             if (int rc = apply(g, single, out)) return rc;
             x_scale = next_x;
+            reach = next_reach;
         }
         return EDGC_OK;
     }
@@ -505,7 +524,7 @@ struct OrthoPass {
             m.a = take(m.sh.side_elems());
             m.v = take(m.sh.side_elems());
             for (uint16_t*& w : m.w) w = take(m.sh.side_elems());
-            m.f = ctx->ortho.f + i;
+            m.f = static_cast<OrthoFactor*>(ctx->ortho.f) + i;
             mats[i] = m;
         }
     }
@@ -598,14 +617,14 @@ extern "C" int edgc_reserve_orthogonalize(edgc_ctx* ctx, edgc_dtype dtype, const
     if (need == 0) return EDGC_OK;
     const size_t parts = static_cast<size_t>(kOrthoGroup) * kOrthoParts;
     bool ok = hipMalloc(&ctx->ortho.ws, need * 2) == hipSuccess;
-    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.part), parts * sizeof(double) + kOrthoGroup * sizeof(float)) == hipSuccess;
+    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.part), parts * sizeof(double) + kOrthoGroup * sizeof(OrthoFactor)) == hipSuccess;
     ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->ortho.sums), ortho_sums_elems(ctx) * sizeof(float)) == hipSuccess;
     if (!ok) {
         (void)hipGetLastError();
         free_ortho(ctx);
         return fail(ctx, EDGC_ENOMEM, "scratch allocation of the orthogonalised update failed");
     }
-    ctx->ortho.f = reinterpret_cast<float*>(ctx->ortho.part + parts);
+    ctx->ortho.f = ctx->ortho.part + parts;
     ctx->ortho.elems = ctx->ortho.held = need;
     ctx->ortho.steps = steps;
     return EDGC_OK;

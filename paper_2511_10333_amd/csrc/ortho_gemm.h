@@ -22,6 +22,15 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
+// X = G / (|G| + eps) is as much smaller than one as eps is larger than the norm, and so are all later ones.  rho = |G| / (|G| + eps) < 2^exponent.  The first
+// X is 2^exponent value times the planes.  A later one, which is at most 2^reach times rho beside what its planes are scaled for, is held 2^-min(0,
+// exponent + reach) times larger.
+struct OrthoFactor {
+    float value;
+    int32_t exponent;
+};
+constexpr int32_t kOrthoFirst = INT32_MIN, kOrthoPlain = INT32_MAX;     // in the place of a reach: of the first X; of what is not scaled
+
 struct OrthoProblem {
     const uint16_t *a, *b;              // operands
     uint64_t lda, ldb;                  // 16-bit elements from row to row
@@ -29,13 +38,15 @@ struct OrthoProblem {
     uint32_t ktiles;                    // tiles of k
     uint32_t tiles_m, tiles_n;          // tiles of the output
     uint32_t rows, cols;                // of `out`, with what is padding: zeros
+    int32_t from;                       // see OrthoFactor
     uint16_t* out;                      // planes, or
     void* to;                           // the caller's matrix
     const uint16_t* e;                  // planes like `out`'s that are added, or null
-    const float* f;                     // what the sums are multiplied by, to the power `power`
+    const OrthoFactor* f;               // of X, or null
     uint64_t ldo;                       // of out and e (16-bit elements), or to
-    uint32_t power, transposed;         // transposed: to[n][m]
-    float alpha, beta, gamma;           // alpha f^power sum + beta e + gamma I
+    uint32_t power, transposed;         // how often X is in the product; transposed: to[n][m]
+    float alpha, beta, gamma;           // alpha (X's factor)^power sum + beta e + gamma I
+    int32_t into;                       // of an X that is written, or kOrthoPlain
 };
 constexpr uint32_t kOrthoProblems = 20;
 // Tiles are given out as in FfArgs: those of whole rounds of the compute units a block each, the others' steps of k in even shares to `workers` further
@@ -199,9 +210,14 @@ __device__ __forceinline__ void ortho_place(const OrthoProblem& p, uint32_t tile
 }
 __device__ __forceinline__ float ortho_factor(const OrthoProblem& p)
 {
+    if (!p.f) return p.alpha;
+    const OrthoFactor f = *p.f;
+    const bool first = p.from == kOrthoFirst;
+    auto held = [&](int32_t reach) { return reach == kOrthoPlain ? 0 : min(0, f.exponent + reach); };
     float factor = p.alpha;
-    for (uint32_t i = 0; i < p.power; ++i) factor *= *p.f;
-    return factor;
+    if (first)
+        for (uint32_t i = 0; i < p.power; ++i) factor *= f.value;
+    return ldexpf(factor, static_cast<int>(p.power) * (first ? f.exponent : held(p.from)) - held(p.into));
 }
 
 // k of a tile, bytes of either operand's tile in LDS, tiles of A and B that are there, all of LDS.  Blocks of 256 rows have a compute unit for themselves, of the
