@@ -482,8 +482,8 @@ struct OrthoPass {
                 p.lda = 2 * m.sh.S; p.ldb = m.sh.L * (single ? 1 : 2);
                 p.M = static_cast<uint32_t>(m.sh.s); p.N = static_cast<uint32_t>(m.sh.l);
                 p.ktiles = static_cast<uint32_t>(m.sh.S / 32);
-                const double scale = out ? (scales ? scales[i0 + i] : 1.0) : std::ldexp(1.0, next_x);
-                p.alpha = static_cast<float>(std::ldexp(scale, -q_scale - (first ? 0 : x_scale)));
+                p.alpha = static_cast<float>(std::ldexp(1.0, (out ? 0 : next_x) - q_scale - (first ? 0 : x_scale)));
+                p.beta = scales ? scales[i0 + i] : 1.0f;
                 p.f = m.f; p.power = 1; p.from = reach; p.into = next_reach;
                 if (out) {
                     p.to = d.grad_out; p.ldo = d.ld_out; p.transposed = m.sh.tall;

@@ -45,7 +45,7 @@ struct OrthoProblem {
     const OrthoFactor* f;               // of X, or null
     uint64_t ldo;                       // of out and e (16-bit elements), or to
     uint32_t power, transposed;         // how often X is in the product; transposed: to[n][m]
-    float alpha, beta, gamma;           // alpha (X's factor)^power sum + beta e + gamma I
+    float alpha, beta, gamma;           // alpha (X's factor)^power sum + beta e + gamma I; to: beta alpha (X's factor)^power sum
     int32_t into;                       // of an X that is written, or kOrthoPlain
 };
 constexpr uint32_t kOrthoProblems = 20;
@@ -123,12 +123,15 @@ __device__ __forceinline__ void ortho_store8(__bf16* row, uint32_t c, uint32_t n
 // part of LDS, so that eight neighbours of a row are stored together.  SYM: a square below the diagonal is stored as its transpose above it too, and one
 // above it not at all.
 constexpr uint32_t kOrthoRow = 36;      // floats: 32 and a pad that spreads the rows over the banks
-__device__ __forceinline__ void ortho_spread(float factor, const f32x16& acc, float* mine, uint32_t lane)
+template <typename T>
+__device__ __forceinline__ void ortho_spread(float factor, float scale, const f32x16& acc, float* mine, uint32_t lane)
 {
+    // the caller's scale by itself: the smallest ones would lose bits beside a factor of 2^-27
+    auto times = [&](float v) { return std::is_same<T, void>::value ? factor * v : factor * v * scale; };
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(mine + (lane & 31) * kOrthoRow + 8 * q + 4 * (lane >> 5)) =
-            float4{factor * acc[4 * q], factor * acc[4 * q + 1], factor * acc[4 * q + 2], factor * acc[4 * q + 3]};
+            float4{times(acc[4 * q]), times(acc[4 * q + 1]), times(acc[4 * q + 2]), times(acc[4 * q + 3])};
 }
 // alpha times the sums of a square, and what is added to them, still in the order of the registers: a loop of squares whose stores are on their way must
 // not load anything, or each waits for the last one's stores
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_ortho_gemm(const Ort
                 if (SYM && n_of(s) > m_of(s)) continue;
                 ff_each<I * J>([&](auto q) {
                     constexpr int k = decltype(q)::value;
-                    if (s == k) ortho_spread(factor, acc[k / J][k % J], mine, l);
+                    if (s == k) ortho_spread<T>(factor, p.beta, acc[k / J][k % J], mine, l);
                 });
                 ortho_square<SYM, T>(p, mine, l, m_of(s), n_of(s));
             }
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(256) void k_ortho_join(const OrthoArgs args)
         ortho_add(p, factor, acc, lane, m, n);
         factor = 1.0f;
     }
-    ortho_spread(factor, acc, mine, lane);
+    ortho_spread<T>(factor, p.beta, acc, mine, lane);
     ortho_square<SYM, T>(p, mine, lane, m, n);
 }
 

@@ -49,6 +49,15 @@ def randn(shape, std, dtype, seed=3):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("steps", [2, 5])
+@pytest.mark.parametrize("scale", [1e37, -1e30, 1e-25, -1e-30, 1e-35, 1e-37])
+def test_scales(scale, steps, dtype):
+    for shape in ((96, 160), (160, 96)):
+        g = randn(shape, 1e-3, dtype)
+        check(run(g, steps, scale), want(g, steps, scale, 1e-7))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("steps", [1, 3, 5, 7])
 @pytest.mark.parametrize("std, eps", [(1e-5, 1e-2), (1e-10, 1e-3), (1e-16, 1e-7), (1e-22, 1e-7), (1e-3, 1e25), (1e-30, 1e-7)])
 def test_an_eps_far_above_the_norm(std, eps, steps, dtype):
