@@ -687,7 +687,7 @@ int edgc_embed_backward(edgc_ctx* ctx, edgc_dtype dtype, const void* ids, int id
  * everything else in fp32; every output is rounded once, and the same call gives
  * the same bits.  q_out may be q, dq either of dq_out and q, with the same strides,
  * and so for keys.  tokens = 0 does nothing (backward: the weights' gradients
- * become zeros).
+ * become zeros; so does dw_k, where it is given, without heads of keys).
  * The backward pass needs scratch for the largest tokens, heads and
  * dim: edgc_reserve_qk_norm, which replaces, keeps and frees as
  * edgc_reserve_block_norm does.

@@ -470,7 +470,7 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
     const QkShape s{dtype, tokens, heads_q, heads_k, dim, rot};
     if (int rc = check_qk(ctx, s, w_q, w_k, positions, pos_bytes, inv_freq, eps)) return rc;
     const size_t esz = dtype == EDGC_F32 ? 4 : 2;
-    if (!dw_q || !aligned_to(dw_q, esz) || (heads_k && (!dw_k || !aligned_to(dw_k, esz)))) return fail(ctx, EDGC_EINVAL, "null or misaligned weight gradient");
+    if (!dw_q || !aligned_to(dw_q, esz) || (heads_k && !dw_k) || (dw_k && !aligned_to(dw_k, esz))) return fail(ctx, EDGC_EINVAL, "null or misaligned weight gradient");
     if (tokens) {
         for (const edgc_heads* h : {q, dq_out})
             if (int rc = check_heads(ctx, h, heads_q, s, false)) return rc;
@@ -511,7 +511,7 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
             if (rc) return rc;
         }
         EDGC_LAUNCH(ctx, st, KID_QK_SUM, 8.0 * blocks * dim, 0.0,
-                    k_qk_sum<T><<<dim3((dim + 31) / 32, heads_k ? 2 : 1), 32 * kQkWays, 0, st>>>(a.part, blocks, dim, dw_q, dw_k));
+                    k_qk_sum<T><<<dim3((dim + 31) / 32, dw_k ? 2 : 1), 32 * kQkWays, 0, st>>>(a.part, blocks, dim, dw_q, dw_k));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         return EDGC_OK;
     });
