@@ -312,7 +312,8 @@ int check_heads(edgc_ctx* ctx, const edgc_heads* h, uint32_t heads, const QkShap
     // no element twice: the nearer of the two dimensions a head or more apart, the other all of it
     const bool heads_near = h->head <= h->token;
     const uint64_t near_n = heads_near ? heads : s.tokens, far_n = heads_near ? s.tokens : heads, near = heads_near ? h->head : h->token, far = heads_near ? h->token : h->head;
-    const uint64_t span = near_n > 1 ? (near_n - 1) * near + s.dim : s.dim;
+    // (far is at most kMaxSpan: what passes that needs no exact span)
+    const uint64_t span = near_n > 1 ? (near > kMaxSpan / (near_n - 1) ? 2 * kMaxSpan : (near_n - 1) * near + s.dim) : s.dim;
     if ((near_n > 1 && near < s.dim) || (far_n > 1 && far < span)) return fail(ctx, EDGC_EINVAL, "heads that are written overlap");
     return EDGC_OK;
 }
