@@ -3,8 +3,7 @@
 //   forward   out[t] = scale table[ids[t] - first], zeros where that is no row of the table
 //   backward  dtable[v] = scale sum of dy[t] over the tokens t with ids[t] - first = v
 //
-// Bounded by memory; what is written goes past the caches (16384 tokens of 5120 bf16: 44.5 us, not 48; the gradient of 50000 words of 4096: 139, not 146).  The
-// backward pass sorts the tokens by row, so that a row's gradient is the sum of neighbours, in the tokens' order, and is written
+// Bounded by memory.  The backward pass sorts the tokens by row, so that a row's gradient is the sum of neighbours, in the tokens' order, and is written
 // once: the same bits for the same tokens, whatever ran before.  k_embed_sort leaves the order and where each row's tokens begin in it, k_embed_sum adds up
 // chunks of the order (a row whose tokens lie in several leaves a part in each) and writes the rows without a token, and k_embed_join adds up the parts.
 #include "row_pack.h"
@@ -52,8 +51,8 @@ __device__ __forceinline__ uint32_t embed_row(const EmbedArgs& a, uint64_t token
     return r < a.vocab ? static_cast<uint32_t>(r) : ~0u;
 }
 
-// A wave takes kEmbedCols columns of a token
-template <typename T, typename I>
+// A wave takes kEmbedCols columns of a token.  STREAM: what is written goes past the caches
+template <typename T, typename I, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_forward(const EmbedArgs a, uint32_t parts)
 {
     constexpr int N = Pack<T>::N;
@@ -77,7 +76,7 @@ __global__ __launch_bounds__(256) void k_embed_forward(const EmbedArgs a, uint32
         for (int i = 0; i < N; ++i) f[i] = row != ~0u ? a.scale * v[u].get(i) : 0.f;
         Pack<T> o;
         o.set(f);
-        o.template store<true>(dst + c0 + u * 64 * N, len(u));
+        o.template store<STREAM>(dst + c0 + u * 64 * N, len(u));
     }
 }
 
@@ -192,7 +191,8 @@ __global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const EmbedArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Their sums
+// Their sums, past the caches (4096 columns of bf16 with the list's norm behind them: 2000 rows 29.2 us, through the caches 30.5; 8000 76.8 and 75.5; 32000
+// 201 and 254)
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kEmbedChunk = 32, kSumAhead = 8;     // tokens of a wave at most; on their way at a time
 constexpr uint32_t kZeroRows = 8;                       // rows that a wave looks for tokens of
@@ -385,13 +385,18 @@ extern "C" int edgc_embed_forward(edgc_ctx* ctx, edgc_dtype dtype, const void* t
     a.ids = ids; a.first = first_id; a.tokens = tokens; a.table = table; a.out = out; a.ld_in = ld_table; a.ld_out = ld_out;
     a.vocab = vocab; a.hidden = hidden; a.scale = scale;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    auto go = [&](auto type, auto id) -> int {
+    // What the next operator can still find in the caches stays there: rows of 4096 bf16 and the norm of them take 48 us for 8192 tokens (past the caches 53), for
+    // 16384, 2^27 bytes, 103 (110), for 32768 220 (215).
+    auto launch = [&](auto type, auto id, auto stream) -> int {
         using T = decltype(type);
         const uint32_t parts = (hidden + kEmbedCols<T> - 1) / kEmbedCols<T>;
         EDGC_LAUNCH(ctx, st, KID_EMBED_FORWARD, 2.0 * sizeof(T) * tokens * hidden, 0.0,
-                    k_embed_forward<T, decltype(id)><<<embed_grid(tokens * parts), 256, 0, st>>>(a, parts));
+                    k_embed_forward<T, decltype(id), stream><<<embed_grid(tokens * parts), 256, 0, st>>>(a, parts));
         EDGC_HIP_TRY(ctx, hipGetLastError());
         return EDGC_OK;
+    };
+    auto go = [&](auto type, auto id) -> int {
+        return static_cast<double>(sizeof(type)) * tokens * hidden > 134217728.0 ? launch(type, id, std::true_type{}) : launch(type, id, std::false_type{});
     };
     if (dtype == EDGC_F32) return id_bytes == 8 ? go(float{}, int64_t{}) : go(float{}, int32_t{});
     return id_bytes == 8 ? go(__bf16{}, int64_t{}) : go(__bf16{}, int32_t{});
