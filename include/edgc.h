@@ -614,10 +614,10 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
  * All products are on the smaller side of a matrix, of fp16 planes that hold 22
  * bits of every operand, summed in fp32; the norm's squares and sums are in 64
  * bits.  What is wrong with A counts a^2 times more after every further step on
- * A instead of on X, so X is formed again after three steps, or fewer where a^2
- * is larger than with these coefficients; with EDGC_F32 at most two steps follow
- * the last one.  fp32 updates are off by no more than some four times what the
- * steps on X in fp32 are, bf16 ones by little more than their rounding, also
+ * A instead of on X, so X is formed again after two steps with EDGC_F32, three
+ * with EDGC_BF16, or fewer where a^2 is larger than with these coefficients.
+ * fp32 updates are about as far off as the same steps on X in fp32 (sides below
+ * 16: up to three times), bf16 ones little more than by their rounding, also
  * where singular values lie far apart.  The same list, reservation and GPU give
  * the same bits.  A gradient of zeros stays zeros; one with Inf or
  * NaN comes out as NaN throughout, and no other one with it.

@@ -150,15 +150,14 @@ __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
 // host
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kOrthoMaxSide = 1u << 14, kOrthoMaxLong = 1u << 20, kOrthoMaxSteps = 64;
-// Steps of a segment at most, of the last one, and what its errors may grow by.  A_0 is off by some 2^-22 of its largest value (its sums of l products more than
-// its planes), which each further step on the same A makes w^2 larger relative to what comes of the smallest singular values, w the largest value of W:
-// 12, of 3.4445, so 141 in a segment of three.  Later steps grow fp32 products' own errors as well, what the last ones carry comes out as it is.  A
-// gradient of one direction above noise, 256 x 2048, bf16: five steps on one A were 1.5e-2 off, three and two 7e-4 with the output's rounding, which alone
-// is 6e-4 there.  fp32, over four decades, 512 x 512 and 16 x 32768: two and three 1.9e-5 and 1.6e-5, three and two 3.6e-6 and 1.1e-5, products of X in fp32
-// 2.0e-6 and 5.2e-6; three alone 1.0e-6 and 8.5e-6, two and one 6e-7 and 1.2e-6, products 4e-7 and 8e-7.
-constexpr uint32_t kOrthoSegment = 3;
-constexpr uint32_t ortho_last(edgc_dtype dt) { return dt == EDGC_F32 ? 2 : 3; }
-constexpr double kOrthoCarried = 150.0;
+// Steps of a segment at most, and what its errors may grow by.  A_0 is off by some 2^-22 of its largest value (its sums of l products as well as its
+// planes), which each further step on the same A makes w^2 larger relative to what comes of the smallest singular values, w the largest value of W: 12, of
+// 3.4445.  bf16, three: a gradient of one direction above noise, 256 x 2048, was 1.5e-2 off with five steps on one A, with three and two it is 7e-4 with
+// the output's rounding, which alone is 6e-4 there.  fp32, two: of 460 lists of all sizes six are more than 1.5 times and 1e-6 further off than fp32
+// products in X itself, up to 3 times, matrices of a side of 13 or less; with three and two 19 of 60, up to 3.5 times; five single steps: up to 1.3
+// times.  A block of hidden 2048 takes 4.0 ms, with three and two 3.45.
+constexpr uint32_t ortho_most(edgc_dtype dt) { return dt == EDGC_F32 ? 2 : 3; }
+constexpr double ortho_carried(edgc_dtype dt) { return dt == EDGC_F32 ? 12.0 : 145.0; }
 
 // A reservation for up to so many steps is for calls of up to so many, one for more is for any
 constexpr uint32_t ortho_few(edgc_dtype dt) { return dt == EDGC_F32 ? 3 : 5; }
@@ -262,13 +261,12 @@ bool ortho_plan(const OrthoCoefs& co, edgc_dtype dt, uint32_t steps, OrthoPlan* 
                 q *= w[k];
                 if (k + 1 < end) carried *= w[k] * w[k];
             }
-            if (!(q <= kOrthoMost && carried <= kOrthoCarried)) return false;
+            if (!(q <= kOrthoMost && carried <= ortho_carried(dt))) return false;
         }
         return true;
     };
-    for (uint32_t most = kOrthoSegment; most > 0; --most) {
-        const uint32_t last = std::min({most, ortho_last(dt), steps});
-        *plan = OrthoPlan{steps, 1 + (steps - last + most - 1) / most};
+    for (uint32_t most = ortho_most(dt); most > 0; --most) {
+        *plan = OrthoPlan{steps, (steps + most - 1) / most};
         if (fits()) break;              // (single steps do)
     }
     return true;

@@ -35,6 +35,8 @@ def gradient(kind, s, l):
         return (randn((s, 8), 1) * 0.3 ** torch.arange(8, dtype=torch.float64)) @ randn((8, l), 2) + 1e-3 * randn((s, l), 3)
     if kind == "one, rounded":                              # (bf16's own roundings are the other directions)
         return randn((s, 1), 1) @ randn((1, l), 2)
+    if kind == "many above noise":
+        return (randn((s, 32), 1) * 0.8 ** torch.arange(32, dtype=torch.float64)) @ randn((32, l), 2) + randn((s, l), 3)
     u, v = torch.linalg.qr(randn((s, s), 1))[0], torch.linalg.qr(randn((l, s), 2))[0]
     return (u * 10.0 ** (-4 * torch.linspace(0, 1, s, dtype=torch.float64))) @ v.t()       # evenly over four decades
 
@@ -85,6 +87,19 @@ def test_fp32_updates_are_off_by_a_few_times_what_fp32_products_are(s, l, kind, 
     assert off <= 4 * plain, (off, plain)
 
 
+@pytest.mark.parametrize("steps", [5, 3, 6])
+@pytest.mark.parametrize("s, l", [(62, 192), (64, 98), (64, 1152), (128, 512), (250, 250), (512, 2048)])
+def test_fp32_updates_of_many_directions_above_noise(s, l, steps):
+    """Where no direction is far below the others, fp32 products are off by little, and two steps on the same A by no more than twice that; and both operands of the
+    last product, Q and X, are rounded to 22 bits and the residual's sign, 2^-23 of it each, which fp32 operands are not."""
+    g = gradient("many above noise", s, l).float()
+    want = steps_of(g, steps)
+    rel = lambda x: float((x.double().cpu() - want).norm() / want.norm())
+    plain, off = rel(steps_of(g, steps, dtype=F32)), rel(run(g.cuda(), steps))
+    print(f"{s}x{l} many above noise, {steps} steps: {off:.2e}, fp32 products {plain:.2e}")
+    assert off <= 2 * plain + 2.0 ** -22, (off, plain)
+
+
 @pytest.mark.parametrize("steps", [3, 2, 5])
 @pytest.mark.parametrize("coefs", [(5.0, -20.0, 16.0), (-5.0, 20.0, -16.0), (4.1, -7.4, 3.25)])
 def test_coefficients_that_carry_errors_further(coefs, steps):
@@ -99,7 +114,7 @@ def test_coefficients_that_carry_errors_further(coefs, steps):
 
 @pytest.mark.parametrize("kind", ["one above noise", "four decades"])
 def test_large_matrices(kind):
-    """Tiles of 128, sums that are not shared."""
+    """Tiles of 128."""
     g = gradient(kind, 1500, 3000).float()
     want = steps_of(g, 5)
     rel = lambda x: float((x.double().cpu() - want).norm() / want.norm())
