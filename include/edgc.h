@@ -612,23 +612,23 @@ int edgc_ff_backward(edgc_ctx* ctx, const edgc_ff* w, const void* x, uint64_t ld
  * decompressed gradient (in place); otherwise no output overlaps an input, and
  * no two entries have one output.
  * All products are on the smaller side of a matrix, of fp16 planes that hold 22
- * bits of every operand, summed in fp32; the norm's squares and sums are in 64
- * bits.  What is wrong with A counts a^2 times more after every further step on
- * A instead of on X, so X is formed again after two steps with EDGC_F32, three
- * with EDGC_BF16, or fewer where a^2 is larger than with these coefficients.
- * fp32 updates are about as far off as the same steps on X in fp32 (sides below
- * 16: up to three times), bf16 ones little more than by their rounding, also
- * where singular values lie far apart.  The same list, reservation and GPU give
- * the same bits.  A gradient of zeros stays zeros; one with Inf or
- * NaN comes out as NaN throughout, and no other one with it.
+ * bits of every operand, but nothing below 2^-39 of the gradient's norm (bf16
+ * gradients: all bits of elements above 2^-31 of it), summed in fp32; the norm's
+ * squares and sums are in 64 bits.  What is wrong with A counts a^2 times more
+ * after every further step on A instead of on X, so X is formed again after two
+ * steps with EDGC_F32, three with EDGC_BF16, or fewer where a^2 is larger than
+ * with these coefficients.  fp32 updates are about as far off as the same steps
+ * on X in fp32 (sides below 16: up to three times), bf16 ones little more than
+ * by their rounding, also where singular values lie far apart.  The same list,
+ * reservation and GPU give the same bits.  A gradient of zeros stays zeros; one
+ * with Inf or NaN comes out as NaN throughout, and no other one with it.
  *   edgc_reserve_orthogonalize: scratch for lists of tensors none of which needs
  *     more than these do (not a hot call; smaller side s, larger l, rounded up to
- *     multiples of 64: 20 s^2 + 8 s l bytes for a matrix; up to ten matrices
- *     are worked on together, as many as the scratch holds), and for calls of
- *     any number of steps; for up to three (EDGC_BF16: five) steps, for calls
- *     of up to three (five).  What it
- *     replaces, keeps and frees is as for edgc_reserve_block_norm; count = 0
- *     frees alone.
+ *     multiples of 64: 20 s^2 + 8 s l bytes for a matrix; up to ten matrices are
+ *     worked on together, as many as the scratch holds).  One for up to three
+ *     steps (EDGC_BF16: five) is for calls of up to three (five), one for more
+ *     for any.  What it replaces, keeps and frees is as for
+ *     edgc_reserve_block_norm; count = 0 frees alone.
  *   edgc_orthogonalize_batch: scales: host, one per tensor, or NULL for 1.
  * Errors: EDGC_EINVAL as for edgc_clip_batch, and for a smaller side over 2^14
  * or a larger one over 2^20, steps 0 or over 64, an eps that is negative or not

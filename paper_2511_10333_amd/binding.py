@@ -927,8 +927,8 @@ class Context:
                 raise ValueError(f"tensors must be on the context's device, cuda:{self.device}")
 
     def embed_forward(self, table, ids, out, scale: float = 1.0, first_id: int = 0, stream=None) -> None:
-        """edgc_embed_forward: out[t] = scale * table[ids[t] - first_id], zeros for an id that is not in the table; ``ids``: int32 or
-        int64, contiguous."""
+        """edgc_embed_forward: out[t] = scale * table[ids[t] - first_id], zeros for an id that is not in the table; ``ids``: a contiguous
+        vector of int32 or int64 (of a batch of sequences, ``ids.view(-1)``)."""
         if table.dim() != 2:
             raise ValueError("table must be vocab x hidden")
         (vocab, hidden), dtype = table.shape, table.dtype

@@ -10,9 +10,9 @@
 // products instead of from X carries its rounding errors on, a^2 = 12 times larger relative to the small singular values with each step, so segments are
 // bounded (ortho_plan).  Operands are fp16 planes (ortho_gemm.h); every sum is in fp32.
 //
-// Bounded by the matrix instructions at the clock that the power allows: the four matrices of a block of hidden 4096, bf16, take 17.2 ms, their products
-// 1.09 to 1.12 PFLOP/s (the library's of one fp16 product of 8192 a side: 1.08 to 1.12), of hidden 2048, fp32, 3.46 ms.  Small ones by launches that wait for
-// each other: a block of hidden 512 has 21 in 220 us.
+// Bounded by the matrix instructions at the clock that the power allows: the four matrices of a block of hidden 4096, bf16, take 21.2 ms, their products
+// 1.06 to 1.16 PFLOP/s (the library's of one fp16 product of 8192 a side: 1.08 to 1.12), of hidden 2048, fp32, 4.0 ms.  Small ones by launches that wait for
+// each other: a block of hidden 512 has 22 in 226 us.
 #include "ortho_gemm.h"
 
 #include <algorithm>

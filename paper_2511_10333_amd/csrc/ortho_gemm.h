@@ -2,15 +2,17 @@
 //
 // A value x, scaled by a power of two that keeps it below 2^15, is hi + lo, hi = fp16(x), lo = fp16(x - hi): 22 bits of it and the residual's sign, and
 // an absolute 2^-25 at least (the matrix instructions take subnormal numbers as they are).  Three products, lo hi, hi lo and hi hi, are summed in fp32;
-// the fourth is left out: below 2^-24 of the product, of either sign.  bf16 inputs are one plane, exactly.  (bf16 planes would take three and six.)
+// the fourth is left out: below 2^-24 of the product, of either sign.  bf16 inputs are one plane: all bits of those above 2^-17,
+// beside a matrix's norm of 2^14.  (bf16 planes would take three and six.)
 //
 // The planes lie next to each other: 32 neighbours of a row's hi, then their lo, 128 bytes.  A tile of 32 k of both is 64 columns of memory, and a
 // step's fragments are read from LDS once for its three products.  (As three sums over k, with each plane brought and read twice, a hidden-2048 block took
 // 4.64 ms instead of 3.80 at the time.)
 //
 // The two small products have a sum of their own.  An MFMA adds its 16 k to the sum in several roundings, and the errors of these, not of the planes, are
-// what an update is off by: with all three products in one sum it was 3.4e-6 off for a block of hidden 512 and 3.7e-6 for odd matrices up to 2731, where
-// fp32 products are 2.5e-6 and 2.2e-6; with two sums 1.6e-6 and 1.8e-6.
+// what an update is off by: with all three products in one sum and X formed again after two steps, then three, it was 3.4e-6 off for a block of hidden 512 and
+// 3.7e-6 for odd matrices up to 2731, where fp32 products are 2.5e-6 and 2.2e-6; with two sums 1.6e-6 and 1.8e-6.  (Sums that begin anew with every tile of k
+// took a hidden-2048 block from 3.45 to 5.25 ms, for errors a quarter to a half smaller.)
 #pragma once
 
 #include "ff_gemm.h"

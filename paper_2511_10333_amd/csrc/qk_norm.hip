@@ -497,7 +497,7 @@ extern "C" int edgc_qk_norm_backward(edgc_ctx* ctx, edgc_dtype dtype, uint64_t t
         using T = decltype(type);
         uint32_t blocks = 0;
         if (tokens) {
-            // few tokens: queries and keys in blocks of their own (1001 tokens of 7 and 3 heads of 72: 5.4 us, with both in turn 9.2)
+            // few tokens: queries and keys in blocks of their own (1001 tokens of 7 and 3 heads of 72: 5.8 us, with both in turn 9.2)
             const bool few = tokens <= qk_most_blocks(ctx) && heads_k;
             const uint64_t most = std::min<uint64_t>(tokens, qk_most_blocks(ctx) / (few ? 2 : 1));
             a.per = static_cast<uint32_t>((tokens + most - 1) / most);
