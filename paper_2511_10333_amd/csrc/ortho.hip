@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256) void k_ortho_pack(const OrthoList list)
 constexpr uint32_t kOrthoMaxSide = 1u << 14, kOrthoMaxLong = 1u << 20, kOrthoMaxSteps = 64;
 // Steps of a segment at most, and what its errors may grow by.  A_0 is off by some 2^-22 of its largest value (its sums of l products as well as its
 // planes), which each further step on the same A makes w^2 larger relative to what comes of the smallest singular values, w the largest value of W: 12, of
-// 3.4445.  bf16, three: a gradient of one direction above noise, 256 x 2048, was 1.5e-2 off with five steps on one A, with three and two it is 7e-4 with
-// the output's rounding, which alone is 6e-4 there.  fp32, two: of 460 lists of all sizes six are more than 1.5 times and 1e-6 further off than fp32
-// products in X itself, up to 3 times, matrices of a side of 13 or less; with three and two 19 of 60, up to 3.5 times; five single steps: up to 1.3
-// times.  A block of hidden 2048 takes 4.0 ms, with three and two 3.45.
+// 3.4445.  bf16, three: of a gradient of one direction above noise, 256 x 2048, five steps on one A were 9.9e-3 off in the directions of its rows, three and two
+// are 7.4e-4, the output's rounding alone 6e-4.  fp32, two: of 460 lists of all sizes seven are more than 1.5 times and 1e-6 further off than fp32 products
+// in X itself, up to 3 times, matrices of a side of 13 or less; with three and two 19 of 60, up to 3.5 times; five single steps: none of 60.  A block of
+// hidden 2048 takes 4.0 ms, with three and two 3.45.
 constexpr uint32_t ortho_most(edgc_dtype dt) { return dt == EDGC_F32 ? 2 : 3; }
 constexpr double ortho_carried(edgc_dtype dt) { return dt == EDGC_F32 ? 12.0 : 145.0; }
 

@@ -11,8 +11,8 @@
 //
 // The two small products have a sum of their own.  An MFMA adds its 16 k to the sum in several roundings, and the errors of these, not of the planes, are
 // what an update is off by: with all three products in one sum and X formed again after two steps, then three, it was 3.4e-6 off for a block of hidden 512 and
-// 3.7e-6 for odd matrices up to 2731, where fp32 products are 2.5e-6 and 2.2e-6; with two sums 1.6e-6 and 1.8e-6.  (Sums that begin anew with every tile of k
-// took a hidden-2048 block from 3.45 to 5.25 ms, for errors a quarter to a half smaller.)
+// 3.7e-6 for odd matrices up to 2731, where fp32 products are 2.5e-6 and 2.2e-6; with two sums 1.6e-6 and 1.8e-6, and with an X every two steps
+// 1.2e-6 and 0.9e-6.  (Sums that begin anew with every tile of k took a hidden-2048 block from 3.45 to 5.25 ms, for errors a quarter to a half smaller.)
 #pragma once
 
 #include "ff_gemm.h"
